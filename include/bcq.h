@@ -263,6 +263,105 @@ bcq_status bcq_gemm_skinny(const bcq_desc *desc, const void *packed,
                            void *stream);
 
 /*
+ * ---- Serving: what stands between the stacked q/k/v projection and the output projection of a decoder block ----
+ *
+ * Three operators beside the binary-coded layers, for a batch of requests that each bring one new token, a few or a chunk:
+ * low-rank adapters of many requests (bcq_lora), norms of q and k per head with the position rotation and the append to a
+ * paged cache in one pass (bcq_rotate), attention over that cache (bcq_attend).  Elements are binary16 or bfloat16
+ * (bcq_dtype; 16-bit patterns behind void *), sums, statistics and norms are binary32, each result is rounded once, to
+ * nearest even.  Index arrays are DEVICE int32; the host does not see their values, so what they hold is bounded in the
+ * kernels: no value of theirs makes a kernel read or write outside the buffers described here.
+ */
+typedef enum { BCQ_F16 = 0, BCQ_BF16 = 1 } bcq_dtype;
+
+/* Largest head dimension and adapter rank (both in multiples of 8). */
+#define BCQ_MAX_HEAD_DIM 256
+#define BCQ_MAX_RANK 256
+
+/*
+ * A paged cache of keys and values (HOST, plain data).  Slot s of the cache is offset s % page_size of page s / page_size;
+ * its key for head h is the head_dim elements from k + (s / page_size) * page_stride + h * head_stride + (s % page_size) *
+ * slot_stride, its value the same place of v.  Strides are in elements, multiples of 8.
+ *   head_dim   a multiple of 8, at most BCQ_MAX_HEAD_DIM
+ *   page_size  a power of two, at most 65536 (others are BCQ_ERR_UNSUPPORTED)
+ * page_size * slot_stride must be below 2^30; pages may lie further apart than 2^31 elements.
+ */
+typedef struct bcq_cache {
+    int32_t dtype;
+    int32_t kv_heads, head_dim;
+    int32_t page_size, num_pages;
+    int64_t page_stride, head_stride, slot_stride;
+} bcq_cache;
+
+/*
+ * Norm of every q and k head, rotation by the token's position, append of k and v to the cache, in one pass over what the
+ * stacked projection left:
+ *     n = x * weight / sqrt(mean(x^2) + eps)        per head of head_dim elements; n = x where the weight is NULL
+ *     (n_a, n_b) -> (n_a cos - n_b sin, n_b cos + n_a sin)   pair i of rot_dim / 2: elements i and i + rot_dim / 2, or
+ *                                                   2 i and 2 i + 1 if interleaved; elements from rot_dim on stay
+ * q heads go to q_out, k heads to the cache, v heads to the cache as they are.
+ *   qkv       DEVICE [tokens] rows of q_heads, then kv_heads k heads, then kv_heads v heads; row stride ld_qkv
+ *   positions DEVICE [tokens]; bounded to 0 .. max_position - 1
+ *   cos_sin   DEVICE [max_position][rot_dim] binary32: rot_dim / 2 cosines, then as many sines; NULL iff rot_dim = 0
+ *   q_weight, k_weight DEVICE [head_dim] of the cache's type, or NULL (no norm of these heads)
+ *   q_out     DEVICE, row stride ld_q >= q_heads * head_dim; may be qkv itself with ld_q = ld_qkv
+ *   slots     DEVICE [tokens]: the token's slot; a value outside the cache (-1) means its k and v are not stored.  Tokens
+ *             of one call have different slots.
+ * Pointers 16-byte aligned (cos_sin 4), ld_qkv and ld_q multiples of 8, rot_dim even and at most head_dim, eps >= 0.
+ * tokens = 0 launches nothing.
+ */
+bcq_status bcq_rotate(const bcq_cache *cache, int32_t tokens, int32_t q_heads, const void *qkv, int64_t ld_qkv,
+                      const int32_t *positions, const float *cos_sin, int32_t max_position, int32_t rot_dim,
+                      int32_t interleaved, const void *q_weight, const void *k_weight, float eps, void *q_out, int64_t ld_q,
+                      const int32_t *slots, void *k_cache, void *v_cache, void *stream);
+
+/*
+ * Attention of new tokens over the cache.  Request r has the new tokens q_start[r] .. q_start[r+1] - 1 (rows of q) and
+ * kv_len[r] keys in the cache, its new tokens' own ones the last of them; key j of it is slot
+ * pages[r][j / page_size] * page_size + j % page_size.  Token i of its n new tokens has position p = kv_len[r] - n + i and
+ * sees the keys j < kv_len[r] with j <= p (causal) and j > p - window (window > 0, causal only):
+ *     out = sum_j softmax_j(scale * q . k_j) v_j
+ * Query head h uses the cache's head h / (q_heads / kv_heads).  A token that sees no key gets zeros; keys that a token does
+ * not see have no part in its result whatever they hold (infinities and NaN too).
+ *   q, out    DEVICE [tokens] rows of q_heads * head_dim, strides ld_q, ld_out (multiples of 8), 16-byte aligned
+ *   q_start   DEVICE [requests + 1], kv_len DEVICE [requests]
+ *   pages     DEVICE [requests] rows of max_pages page numbers, row stride max_pages; kv_len[r] <= max_pages * page_size
+ *   max_new   no request has more new tokens than this (those behind it are not computed)
+ *   scale     > 0
+ *   workspace DEVICE, bcq_attend_workspace_bytes(...) bytes, 16-byte aligned; scratch, no init, used by one call at a time
+ * tokens = 0 or requests = 0 launches nothing.
+ */
+size_t bcq_attend_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_new);
+bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v_cache, int32_t tokens, int32_t requests,
+                      int32_t q_heads, const void *q, int64_t ld_q, const int32_t *q_start, const int32_t *kv_len,
+                      const int32_t *pages, int32_t max_pages, int32_t max_new, float scale, int32_t causal, int32_t window,
+                      void *out, int64_t ld_out, void *workspace, void *stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared projection of N inputs and M outputs:
+ *     Y[t] = base[t] + scale[a] * B[a] (A[a] X[t]),   a = adapter[t];   Y[t] = base[t] where a is outside 0 .. count - 1
+ *   A       DEVICE [count][max_rank][N], B DEVICE [count][M][max_rank]; only the first rank[a] rows of A[a] and columns of
+ *           B[a] belong to the adapter, the others have no part in the result whatever they hold
+ *   rank    DEVICE [count] int32, bounded to 0 .. max_rank, or NULL (max_rank for all)
+ *   scale   DEVICE [count] binary32, or NULL (1 for all)
+ *   adapter DEVICE [tokens] int32
+ *   X       DEVICE [tokens] rows of N, stride ldx;  base, Y DEVICE [tokens] rows of M, strides ld_base, ldy; Y may be base
+ *   workspace DEVICE, bcq_lora_workspace_bytes(desc, tokens) bytes, 16-byte aligned; scratch, no init
+ * N and max_rank multiples of 8, max_rank at most BCQ_MAX_RANK; A, B, X 16-byte aligned, ldx a multiple of 8; base and Y
+ * aligned to 2 bytes, any M and strides (multiples of 8 elements and 16 bytes are faster).  tokens = 0 launches nothing.
+ */
+typedef struct bcq_adapters {
+    int32_t dtype;
+    int32_t count, max_rank;
+    int32_t M, N;
+} bcq_adapters;
+
+size_t bcq_lora_workspace_bytes(const bcq_adapters *desc, int32_t tokens);
+bcq_status bcq_lora(const bcq_adapters *desc, const void *A, const void *B, const int32_t *rank, const float *scale,
+                    int32_t tokens, const int32_t *adapter, const void *X, int64_t ldx, const void *base, int64_t ld_base,
+                    void *Y, int64_t ldy, void *workspace, void *stream);
+
+/*
  * Streaming-read probe: reads `bytes` (a multiple of 16) of DEVICE memory with
  * the same 128-bit coalesced loads and launch shape the GEMV uses and writes a
  * 4-byte checksum per workgroup to `sink` (DEVICE, at least

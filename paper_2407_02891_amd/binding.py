@@ -16,7 +16,12 @@ BCQ_MAX_BATCH = 64
 EXPORTS = ["bcq_packed_bytes", "bcq_workspace_bytes", "bcq_workspace_init", "bcq_pack",
            "bcq_pack_rows", "bcq_from_linear", "bcq_quant_workspace_bytes", "bcq_quant_hessian", "bcq_quant_factor_workspace_bytes", "bcq_quant_factor", "bcq_quant_search",
            "bcq_quant_gptq", "bcq_from_linear_rows", "bcq_unpack", "bcq_gemv", "bcq_gemv_noalloc", "bcq_gemm_skinny", "bcq_read_probe_sink_bytes",
-           "bcq_read_probe", "bcq_set_option", "bcq_status_string"]
+           "bcq_read_probe", "bcq_set_option", "bcq_status_string",
+           "bcq_rotate", "bcq_attend_workspace_bytes", "bcq_attend", "bcq_lora_workspace_bytes", "bcq_lora"]
+
+BCQ_F16, BCQ_BF16 = range(2)
+BCQ_MAX_HEAD_DIM = 256
+BCQ_MAX_RANK = 256
 
 
 class Desc(ctypes.Structure):
@@ -24,6 +29,19 @@ class Desc(ctypes.Structure):
     _fields_ = [("M", ctypes.c_int32), ("N", ctypes.c_int32), ("q", ctypes.c_int32),
                 ("group", ctypes.c_int32), ("has_offset", ctypes.c_int32),
                 ("layout_version", ctypes.c_int32)]
+
+
+class Cache(ctypes.Structure):
+    """struct bcq_cache"""
+    _fields_ = [("dtype", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64)]
+
+
+class AdaptersDesc(ctypes.Structure):
+    """struct bcq_adapters"""
+    _fields_ = [("dtype", ctypes.c_int32), ("count", ctypes.c_int32), ("max_rank", ctypes.c_int32),
+                ("M", ctypes.c_int32), ("N", ctypes.c_int32)]
 
 
 class BcqError(RuntimeError):
@@ -71,6 +89,14 @@ def lib():
         L.bcq_read_probe_sink_bytes.restype, L.bcq_read_probe_sink_bytes.argtypes = sz, []
         L.bcq_read_probe.restype, L.bcq_read_probe.argtypes = i32, [vp, sz, vp, vp]
         L.bcq_set_option.restype, L.bcq_set_option.argtypes = i32, [ctypes.c_char_p, i32]
+        cp, ap, i64, f32 = ctypes.POINTER(Cache), ctypes.POINTER(AdaptersDesc), ctypes.c_int64, ctypes.c_float
+        L.bcq_rotate.restype = i32
+        L.bcq_rotate.argtypes = [cp, i32, i32, vp, i64, vp, vp, i32, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp, vp]
+        L.bcq_attend_workspace_bytes.restype, L.bcq_attend_workspace_bytes.argtypes = sz, [cp, i32, i32, i32, i32]
+        L.bcq_attend.restype = i32
+        L.bcq_attend.argtypes = [cp, vp, vp, i32, i32, i32, vp, i64, vp, vp, vp, i32, i32, f32, i32, i32, vp, i64, vp, vp]
+        L.bcq_lora_workspace_bytes.restype, L.bcq_lora_workspace_bytes.argtypes = sz, [ap, i32]
+        L.bcq_lora.restype, L.bcq_lora.argtypes = i32, [ap, vp, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp]
         L.bcq_status_string.restype, L.bcq_status_string.argtypes = ctypes.c_char_p, [i32]
         _lib = L
     return _lib
@@ -201,6 +227,33 @@ def read_probe(buf, nbytes, sink, stream=None):
 
 def read_probe_sink_bytes():
     return int(lib().bcq_read_probe_sink_bytes())
+
+
+def rotate(cache, tokens, q_heads, qkv, ld_qkv, positions, cos_sin, max_position, rot_dim, interleaved, q_weight, k_weight,
+           eps, q_out, ld_q, slots, k_cache, v_cache, stream=None):
+    _check(lib().bcq_rotate(ctypes.byref(cache), tokens, q_heads, _ptr(qkv), ld_qkv, _ptr(positions), _ptr(cos_sin),
+                            max_position, rot_dim, 1 if interleaved else 0, _ptr(q_weight), _ptr(k_weight), eps, _ptr(q_out),
+                            ld_q, _ptr(slots), _ptr(k_cache), _ptr(v_cache), _stream(stream)), "bcq_rotate")
+
+
+def attend_workspace_bytes(cache, tokens, requests, q_heads, max_new):
+    return int(lib().bcq_attend_workspace_bytes(ctypes.byref(cache), tokens, requests, q_heads, max_new))
+
+
+def attend(cache, k_cache, v_cache, tokens, requests, q_heads, q, ld_q, q_start, kv_len, pages, max_pages, max_new, scale,
+           causal, window, out, ld_out, workspace, stream=None):
+    _check(lib().bcq_attend(ctypes.byref(cache), _ptr(k_cache), _ptr(v_cache), tokens, requests, q_heads, _ptr(q), ld_q,
+                            _ptr(q_start), _ptr(kv_len), _ptr(pages), max_pages, max_new, scale, 1 if causal else 0, window,
+                            _ptr(out), ld_out, _ptr(workspace), _stream(stream)), "bcq_attend")
+
+
+def lora_workspace_bytes(desc, tokens):
+    return int(lib().bcq_lora_workspace_bytes(ctypes.byref(desc), tokens))
+
+
+def lora(desc, A, B, rank, scale, tokens, adapter, X, ldx, base, ld_base, Y, ldy, workspace, stream=None):
+    _check(lib().bcq_lora(ctypes.byref(desc), _ptr(A), _ptr(B), _ptr(rank), _ptr(scale), tokens, _ptr(adapter), _ptr(X), ldx,
+                          _ptr(base), ld_base, _ptr(Y), ldy, _ptr(workspace), _stream(stream)), "bcq_lora")
 
 
 def set_option(name, value):

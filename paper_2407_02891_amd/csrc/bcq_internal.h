@@ -70,6 +70,47 @@ constexpr int kStaticScratchRows = 131072;
 // Device address of the current device's copy of that array (asked from the runtime on first use).
 hipError_t static_scratch(void **ptr);
 
+// Serving operators: arguments as checked by the entry points (bcq_serve_api.hip).
+struct RotateArgs {
+    const uint16_t *qkv, *q_weight, *k_weight;
+    const int *positions, *slots;
+    const float *cos_sin;
+    uint16_t *q_out, *k, *v;
+    long long ld_qkv, ld_q;
+    int tokens, q_heads, rot_dim, max_position;
+    float eps;
+    bool interleaved;
+    bcq_cache cache;
+};
+hipError_t launch_rotate(const RotateArgs &a, hipStream_t stream);
+
+struct AttendArgs {
+    const uint16_t *k, *v, *q;
+    const int *q_start, *kv_len, *pages;
+    uint16_t *out;
+    long long ld_q, ld_out;
+    int tokens, requests, q_heads, max_pages, max_new, window;
+    float scale;
+    bool causal;
+    void *workspace;
+    bcq_cache cache;
+};
+size_t attend_workspace_bytes(const bcq_cache &c, int tokens, int requests, int q_heads, int max_new);
+hipError_t launch_attend(const AttendArgs &a, hipStream_t stream);
+
+struct LoraArgs {
+    const uint16_t *A, *B, *X, *base;
+    const int *rank, *adapter;
+    const float *scale;
+    uint16_t *Y;
+    long long ldx, ld_base, ldy;
+    int tokens;
+    void *workspace;
+    bcq_adapters desc;
+};
+size_t lora_workspace_bytes(const bcq_adapters &d, int tokens);
+hipError_t launch_lora(const LoraArgs &a, hipStream_t stream);
+
 constexpr int kProbeBlocks = 512;  // the GEMV's grid: two workgroups per CU
 
 constexpr int kTraceSlots = 16;  // words per wave in the tracing build's timeline buffer
