@@ -331,7 +331,8 @@ bcq_status bcq_rotate(const bcq_cache *cache, int32_t tokens, int32_t q_heads, c
  *   workspace DEVICE, bcq_attend_workspace_bytes(...) bytes, 16-byte aligned; scratch, no init, used by one call at a time
  * tokens = 0 or requests = 0 launches nothing.
  */
-size_t bcq_attend_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_new);
+size_t bcq_attend_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_pages,
+                                  int32_t max_new);
 bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v_cache, int32_t tokens, int32_t requests,
                       int32_t q_heads, const void *q, int64_t ld_q, const int32_t *q_start, const int32_t *kv_len,
                       const int32_t *pages, int32_t max_pages, int32_t max_new, float scale, int32_t causal, int32_t window,

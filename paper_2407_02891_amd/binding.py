@@ -92,7 +92,7 @@ def lib():
         cp, ap, i64, f32 = ctypes.POINTER(Cache), ctypes.POINTER(AdaptersDesc), ctypes.c_int64, ctypes.c_float
         L.bcq_rotate.restype = i32
         L.bcq_rotate.argtypes = [cp, i32, i32, vp, i64, vp, vp, i32, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp, vp]
-        L.bcq_attend_workspace_bytes.restype, L.bcq_attend_workspace_bytes.argtypes = sz, [cp, i32, i32, i32, i32]
+        L.bcq_attend_workspace_bytes.restype, L.bcq_attend_workspace_bytes.argtypes = sz, [cp, i32, i32, i32, i32, i32]
         L.bcq_attend.restype = i32
         L.bcq_attend.argtypes = [cp, vp, vp, i32, i32, i32, vp, i64, vp, vp, vp, i32, i32, f32, i32, i32, vp, i64, vp, vp]
         L.bcq_lora_workspace_bytes.restype, L.bcq_lora_workspace_bytes.argtypes = sz, [ap, i32]
@@ -236,8 +236,8 @@ def rotate(cache, tokens, q_heads, qkv, ld_qkv, positions, cos_sin, max_position
                             ld_q, _ptr(slots), _ptr(k_cache), _ptr(v_cache), _stream(stream)), "bcq_rotate")
 
 
-def attend_workspace_bytes(cache, tokens, requests, q_heads, max_new):
-    return int(lib().bcq_attend_workspace_bytes(ctypes.byref(cache), tokens, requests, q_heads, max_new))
+def attend_workspace_bytes(cache, tokens, requests, q_heads, max_pages, max_new):
+    return int(lib().bcq_attend_workspace_bytes(ctypes.byref(cache), tokens, requests, q_heads, max_pages, max_new))
 
 
 def attend(cache, k_cache, v_cache, tokens, requests, q_heads, q, ld_q, q_start, kv_len, pages, max_pages, max_new, scale,

@@ -1,0 +1,68 @@
+// Shared by the two attention kernels (not public): their parameters, what a request needs, and the softmax's running statistics.
+#pragma once
+#include "bcq_half.h"
+#include "bcq_internal.h"
+
+namespace bcq {
+
+struct AttendParams {
+    const uint16_t *k, *v, *q;
+    const int *q_start, *kv_len, *pages;
+    uint16_t *out;
+    float *part;       // unnormalised sums of a split request: [slot][kv head][row][head_dim of the kernel]
+    f32x2 *stat;       // their (maximum, sum of weights): [slot][kv head][row]
+    long long ld_q, ld_out, page_stride, head_stride;
+    int slot_stride;
+    int tokens, requests, kv_heads, group;  // group: query heads of a kv head
+    int head_dim, page_shift, num_pages, max_pages;
+    int max_new, window, causal;
+    float scale;       // times log2 e
+    int rows;          // requests of at most this many rows (new tokens times group) are the stream kernel's
+    int workers;       // stream kernel: waves per kv head
+    int parts;         // chunk kernel: pieces that a tile's keys are cut into
+};
+
+// One request as the kernels see it, whatever the arrays hold: rows of q inside 0 .. tokens, keys inside its row of pages.
+struct Request {
+    int start, n;      // new tokens
+    int todo;          // those of them that are computed
+    int len;           // keys
+    int begin, end;    // keys that any of them sees
+};
+
+__device__ __forceinline__ Request load_request(const AttendParams &p, int r)
+{
+    Request q;
+    q.start = min(max(p.q_start[r], 0), p.tokens);
+    q.n = min(max(p.q_start[r + 1], q.start), p.tokens) - q.start;
+    q.todo = min(q.n, p.max_new);
+    q.len = (int)min((long long)max(p.kv_len[r], 0), (long long)p.max_pages << p.page_shift);
+    const int first = q.len - q.n;  // position of the first new token
+    q.end = p.causal ? min(max(first + q.todo, 0), q.len) : q.len;
+    q.begin = p.window ? min(max(first + 1 - p.window, 0), q.end) : 0;
+    return q;
+}
+
+// Keys that token i of a request sees: [begin, end), none if end <= begin.
+__device__ __forceinline__ void visible_keys(const AttendParams &p, const int n, const int len, int i, int &begin, int &end)
+{
+    const int position = len - n + i;
+    end = p.causal ? min(position + 1, len) : len;
+    begin = p.window ? max(position + 1 - p.window, 0) : 0;
+}
+
+__device__ __forceinline__ int page_of(const AttendParams &p, int r, int key)
+{
+    return min(max(p.pages[(long long)r * p.max_pages + (key >> p.page_shift)], 0), p.num_pages - 1);
+}
+
+// What elements behind head_dim are loaded from.
+static __device__ __attribute__((aligned(16))) const uint16_t g_zeros[8] = {};
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The chunk kernel (bcq_attend_chunk.hip): requests of more than p.rows rows.  dim: the padded head_dim.
+int chunk_parts(int tokens, int group, int kv_heads, int dim, long long most_keys);
+void launch_chunks(const AttendParams &p, int dim, bool any, bool bf16, hipStream_t s);
+
+}  // namespace bcq

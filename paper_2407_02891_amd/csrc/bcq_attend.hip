@@ -1,64 +1,499 @@
-// Attention of new tokens over a paged cache, one wave per (token, query head).  64 keys a step: a lane has one key's score, then the
-// lanes share the head's elements and walk the keys; running maximum and sum of the softmax, one pass over the keys.
-#include "bcq_half.h"
-#include "bcq_internal.h"
+// Attention of a few new tokens per request over a paged cache: what serving does at every step.
+//
+//   out = sum_j softmax_j(scale q . k_j) v_j
+//
+// Bound by the bytes of K and V.  A row is a (new token, query head) pair; the rows that share a kv head are the columns of a matrix
+// instruction, so a key is read once for all of them.
+//  * The blocks of 32 keys of all requests form one line, which is cut into as many equal pieces as there are waves for a kv head
+//    (from the lengths on the device: the host does not see them).  A wave walks its piece, over the ends of requests, and leaves for each
+//    request sums, maximum and weight (slot wave + request, which no two share); a request that one wave has to itself is finished there.
+//    A second launch joins the others.
+//  * S^T = K Q^T: a lane gets four keys' scores of one row, and the same lane group's weights are the operand of O^T = V^T P^T as they
+//    are, because the keys of a product may be numbered in any order.  V passes through LDS (the wave's own, no barrier), whose transposing read
+//    gives four keys of one element.
+//  * The next block's K and V are requested when this one's have been used, and its page numbers a block earlier.
+//  * Weights are taken relative to a running maximum that is renewed only when a score passes it by 2^8, so O is hardly ever rescaled.
+//    They enter the second product as the sum of two 16-bit numbers (22 or 16 bits): it costs a matrix instruction more, and those wait for memory.
+#include "bcq_attend.h"
 
 namespace bcq {
 
-template <bool BF>
-__global__ __launch_bounds__(64) void bcq_attend_kernel(AttendArgs p)
+namespace {
+
+constexpr int kBlock = 32;  // keys of a step
+constexpr int kWaves = 4;
+constexpr float kGrow = 8.0f;
+constexpr int kStreamRows = 16;
+
+// Waves per SIMD: what the registers allow.
+constexpr int stream_occupancy(int dim, bool any) { return dim == 64 ? (any ? 3 : 4) : dim == 128 ? 2 : 1; }
+
+// Blocks of a request in the line; a request whose rows see nothing has one, which writes its zeros.
+__device__ __forceinline__ int blocks_of(const AttendParams &p, const Request &q)
 {
-    __shared__ float q[BCQ_MAX_HEAD_DIM];
-    __shared__ float weight[64];
-    __shared__ long long place[64];
-    const int t = blockIdx.x, head = blockIdx.y, lane = threadIdx.x, D = p.cache.head_dim, page = p.cache.page_size;
-    int r = 0;
-    while (r < p.requests && !(p.q_start[r] <= t && t < p.q_start[r + 1])) ++r;
-    if (r == p.requests) return;
-    const int start = max(p.q_start[r], 0), n = min(p.q_start[r + 1], p.tokens) - start, i = t - start;
-    if (i >= min(n, p.max_new)) return;
-    const int len = (int)min((long long)max(p.kv_len[r], 0), (long long)p.max_pages * page), position = len - n + i;
-    const int end = p.causal ? min(len, position + 1) : len, begin = p.window ? max(0, position + 1 - p.window) : 0;
-    const int kv_head = head / (p.q_heads / p.cache.kv_heads);
-    for (int d = lane; d < D; d += 64) q[d] = to_float<BF>(p.q[t * p.ld_q + (long long)head * D + d]);
-    float most = -INFINITY, sum = 0.0f, o[BCQ_MAX_HEAD_DIM / 64] = {};
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        __syncthreads();
-        const int j = min(j0 + lane, end - 1);
-        const int id = min(max(p.pages[(long long)r * p.max_pages + j / page], 0), p.cache.num_pages - 1);
-        const long long at = id * p.cache.page_stride + kv_head * p.cache.head_stride + (j % page) * p.cache.slot_stride;
-        float s = 0.0f;
-        for (int d = 0; d < D; ++d) s = fmaf(q[d], to_float<BF>(p.k[at + d]), s);
-        s = j0 + lane < end ? s * p.scale : -INFINITY;
-        float m = s;
-        for (int step = 32; step > 0; step >>= 1) m = fmaxf(m, __shfl_xor(m, step));
-        m = fmaxf(m, most);
-        const float base = m == -INFINITY ? 0.0f : m, shrink = expf(most - base);
-        const float e = expf(s - base);
-        float es = e;
-        for (int step = 32; step > 0; step >>= 1) es += __shfl_xor(es, step);
-        sum = sum * shrink + es;
-        most = m;
-        weight[lane] = e;
-        place[lane] = at;
-        __syncthreads();
-        for (int c = 0; c < BCQ_MAX_HEAD_DIM / 64; ++c) {
-            o[c] *= shrink;
-            if (lane + 64 * c < D)
-                for (int k = 0; k < min(64, end - j0); ++k) o[c] = fmaf(weight[k], to_float<BF>(p.v[place[k] + lane + 64 * c]), o[c]);
-        }
-    }
-    for (int c = 0; c < BCQ_MAX_HEAD_DIM / 64; ++c)
-        if (lane + 64 * c < D) p.out[t * p.ld_out + (long long)head * D + lane + 64 * c] = from_float<BF>(begin < end ? o[c] / sum : 0.0f);
+    if (q.todo == 0 || q.todo * p.group > p.rows) return 0;
+    return max(1, (q.end + kBlock - 1) / kBlock - q.begin / kBlock);
 }
 
-size_t attend_workspace_bytes(const bcq_cache &, int, int, int, int) { return 0; }
+__device__ __forceinline__ int prefix_sum(int v, int lane)
+{
+#pragma unroll
+    for (int step = 1; step < 64; step <<= 1) {
+        const int below = __shfl_up(v, step);
+        if (lane >= step) v += below;
+    }
+    return v;
+}
+
+// Sixty-four requests, one a lane, with the blocks up to and with each of them.
+struct Window {
+    Request q;
+    int blocks, upto;
+    __device__ __forceinline__ void load(const AttendParams &p, int first, int before, int lane)
+    {
+        const int r = first + lane;
+        q = load_request(p, min(r, p.requests - 1));
+        blocks = r < p.requests ? blocks_of(p, q) : 0;
+        upto = before + prefix_sum(blocks, lane);
+    }
+};
+
+__device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+// Waves that share the line: no more than it has blocks.
+__device__ __forceinline__ int workers_of(const AttendParams &p, int total) { return min(p.workers, max(total, 1)); }
+__device__ __forceinline__ int first_block(int worker, int workers, int total) { return (int)((long long)worker * total / workers); }
+__device__ __forceinline__ int worker_of(int block, int workers, int total) { return (int)((((long long)block + 1) * workers - 1) / total); }
+
+// A wave's share of one request.
+struct Segment {
+    int r, start, n, todo, len;
+    int key, blocks;   // first key (of a block), blocks
+    bool whole;        // all of the request
+};
+
+}  // namespace
+
+// DT: head_dim, or what it is padded to.  ANY: head_dim < DT, or pages of fewer than 16 slots.
+template <int DT, bool BF, bool ANY>
+__global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_attend_stream_kernel(AttendParams p)
+{
+    constexpr int C = DT / 32, DV = DT / 16;     // matrix steps over head_dim; tiles of O
+    constexpr int kRowLanes = DT / 8, kRows = 64 / kRowLanes;  // a load of V covers kRows keys
+    __shared__ __attribute__((aligned(16))) uint16_t v_lds[kWaves][kBlock * DT];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r16 = lane & 15, g = lane >> 4;
+    const int index = blockIdx.x * kWaves + wave;
+    const int head = index % p.kv_heads, worker = index / p.kv_heads;
+    int first_head = head * p.group;  // (of q)
+    if (ANY) asm("" : "+v"(first_head));
+    uint16_t *const vs = v_lds[wave];
+    // element d of key j in LDS: 16-element units of a row exchanged by the key, so that eight keys' units of one number fill all banks
+    const auto v_at = [&](int key, int d) {
+        const int turn = DT == 64 ? key >> 1 & 3 : key & 7;
+        return vs + key * DT + ((d >> 4 ^ turn) << 4) + (d & 15);
+    };
+
+    // ---- this wave's piece of the line ----
+    Window w;
+    int total = 0, first = 0;
+    for (int c = 0; c < p.requests; c += 64) {
+        w.load(p, c, total, lane);
+        total = lane_of(w.upto, 63);
+    }
+    const int workers = workers_of(p, total);
+    if (worker >= workers || total == 0) return;
+    int at = first_block(worker, workers, total);
+    const int stop = first_block(worker + 1, workers, total);
+    if (p.requests > 64) w.load(p, 0, 0, lane);
+    const auto segment_at = [&](int place) {
+        while (lane_of(w.upto, 63) <= place) w.load(p, first += 64, lane_of(w.upto, 63), lane);
+        const int l = __builtin_ctzll(__ballot(w.upto > place));
+        const int upto = lane_of(w.upto, l), from = upto - lane_of(w.blocks, l);
+        Segment e;
+        e.r = first + l;
+        e.start = lane_of(w.q.start, l);
+        e.n = lane_of(w.q.n, l);
+        e.todo = lane_of(w.q.todo, l);
+        e.len = lane_of(w.q.len, l);
+        e.key = (lane_of(w.q.begin, l) / kBlock + place - from) * kBlock;
+        e.blocks = min(upto, stop) - place;
+        e.whole = from == place && upto <= stop;
+        return e;
+    };
+
+    // ---- requests to memory: lane (g, r16) has of K the elements 32 c + 8 g .. of keys r16 and 16 + r16 ----
+    u32x4 kr[2][C], vr[2][C];
+    long long page_stride = p.page_stride, head_offset = head * p.head_stride;
+    int slot_stride = p.slot_stride, last_page = p.num_pages - 1;
+    if (ANY) asm("" : "+v"(page_stride), "+v"(head_offset), "+v"(slot_stride), "+v"(last_page));  // (scalar registers are scarce there)
+    int dim = p.head_dim;
+    if (ANY) asm("" : "+v"(dim));
+    int id[2];  // page numbers of the block that is requested next
+    const auto find_pages = [&](int r, int len, int first_key) {
+        if (ANY) return;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) id[t] = page_of(p, r, min(first_key + 16 * t, max(len - 1, 0) & ~15));
+    };
+    const auto request = [&](int r, int len, int first_key) {
+        const int last = max(len - 1, 0);
+        if (ANY) asm volatile("" : "+v"(dim));  // (compared here, not held as masks through the loop)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int key = min(first_key + 16 * t, last & ~15);  // keys behind the last are the last's copies, and masked
+            if (!ANY) {
+                const long long base = __builtin_amdgcn_readfirstlane(id[t]) * page_stride + head_offset +
+                                       (long long)((key & ((1 << p.page_shift) - 1)) * p.slot_stride);
+                const char *const kp = reinterpret_cast<const char *>(p.k + base), *const vp = reinterpret_cast<const char *>(p.v + base);
+                const unsigned k_off = 2 * (unsigned)(min(r16, last - key) * p.slot_stride + 8 * g);
+#pragma unroll
+                for (int c = 0; c < C; ++c) kr[t][c] = *reinterpret_cast<const u32x4 *>(kp + k_off + 64 * c);
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const unsigned v_off = 2 * (unsigned)(min(c * kRows + lane / kRowLanes, last - key) * p.slot_stride + 8 * (lane % kRowLanes));
+                    vr[t][c] = *reinterpret_cast<const u32x4 *>(vp + v_off);
+                }
+            } else {
+                const auto place = [&](int row) {
+                    const int j = min(key + row, last);
+                    const int page = min(max(p.pages[(long long)r * p.max_pages + (j >> p.page_shift)], 0), last_page);
+                    return page * page_stride + head_offset + (long long)((j & ((1 << p.page_shift) - 1)) * slot_stride);
+                };
+                const auto load = [&](const uint16_t *row, int d) { return *reinterpret_cast<const u32x4 *>(d < dim ? row + d : g_zeros); };
+                const uint16_t *const kp = p.k + place(r16);
+#pragma unroll
+                for (int c = 0; c < C; ++c) kr[t][c] = load(kp, 32 * c + 8 * g);
+#pragma unroll
+                for (int c = 0; c < C; ++c) vr[t][c] = load(p.v + place(c * kRows + lane / kRowLanes), 8 * (lane % kRowLanes));
+            }
+        }
+    };
+
+    Segment now = segment_at(at);
+    find_pages(now.r, now.len, now.key);
+    request(now.r, now.len, now.key);
+    if (now.blocks > 1) find_pages(now.r, now.len, now.key + kBlock);
+
+    // ---- rows: column r16 is token r16 / group, query head r16 mod group ----
+    const int token = r16 / p.group, member = r16 % p.group;
+    u32x4 q[C];
+    f32x4 o[DV];
+    float most, base, sum;
+    int from, to;          // keys that the row sees
+    int all_from, all_to;  // keys that every row sees
+    const auto begin_request = [&](const Segment &b) {
+        int unused;
+        visible_keys(p, b.n, b.len, 0, unused, all_to);
+        visible_keys(p, b.n, b.len, b.todo - 1, all_from, unused);
+        visible_keys(p, b.n, b.len, token, from, to);
+        most = -INFINITY;
+        base = sum = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DV; ++d) o[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const bool real = token < b.todo;
+        const uint16_t *const src = p.q + (long long)(b.start + (real ? token : 0)) * p.ld_q + (first_head + member) * p.head_dim;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            q[c] = u32x4{0, 0, 0, 0};
+            if (real && (!ANY || 32 * c + 8 * g < dim)) q[c] = *reinterpret_cast<const u32x4 *>(src + 32 * c + 8 * g);
+        }
+    };
+    begin_request(now);
+
+    while (true) {
+        // V to LDS, scores
+        const int key0 = now.key;
+        const bool masked = key0 + kBlock > all_to || key0 < all_from;
+        // Infinities or NaN among values that not every row sees: zero times them must not reach the rows that do not.  They are replaced by
+        // zeros, and what they make of the rows that do see them, an infinity or a NaN, is found by products of ones.
+        bool odd = false;
+        if (masked) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) odd |= not_finite<BF>(vr[t][c][i]);
+            odd = __ballot(odd) != 0;
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                *reinterpret_cast<u32x4 *>(v_at(16 * t + c * kRows + lane / kRowLanes, 8 * (lane % kRowLanes))) = vr[t][c];
+        f32x4 s[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < C; ++c) s[t] = mfma16<BF>(kr[t][c], q[c], s[t]);
+        }
+        now.key += kBlock;
+        --now.blocks;
+        ++at;
+        Segment next = now;
+        if (at < stop) {
+            if (!now.blocks) {
+                next = segment_at(at);
+                find_pages(next.r, next.len, next.key);
+            }
+            request(next.r, next.len, next.key);
+            if (next.blocks > 1) find_pages(next.r, next.len, next.key + kBlock);
+        }
+        // weights: number 4 t + i of a lane is key 16 t + 4 g + i
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * p.scale;
+        if (masked) {
+            const unsigned span = max(to - from, 0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (unsigned)(key0 + 16 * (e >> 2) + 4 * g + (e & 3) - from) < span ? x[e] : -INFINITY;
+        }
+        float high = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) high = fmaxf(high, x[e]);
+        if (__ballot(high > most + kGrow)) {
+            const float m = fmaxf(most, max_over_groups(high));
+            const float shrink = most == -INFINITY ? 1.0f : exp2_fast(most - m);
+            most = m;
+            base = m == -INFINITY ? 0.0f : m;
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < DV; ++d) o[d] *= shrink;
+        }
+        u32x4 high_part, low_part;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float a = exp2_fast(x[e] - base), b = exp2_fast(x[e + 1] - base);
+            sum += a + b;
+            const uint32_t pair = from_float2<BF>(a, b);
+            const f32x2 kept = to_float2<BF>(pair);
+            high_part[e / 2] = pair;
+            low_part[e / 2] = from_float2<BF>(a - kept.x, b - kept.y);
+        }
+        asm volatile("" ::: "memory");
+        const auto column = [&](int d) {  // the operand V^T: elements 16 d + r16 of keys 4 g .. and 16 + 4 g ..
+            const u32x2 v0 = lds_column(v_at(lane >> 2, 16 * d + 4 * (lane & 3))), v1 = lds_column(v_at(16 + (lane >> 2), 16 * d + 4 * (lane & 3)));
+            return u32x4{v0.x, v0.y, v1.x, v1.y};
+        };
+        if (odd) {
+            u32x4 sees;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int key = key0 + 16 * (e >> 1) + 4 * g + 2 * (e & 1);
+                sees[e] = (key >= from && key < to ? kOne<BF> : 0u) | (key + 1 >= from && key + 1 < to ? kOne<BF> << 16 : 0u);
+            }
+#pragma unroll
+            for (int d = 0; d < DV; ++d) {
+                const u32x4 a = column(d);
+                u32x4 up, down;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) up[e] = ones_where_infinite<BF>(a[e], 0), down[e] = ones_where_infinite<BF>(a[e], 0x8000u);
+                const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                const f32x4 ups = mfma16<BF>(up, sees, zero), downs = mfma16<BF>(down, sees, zero);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[d][i] += (ups[i] > 0.0f ? INFINITY : 0.0f) - (downs[i] > 0.0f ? INFINITY : 0.0f);
+                __builtin_amdgcn_sched_barrier(0);  // (rare: registers count, not time)
+            }
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    u32x4 *const mine = reinterpret_cast<u32x4 *>(v_at(16 * t + c * kRows + lane / kRowLanes, 8 * (lane % kRowLanes)));
+                    u32x4 x = *mine;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = finite_only<BF>(x[i]);
+                    *mine = x;
+                }
+            asm volatile("" ::: "memory");
+        }
+#pragma unroll
+        for (int d = 0; d < DV; ++d) {
+            const u32x4 a = column(d);
+            o[d] = mfma16<BF>(a, low_part, mfma16<BF>(a, high_part, o[d]));
+        }
+        asm volatile("" ::: "memory");
+        if (now.blocks) continue;
+        const float weight = sum_over_groups(sum), unit = 1.0f / weight;
+        if (token < now.todo) {
+            if (now.whole) {
+                uint16_t *const dst = p.out + (long long)(now.start + token) * p.ld_out + (first_head + member) * p.head_dim;
+                if (ANY) asm volatile("" : "+v"(dim));  // (compared here, not held as masks through the loop)
+#pragma unroll
+                for (int d = 0; d < DV; ++d)
+                    if (!ANY || 16 * d + 4 * g < dim) {
+                        f32x4 y = o[d] * unit;
+                        if (to <= from) y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                        *reinterpret_cast<u32x2 *>(dst + 16 * d + 4 * g) = u32x2{from_float2<BF>(y[0], y[1]), from_float2<BF>(y[2], y[3])};
+                    }
+            } else {
+                const long long slot = ((long long)now.r * p.kv_heads + index) * kStreamRows + r16;  // (index: worker * kv_heads + head)
+#pragma unroll
+                for (int d = 0; d < DV; ++d) *reinterpret_cast<f32x4 *>(p.part + slot * DT + 16 * d + 4 * g) = o[d];
+                if (g == 0) p.stat[slot] = f32x2{most, weight};
+            }
+        }
+        if (at == stop) break;
+        now = next;
+        begin_request(now);
+    }
+}
+
+// Joins what the waves left of a request: a workgroup per (request, kv head, row), its waves share the pieces.
+template <int DT, bool BF>
+__global__ __launch_bounds__(64 * kWaves) void bcq_attend_join_kernel(AttendParams p)
+{
+    constexpr int E = DT / 64;  // elements of a lane
+    __shared__ float shared[kWaves][DT + 2];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = blockIdx.x, head = blockIdx.y, row = blockIdx.z;
+    const Request q = load_request(p, r);
+    const int own = blocks_of(p, q);
+    if (own == 0 || row >= q.todo * p.group) return;
+    int total = 0, upto = 0;
+    for (int c = 0; c < p.requests; c += 64) {
+        Window w;
+        w.load(p, c, total, lane);
+        total = lane_of(w.upto, 63);
+        if (r >= c && r < c + 64) upto = lane_of(w.upto, r - c);
+    }
+    const int workers = workers_of(p, total);
+    const int w0 = worker_of(upto - own, workers, total), w1 = worker_of(upto - 1, workers, total);
+    if (w0 == w1) return;  // finished by its one wave
+    const auto slot = [&](int w) { return ((long long)(w + r) * p.kv_heads + head) * kStreamRows + row; };
+    float most = -INFINITY;
+    for (int w = w0 + lane; w <= w1; w += 64) most = fmaxf(most, p.stat[slot(w)].x);
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) most = fmaxf(most, __shfl_xor(most, step));
+    const float base = most == -INFINITY ? 0.0f : most;
+    float weight = 0.0f, y[E] = {};
+#pragma unroll 4
+    for (int w = w0 + wave; w <= w1; w += kWaves) {
+        const long long s = slot(w);
+        const f32x2 stat = p.stat[s];
+        const float scale = exp2_fast(stat.x - base);
+        weight = fmaf(stat.y, scale, weight);
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = fmaf(p.part[s * DT + lane * E + e], scale, y[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) shared[wave][lane * E + e] = y[e];
+    if (lane == 0) shared[wave][DT] = weight;
+    __syncthreads();
+    if (wave != 0) return;
+    float all = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        all += shared[w][DT];
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] += shared[w][lane * E + e];
+    }
+    const int token = row / p.group;
+    int from, to;
+    visible_keys(p, q.n, q.len, token, from, to);
+    uint16_t *const dst = p.out + (long long)(q.start + token) * p.ld_out + (head * p.group + row % p.group) * p.head_dim;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (lane * E + e < p.head_dim) dst[lane * E + e] = from_float<BF>(to > from ? y[e] / all : 0.0f);
+}
+
+namespace {
+
+int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+
+struct StreamPlan {
+    int dim, workers;
+    bool any;
+    size_t slots, part_bytes;
+};
+StreamPlan stream_plan(const bcq_cache &c, int requests)
+{
+    StreamPlan s;
+    s.dim = padded_dim(c.head_dim);
+    s.any = c.head_dim != s.dim || c.page_size < 16;
+    s.workers = (compute_units() * kWaves * stream_occupancy(s.dim, s.any) + c.kv_heads - 1) / c.kv_heads;  // as many waves as the chip holds
+    s.slots = (size_t)(s.workers + requests) * c.kv_heads * kStreamRows;
+    s.part_bytes = s.slots * s.dim * sizeof(float);
+    return s;
+}
+
+template <int DT, bool BF>
+void stream_and_join(const AttendParams &p, bool any, hipStream_t s)
+{
+    const int groups = (p.workers * p.kv_heads + kWaves - 1) / kWaves;
+    if (any) bcq_attend_stream_kernel<DT, BF, true><<<groups, 64 * kWaves, 0, s>>>(p);
+    else bcq_attend_stream_kernel<DT, BF, false><<<groups, 64 * kWaves, 0, s>>>(p);
+    const long long most = (long long)p.max_new * p.group;
+    const dim3 grid(p.requests, p.kv_heads, (unsigned)(most < kStreamRows ? most : kStreamRows));
+    bcq_attend_join_kernel<DT, BF><<<grid, 64 * kWaves, 0, s>>>(p);
+}
+
+template <bool BF>
+void by_dim(const AttendParams &p, int dim, bool any, hipStream_t s)
+{
+    if (dim == 64) stream_and_join<64, BF>(p, any, s);
+    else if (dim == 128) stream_and_join<128, BF>(p, any, s);
+    else stream_and_join<256, BF>(p, any, s);
+}
+
+// Which kernels a call needs: the stream kernel has the requests of up to kStreamRows rows, the chunk kernel the others.  The host knows tokens,
+// requests and the longest chunk: where no request can be of one of the kinds, its kernel is not launched and the other takes what there is.
+struct Split {
+    bool stream, chunk;
+};
+Split split(int tokens, int requests, int group, int max_new)
+{
+    if ((long long)max_new * group <= kStreamRows) return {true, false};
+    return {group <= kStreamRows && tokens != (long long)requests * max_new, true};
+}
+
+size_t chunk_part_bytes(int parts, int tokens, int q_heads, int dim) { return parts > 1 ? (size_t)parts * tokens * q_heads * dim * sizeof(float) : 0; }
+size_t chunk_bytes(int parts, int tokens, int q_heads, int dim)
+{
+    return parts > 1 ? chunk_part_bytes(parts, tokens, q_heads, dim) + (size_t)parts * tokens * q_heads * sizeof(f32x2) : 0;
+}
+
+}  // namespace
+
+size_t attend_workspace_bytes(const bcq_cache &c, int tokens, int requests, int q_heads, int max_new, int max_pages)
+{
+    const Split which = split(tokens, requests, q_heads / c.kv_heads, max_new);
+    const StreamPlan s = stream_plan(c, requests);
+    const size_t one = which.stream ? s.part_bytes + s.slots * sizeof(f32x2) : 0;
+    if (!which.chunk) return one;
+    const int parts = chunk_parts(tokens, q_heads / c.kv_heads, c.kv_heads, s.dim, (long long)max_pages * c.page_size);
+    const size_t other = chunk_bytes(parts, tokens, q_heads, s.dim);
+    return one > other ? one : other;  // one after the other
+}
 
 hipError_t launch_attend(const AttendArgs &a, hipStream_t stream)
 {
-    const dim3 grid(a.tokens, a.q_heads);
-    if (a.cache.dtype == BCQ_BF16) bcq_attend_kernel<true><<<grid, 64, 0, stream>>>(a);
-    else bcq_attend_kernel<false><<<grid, 64, 0, stream>>>(a);
+    const bcq_cache &c = a.cache;
+    const StreamPlan plan = stream_plan(c, a.requests);
+    AttendParams p = {};
+    p.k = a.k, p.v = a.v, p.q = a.q, p.q_start = a.q_start, p.kv_len = a.kv_len, p.pages = a.pages, p.out = a.out;
+    p.part = static_cast<float *>(a.workspace);
+    p.ld_q = a.ld_q, p.ld_out = a.ld_out, p.page_stride = c.page_stride, p.head_stride = c.head_stride, p.slot_stride = (int)c.slot_stride;
+    p.tokens = a.tokens, p.requests = a.requests, p.kv_heads = c.kv_heads, p.group = a.q_heads / c.kv_heads;
+    p.head_dim = c.head_dim, p.page_shift = __builtin_ctz(c.page_size), p.num_pages = c.num_pages, p.max_pages = a.max_pages;
+    p.max_new = a.max_new, p.window = a.window, p.causal = a.causal;
+    p.scale = (float)(a.scale * 1.4426950408889634);
+    const Split which = split(a.tokens, a.requests, p.group, a.max_new);
+    if (which.stream) {
+        p.rows = kStreamRows, p.workers = plan.workers;
+        p.stat = reinterpret_cast<f32x2 *>(static_cast<char *>(a.workspace) + plan.part_bytes);
+        if (c.dtype == BCQ_BF16) by_dim<true>(p, plan.dim, plan.any, stream);
+        else by_dim<false>(p, plan.dim, plan.any, stream);
+    }
+    if (which.chunk) {
+        p.rows = which.stream ? kStreamRows : 0;
+        p.parts = chunk_parts(a.tokens, p.group, c.kv_heads, plan.dim, (long long)a.max_pages * c.page_size);
+        p.stat = reinterpret_cast<f32x2 *>(static_cast<char *>(a.workspace) + chunk_part_bytes(p.parts, a.tokens, a.q_heads, plan.dim));
+        launch_chunks(p, plan.dim, plan.any, c.dtype == BCQ_BF16, stream);
+    }
     return hipGetLastError();
 }
 

@@ -1,0 +1,381 @@
+// Attention of chunks of new tokens over a paged cache: the requests with more rows than the stream kernel takes.
+//
+//   out = sum_j softmax_j(scale q . k_j) v_j
+//
+// Bound by the matrix instructions (4 head_dim operations for a pair of row and key), and by the vector instructions of the softmax beside
+// them.  A workgroup has a tile of 128 rows ((new token, query head) pairs that share a kv head), 32 a wave, and walks the keys that any of
+// them sees.
+//  * K and V blocks go straight to LDS, two buffers each: the next block is on its way while this one is used.  The 16-byte pieces of a row are exchanged by the row's number, on the global side of the transfer, so that
+//    both kinds of reads find all banks.
+//  * S^T = K Q^T with Q in registers: a lane has one row's scores, 32 for a block of 64 keys, so a row's maximum and sum need one exchange between
+//    two lanes; its weights, rounded to 16 bits, are the operand of O^T = V^T P^T as they are, for the keys of a product may be numbered in any order.
+//    V's side of it comes from the transposing read.  The rounding of the weights adds to a result what its own rounding does (1.4 times in the mean square).
+//  * Maxima are renewed only when a score passes them by 2^8; blocks that all of a wave's rows see have no masks, those that none sees are left out.
+//  * Few tiles and many keys: the keys of a tile are cut into `parts`, whose sums a second launch joins.
+#include "bcq_attend.h"
+
+namespace bcq {
+
+namespace {
+
+constexpr int kWaves = 4, kChunkRows = 32 * kWaves;
+constexpr float kGrow = 8.0f;
+constexpr int chunk_keys(int dim) { return dim == 256 ? 32 : 64; }  // a block
+constexpr int chunk_occupancy(int dim) { return dim == 256 ? 1 : 2; }
+
+typedef __attribute__((address_space(3))) void *lds_void;
+typedef const __attribute__((address_space(1))) void *global_void;
+
+// Sixteen bytes a lane from memory to LDS: lane l's to `to` (the wave's) + 16 l.
+__device__ __forceinline__ void load_to_lds(const uint16_t *from, uint16_t *to)
+{
+    __builtin_amdgcn_global_load_lds((global_void)from, (lds_void)to, 16, 0, 0);
+}
+
+// All but the newest `most` requests of this wave have arrived.
+template <int most>
+__device__ __forceinline__ void arrived()
+{
+    __builtin_amdgcn_s_waitcnt((most & 15) | (most >> 4) << 14 | 0xf70);  // (the other counters' fields: no wait)
+}
+
+__device__ __forceinline__ int tile_slots_before(const AttendParams &p, int r)
+{
+    return (int)((long long)min(max(p.q_start[r], 0), p.tokens) * p.group / kChunkRows) + r;
+}
+
+}  // namespace
+
+// DT: head_dim, or what it is padded to.  ANY: head_dim < DT, or pages of fewer than 16 slots.
+template <int DT, bool BF, bool ANY>
+__global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_chunk_kernel(AttendParams p)
+{
+    constexpr int KB = chunk_keys(DT), KT = KB / 32, C = DT / 16, DV = DT / 32;
+    constexpr int kPieces = DT / 8, kRows = 64 / kPieces;       // 16-byte pieces of a key; keys of one transfer of a wave
+    constexpr int kTransfers = KB / (kRows * kWaves);           // of a wave for a block of K, and for one of V
+    // Two buffers each, as objects of their own: the compiler holds reads of one back for the transfers to it alone.
+    __shared__ __attribute__((aligned(1024))) uint16_t k0[KB * DT], k1[KB * DT], v0[KB * DT], v1[KB * DT];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r32 = lane & 31, h = lane >> 5;
+
+    // ---- which rows: the slots of a request's tiles begin at q_start * group / 128 + r, the last tiles (with the most keys) first ----
+    const int head = blockIdx.x % p.kv_heads, part = blockIdx.y;
+    const int slot = gridDim.x / p.kv_heads - 1 - blockIdx.x / p.kv_heads;
+    int r = 0;
+    for (int high = p.requests; high - r > 1;) {
+        const int middle = (r + high) >> 1;
+        if (tile_slots_before(p, middle) <= slot) r = middle;
+        else high = middle;
+    }
+    const Request q = load_request(p, r);
+    const int rows = q.todo * p.group, row0 = (slot - tile_slots_before(p, r)) * kChunkRows;
+    if (rows <= p.rows || row0 < 0 || row0 >= rows) return;
+
+    // ---- which keys ----
+    const int row = row0 + 32 * wave + r32;
+    const bool real = row < rows;
+    const int token = row / p.group, member = row - token * p.group;
+    int from, to, low, end, tile_from, tile_to, all_from, all_to;
+    visible_keys(p, q.n, q.len, token, from, to);
+    visible_keys(p, q.n, q.len, row0 / p.group, low, tile_to);                                          // of the tile: any sees [low, end), all see
+    visible_keys(p, q.n, q.len, (min(row0 + kChunkRows, rows) - 1) / p.group, tile_from, end);          // [tile_from, tile_to)
+    const int first_token = (row0 + 32 * wave) / p.group, last_token = (min(row0 + 32 * wave + 32, rows) - 1) / p.group;
+    int any_from, any_to;  // of the wave, the same
+    visible_keys(p, q.n, q.len, first_token, any_from, all_to);
+    visible_keys(p, q.n, q.len, last_token, all_from, any_to);
+    const bool has_rows = row0 + 32 * wave < rows;
+    end = max(end, 0);
+    const int block0 = min(low, end) / KB, blocks = (end + KB - 1) / KB - block0;
+    const int b0 = block0 + (int)((long long)blocks * part / p.parts), b1 = block0 + (int)((long long)blocks * (part + 1) / p.parts);
+
+    // ---- K and V of a block to LDS ----
+    const int piece = lane % kPieces, in_rows = lane / kPieces;
+    const uint16_t *const k_head = p.k + head * p.head_stride, *const v_head = p.v + head * p.head_stride;
+    const int last = max(q.len - 1, 0);
+    int id[kTransfers];
+    const auto key_of = [&](int key0, int i) { return key0 + (i * kWaves + wave) * kRows; };   // first key of a transfer; all in one sixteen
+    const auto find_pages = [&](int key0) {
+#pragma unroll
+        for (int i = 0; i < kTransfers; ++i) id[i] = page_of(p, r, min(key_of(key0, i) + (ANY ? in_rows : 0), last));
+    };
+    const auto request = [&](int key0, uint16_t *to_k, uint16_t *to_v) {
+        int dim = p.head_dim;
+        if (ANY) asm volatile("" : "+v"(dim));  // (compared here, not held as masks through the loop)
+#pragma unroll
+        for (int i = 0; i < kTransfers; ++i) {
+            const int in_lds = (i * kWaves + wave) * kRows + in_rows;
+            const int k_d = 8 * (piece ^ (in_lds & (DT == 64 ? 7 : 15)));
+            const int v_d = 8 * (((piece >> 1 ^ (in_lds & (DT == 64 ? 3 : 7))) << 1) + (piece & 1));
+            const uint16_t *k, *v;
+            if (ANY) {
+                const int key = min(key_of(key0, i) + in_rows, last);     // keys behind the last are the last's copies, and masked
+                const long long at = id[i] * p.page_stride + (long long)((key & ((1 << p.page_shift) - 1)) * p.slot_stride);
+                k = k_d < dim ? k_head + at + k_d : g_zeros;
+                v = v_d < dim ? v_head + at + v_d : g_zeros;
+            } else {
+                const int tile = min(key_of(key0, i), last) & ~15;
+                const long long base = __builtin_amdgcn_readfirstlane(id[i]) * p.page_stride + (long long)((tile & ((1 << p.page_shift) - 1)) * p.slot_stride);
+                const unsigned row = (unsigned)((min(key_of(key0, i) + in_rows, last) - tile) * p.slot_stride);
+                k = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(k_head + base) + 2u * (row + k_d));
+                v = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(v_head + base) + 2u * (row + v_d));
+            }
+            load_to_lds(k, to_k + (i * kWaves + wave) * kRows * DT);
+            load_to_lds(v, to_v + (i * kWaves + wave) * kRows * DT);
+        }
+    };
+    // element d of key j
+    const auto k_at = [&](const uint16_t *buffer, int key, int d) { return buffer + key * DT + ((d >> 3 ^ (key & (DT == 64 ? 7 : 15))) << 3); };
+    const auto v_at = [&](const uint16_t *buffer, int key, int d) {
+        return buffer + key * DT + ((d >> 4 ^ (key & (DT == 64 ? 3 : 7))) << 4) + (d & 15);
+    };
+
+    // ---- Q: lane (h, r32) has of row r32 the elements 16 c + 8 h .. ----
+    u32x4 qr[C];
+    {
+        const uint16_t *const src = p.q + (long long)(q.start + (real ? token : 0)) * p.ld_q + (head * p.group + (real ? member : 0)) * p.head_dim;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int d = 16 * c + 8 * h;
+            qr[c] = u32x4{0, 0, 0, 0};
+            if (real && (!ANY || d < p.head_dim)) qr[c] = *reinterpret_cast<const u32x4 *>(src + d);
+        }
+    }
+    f32x16 o[DV];
+#pragma unroll
+    for (int d = 0; d < DV; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float most = -INFINITY, base = 0.0f, sum = 0.0f;
+
+    const auto step = [&](int b, const uint16_t *kb, uint16_t *vb, uint16_t *next_k, uint16_t *next_v) {
+        const int key0 = b * KB;
+        const bool more = b + 1 < b1;
+        if (more) find_pages(key0 + KB);
+        asm volatile("" ::: "memory");
+        arrived<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (more) request(key0 + KB, next_k, next_v);  // (every wave is through with the other buffers)
+        const bool work = has_rows && key0 < any_to && key0 + KB > any_from;
+        // the operand V^T: elements 32 d + r32 of keys 16 u + 4 h .. and 16 u + 8 + 4 h ..
+        const auto column = [&](int u, int d, int lane) {
+            const int key = 16 * u + 4 * (lane >> 5) + ((lane & 15) >> 2), e = 32 * d + (lane & 16) + 4 * (lane & 3);
+            const u32x2 v0 = lds_column(v_at(vb, key, e)), v1 = lds_column(v_at(vb, key + 8, e));
+            return u32x4{v0.x, v0.y, v1.x, v1.y};
+        };
+        if (key0 + KB > tile_to || key0 < tile_from) {
+            // Not all rows of the tile see all of these keys.  Infinities or NaN among the values: zero times them must not reach the rows that do not
+            // see them.  They are replaced by zeros, and what they make of the rows that do, an infinity or a NaN, is found by products of ones.  (Every wave looks at the whole block, so all of them meet at the barriers or none.)
+            int it = lane;
+            asm volatile("" : "+v"(it));  // what follows from it is not worth registers over the loop
+            bool odd = false;
+#pragma unroll 1
+            for (int i = it; i < KB * DT / 8; i += 64) {
+                const u32x4 x = *reinterpret_cast<const u32x4 *>(vb + 8 * i);
+                odd |= not_finite<BF>(x[0]) || not_finite<BF>(x[1]) || not_finite<BF>(x[2]) || not_finite<BF>(x[3]);
+            }
+            if (__ballot(odd)) {
+                if (work) {
+                    const unsigned span = max(to - from, 0);
+#pragma unroll
+                    for (int d = 0; d < DV; ++d) {
+#pragma unroll 1
+                        for (uint32_t sign = 0; sign <= 0x8000u; sign += 0x8000u) {
+                            f32x16 found;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) found[i] = 0.0f;
+#pragma unroll 1
+                            for (int u = 0; u < KB / 16; ++u) {
+                                u32x4 a = column(u, d, it), sees;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const int key = key0 + 16 * u + 8 * (e >> 1) + 4 * (it >> 5) + 2 * (e & 1);
+                                    sees[e] = ((unsigned)(key - from) < span ? kOne<BF> : 0u) | ((unsigned)(key + 1 - from) < span ? kOne<BF> << 16 : 0u);
+                                    a[e] = ones_where_infinite<BF>(a[e], sign);
+                                }
+                                found = mfma32<BF>(a, sees, found);
+                            }
+                            const float infinity = sign ? -INFINITY : INFINITY;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[d][i] += found[i] > 0.0f ? infinity : 0.0f;
+                        }
+                        asm volatile("" : "+v"(o[d]));  // (before the next ones)
+                    }
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+#pragma unroll 1
+                for (int i = wave * 64 + it; i < KB * DT / 8; i += 64 * kWaves) {
+                    u32x4 x = *reinterpret_cast<const u32x4 *>(vb + 8 * i);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = finite_only<BF>(x[e]);
+                    *reinterpret_cast<u32x4 *>(vb + 8 * i) = x;
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+            }
+        }
+        u32x4 weight[KB / 16];
+        if (work) {
+            f32x16 s[KT];
+#pragma unroll
+            for (int t = 0; t < KT; ++t) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const u32x4 a = *reinterpret_cast<const u32x4 *>(k_at(kb, 32 * t + r32, 16 * c + 8 * h));
+                    s[t] = mfma32<BF>(a, qr[c], s[t]);
+                }
+            }
+            // number 16 t + 4 u + i of a lane is key 32 t + 8 u + 4 h + i
+            float x[16 * KT];
+#pragma unroll
+            for (int e = 0; e < 16 * KT; ++e) x[e] = s[e >> 4][e & 15];
+            if (key0 + KB > all_to || key0 < all_from) {
+                const unsigned span = max(to - from, 0);
+#pragma unroll
+                for (int e = 0; e < 16 * KT; ++e)
+                    x[e] = (unsigned)(key0 + 32 * (e >> 4) + 8 * (e >> 2 & 3) + 4 * h + (e & 3) - from) < span ? x[e] : -INFINITY;
+            }
+            float high = x[0];
+#pragma unroll
+            for (int e = 1; e < 16 * KT; ++e) high = fmaxf(high, x[e]);
+            high *= p.scale;
+            if (__ballot(high > most + kGrow)) {
+                const auto other = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, high), __builtin_bit_cast(unsigned, high), false, false);
+                const float m = fmaxf(most, fmaxf(__builtin_bit_cast(float, (unsigned)other[0]), __builtin_bit_cast(float, (unsigned)other[1])));
+                const float shrink = most == -INFINITY ? 1.0f : exp2_fast(most - m);
+                most = m;
+                base = m == -INFINITY ? 0.0f : m;
+                sum *= shrink;
+#pragma unroll
+                for (int d = 0; d < DV; ++d) o[d] *= shrink;
+            }
+#pragma unroll
+            for (int e = 0; e < 16 * KT; e += 2) {
+                const float w0 = exp2_fast(fmaf(x[e], p.scale, -base)), w1 = exp2_fast(fmaf(x[e + 1], p.scale, -base));
+                sum += w0 + w1;
+                weight[e >> 3][e >> 1 & 3] = from_float2<BF>(w0, w1);
+            }
+        }
+        if (work) {
+#pragma unroll
+            for (int u = 0; u < KB / 16; ++u)
+#pragma unroll
+                for (int d = 0; d < DV; ++d) o[d] = mfma32<BF>(column(u, d, lane), weight[u], o[d]);
+        }
+    };
+    if (b0 < b1) {
+        find_pages(b0 * KB);
+        request(b0 * KB, k0, v0);
+    }
+    for (int b = b0; b < b1; b += 2) {
+        step(b, k0, v0, k1, v1);
+        if (b + 1 < b1) step(b + 1, k1, v1, k0, v0);
+    }
+
+    // ---- results: lane (h, r32) has of row r32 the elements 32 d + 8 u + 4 h + i in number 4 u + i of o[d] ----
+    const auto twin = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, sum), __builtin_bit_cast(unsigned, sum), false, false);
+    sum = __builtin_bit_cast(float, (unsigned)twin[0]) + __builtin_bit_cast(float, (unsigned)twin[1]);
+    if (!real) return;
+    if (p.parts == 1) {
+        const float unit = 1.0f / sum;
+        const bool empty = to <= from;
+        uint16_t *const dst = p.out + (long long)(q.start + token) * p.ld_out + (head * p.group + member) * p.head_dim;
+#pragma unroll
+        for (int d = 0; d < DV; ++d)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int e = 32 * d + 8 * u + 4 * h;
+                float y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[i] = empty ? 0.0f : o[d][4 * u + i] * unit;
+                if (!ANY || e < p.head_dim) *reinterpret_cast<u32x2 *>(dst + e) = u32x2{from_float2<BF>(y[0], y[1]), from_float2<BF>(y[2], y[3])};
+            }
+    } else {
+        const long long at = ((long long)part * p.kv_heads + head) * p.tokens * p.group + (long long)q.start * p.group + row;
+#pragma unroll
+        for (int d = 0; d < DV; ++d)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                *reinterpret_cast<f32x4 *>(p.part + at * DT + 32 * d + 8 * u + 4 * h) =
+                    f32x4{o[d][4 * u], o[d][4 * u + 1], o[d][4 * u + 2], o[d][4 * u + 3]};
+        if (h == 0) p.stat[at] = f32x2{most, sum};
+    }
+}
+
+// Joins the parts: a wave per row.
+template <int DT, bool BF>
+__global__ __launch_bounds__(64) void bcq_attend_chunk_join_kernel(AttendParams p)
+{
+    constexpr int E = DT / 64;
+    const int lane = threadIdx.x, token = blockIdx.x / p.group, member = blockIdx.x % p.group, head = blockIdx.y;
+    int r = 0;
+    for (int high = p.requests; high - r > 1;) {
+        const int middle = (r + high) >> 1;
+        if (p.q_start[middle] <= token) r = middle;
+        else high = middle;
+    }
+    const Request q = load_request(p, r);
+    const int i = token - q.start;
+    if (i < 0 || i >= q.todo || q.todo * p.group <= p.rows) return;
+    const long long step = (long long)p.kv_heads * p.tokens * p.group, at = (long long)head * p.tokens * p.group + blockIdx.x;
+    float most = -INFINITY;
+    for (int k = lane; k < p.parts; k += 64) most = fmaxf(most, p.stat[k * step + at].x);
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+    const float base = most == -INFINITY ? 0.0f : most;
+    float weight = 0.0f, y[E] = {};
+#pragma unroll 4
+    for (int k = 0; k < p.parts; ++k) {
+        const f32x2 stat = p.stat[k * step + at];
+        const float scale = exp2_fast(stat.x - base);
+        weight = fmaf(stat.y, scale, weight);
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] = fmaf(p.part[(k * step + at) * DT + lane * E + e], scale, y[e]);
+    }
+    int from, to;
+    visible_keys(p, q.n, q.len, i, from, to);
+    uint16_t *const dst = p.out + (long long)token * p.ld_out + (head * p.group + member) * p.head_dim;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (lane * E + e < p.head_dim) dst[lane * E + e] = from_float<BF>(to > from ? y[e] / weight : 0.0f);
+}
+
+// Pieces that the keys of a tile are cut into: enough workgroups for two on every compute unit, none with fewer than four blocks of the longest row of pages.
+int chunk_parts(int tokens, int group, int kv_heads, int dim, long long most_keys)
+{
+    const long long tiles = ((long long)tokens * group / kChunkRows + 1) * kv_heads;
+    const long long wanted = (long long)compute_units() * chunk_occupancy(dim) / tiles, most = most_keys / (4 * chunk_keys(dim));
+    const long long parts = wanted < most ? wanted : most;
+    return (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+}
+
+template <int DT, bool BF>
+static void chunks(const AttendParams &p, bool any, hipStream_t s)
+{
+    const long long slots = (long long)p.tokens * p.group / kChunkRows + p.requests;
+    const dim3 grid((unsigned)(slots * p.kv_heads), p.parts);
+    if (any) bcq_attend_chunk_kernel<DT, BF, true><<<grid, 64 * kWaves, 0, s>>>(p);
+    else bcq_attend_chunk_kernel<DT, BF, false><<<grid, 64 * kWaves, 0, s>>>(p);
+    if (p.parts > 1) bcq_attend_chunk_join_kernel<DT, BF><<<dim3(p.tokens * p.group, p.kv_heads), 64, 0, s>>>(p);
+}
+
+template <bool BF>
+static void by_dim(const AttendParams &p, int dim, bool any, hipStream_t s)
+{
+    if (dim == 64) chunks<64, BF>(p, any, s);
+    else if (dim == 128) chunks<128, BF>(p, any, s);
+    else chunks<256, BF>(p, any, s);
+}
+
+void launch_chunks(const AttendParams &p, int dim, bool any, bool bf16, hipStream_t s)
+{
+    if (bf16) by_dim<true>(p, dim, any, s);
+    else by_dim<false>(p, dim, any, s);
+}
+
+}  // namespace bcq

@@ -95,7 +95,7 @@ struct AttendArgs {
     void *workspace;
     bcq_cache cache;
 };
-size_t attend_workspace_bytes(const bcq_cache &c, int tokens, int requests, int q_heads, int max_new);
+size_t attend_workspace_bytes(const bcq_cache &c, int tokens, int requests, int q_heads, int max_new, int max_pages);
 hipError_t launch_attend(const AttendArgs &a, hipStream_t stream);
 
 struct LoraArgs {

@@ -73,19 +73,22 @@ bcq_status bcq_rotate(const bcq_cache *cache, int32_t tokens, int32_t q_heads, c
     return launch_rotate(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
 }
 
-static bcq_status attend_shape(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_new)
+static bcq_status attend_shape(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_pages, int32_t max_new)
 {
     bcq_status why;
     if (!cache_ok(cache, &why)) return why;
-    if (tokens < 0 || requests < 0 || q_heads < 1 || q_heads % cache->kv_heads || max_new < 1) return BCQ_ERR_INVALID_ARG;
+    if (tokens < 0 || requests < 0 || q_heads < 1 || q_heads % cache->kv_heads || max_pages < 1 || max_new < 1) return BCQ_ERR_INVALID_ARG;
     if (tokens > kMaxTokens || requests > kMaxTokens || q_heads > 1024) return BCQ_ERR_UNSUPPORTED;
+    if ((int64_t)max_pages * cache->page_size > (1 << 30) || (int64_t)requests * (max_pages * (int64_t)cache->page_size / 32 + 1) > 0x7fffffffLL)
+        return BCQ_ERR_UNSUPPORTED;  // keys of a request, and blocks of keys of all requests, are int
     return BCQ_OK;
 }
 
-size_t bcq_attend_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_new)
+size_t bcq_attend_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_pages,
+                                  int32_t max_new)
 {
-    if (attend_shape(cache, tokens, requests, q_heads, max_new) != BCQ_OK || tokens == 0 || requests == 0) return 0;
-    return attend_workspace_bytes(*cache, tokens, requests, q_heads, max_new);
+    if (attend_shape(cache, tokens, requests, q_heads, max_pages, max_new) != BCQ_OK || tokens == 0 || requests == 0) return 0;
+    return attend_workspace_bytes(*cache, tokens, requests, q_heads, max_new, max_pages);
 }
 
 bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v_cache, int32_t tokens, int32_t requests,
@@ -93,18 +96,17 @@ bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v
                       const int32_t *pages, int32_t max_pages, int32_t max_new, float scale, int32_t causal, int32_t window,
                       void *out, int64_t ld_out, void *workspace, void *stream)
 {
-    const bcq_status why = attend_shape(cache, tokens, requests, q_heads, max_new);
+    const bcq_status why = attend_shape(cache, tokens, requests, q_heads, max_pages, max_new);
     if (why != BCQ_OK) return why;
     const int64_t cols = (int64_t)q_heads * cache->head_dim;
-    if (!row_stride_ok(ld_q, cols) || !row_stride_ok(ld_out, cols) || max_pages < 1) return BCQ_ERR_INVALID_ARG;
+    if (!row_stride_ok(ld_q, cols) || !row_stride_ok(ld_out, cols) ) return BCQ_ERR_INVALID_ARG;
     if (!(scale > 0.0f) || isinf(scale) || (causal != 0 && causal != 1) || window < 0 || (window > 0 && !causal)) return BCQ_ERR_INVALID_ARG;
-    if ((int64_t)max_pages * cache->page_size > (1 << 30)) return BCQ_ERR_UNSUPPORTED;
     if (tokens == 0 || requests == 0) return BCQ_OK;
     if (!k_cache || !v_cache || !q || !q_start || !kv_len || !pages || !out) return BCQ_ERR_INVALID_ARG;
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(q_start, 4) || !aligned(kv_len, 4) ||
         !aligned(pages, 4))
         return BCQ_ERR_INVALID_ARG;
-    if (attend_workspace_bytes(*cache, tokens, requests, q_heads, max_new) > 0 && (!workspace || !aligned(workspace, 16))) return BCQ_ERR_WORKSPACE;
+    if (attend_workspace_bytes(*cache, tokens, requests, q_heads, max_new, max_pages) > 0 && (!workspace || !aligned(workspace, 16))) return BCQ_ERR_WORKSPACE;
     AttendArgs a{half(k_cache), half(v_cache), half(q), q_start, kv_len, pages, half(out), ld_q, ld_out, tokens, requests, q_heads, max_pages,
                  max_new, window, scale, causal != 0, workspace, *cache};
     return launch_attend(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;

@@ -91,7 +91,7 @@ class PagedCache:
             out = torch.empty((T, q_heads * D), dtype=self.dtype, device=self.device)
         _need(out.shape[0] == T, where, "out: a row per token")
         ld_out = _rows(where, "out", out, q_heads * D, self.dtype, self.device)
-        nbytes = B.attend_workspace_bytes(self.desc, T, R, q_heads, max_new)
+        nbytes = B.attend_workspace_bytes(self.desc, T, R, q_heads, pages.shape[1], max_new)
         ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
         B.attend(self.desc, self.k, self.v, T, R, q_heads, q, ld, q_start, kv_len, pages, pages.shape[1], max_new,
                  D ** -0.5 if scale is None else scale, causal, window, out, ld_out, ws)

@@ -86,9 +86,9 @@ def test_attend_limits_and_workspace():
     assert attend(cache(), tokens=0, q=None) == B.BCQ_OK
     assert attend(cache(), requests=0, q=None) == B.BCQ_OK
     c = cache()
-    assert bcq.attend_workspace_bytes(c, 0, 4, 64, 1) == 0
-    assert bcq.attend_workspace_bytes(c, 4, 4, 60, 1) == 0
-    if bcq.attend_workspace_bytes(c, 4, 2, 64, 2):
+    assert bcq.attend_workspace_bytes(c, 0, 4, 64, 10, 1) == 0
+    assert bcq.attend_workspace_bytes(c, 4, 4, 60, 10, 1) == 0
+    if bcq.attend_workspace_bytes(c, 4, 2, 64, 10, 2):
         assert attend(c, workspace=None) == B.BCQ_ERR_WORKSPACE
         assert attend(c, workspace=OK + 4) == B.BCQ_ERR_WORKSPACE
 
