@@ -32,12 +32,8 @@ __device__ __forceinline__ void load_to_lds(const uint16_t *from, uint16_t *to)
     __builtin_amdgcn_global_load_lds((global_void)from, (lds_void)to, 16, 0, 0);
 }
 
-// All but the newest `most` requests of this wave have arrived.
-template <int most>
-__device__ __forceinline__ void arrived()
-{
-    __builtin_amdgcn_s_waitcnt((most & 15) | (most >> 4) << 14 | 0xf70);  // (the other counters' fields: no wait)
-}
+// This wave's transfers to LDS have arrived, and its reads of LDS have returned: what the barrier after it promises the other waves.
+__device__ __forceinline__ void all_arrived() { __builtin_amdgcn_s_waitcnt(0x0070); }  // vmcnt(0) lgkmcnt(0)
 
 __device__ __forceinline__ int tile_slots_before(const AttendParams &p, int r)
 {
@@ -152,7 +148,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
         const bool more = b + 1 < b1;
         if (more) find_pages(key0 + KB);
         asm volatile("" ::: "memory");
-        arrived<0>();
+        all_arrived();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (more) request(key0 + KB, next_k, next_v);  // (every wave is through with the other buffers)
@@ -202,7 +198,8 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
                         asm volatile("" : "+v"(o[d]));  // (before the next ones)
                     }
                 }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                asm volatile("" ::: "memory");
+                all_arrived();
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
 #pragma unroll 1
@@ -212,7 +209,8 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
                     for (int e = 0; e < 4; ++e) x[e] = finite_only<BF>(x[e]);
                     *reinterpret_cast<u32x4 *>(vb + 8 * i) = x;
                 }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                asm volatile("" ::: "memory");
+                all_arrived();
                 __builtin_amdgcn_s_barrier();
                 asm volatile("" ::: "memory");
             }

@@ -35,7 +35,7 @@ bool adapters_ok(const bcq_adapters *d, bcq_status *why)
     if (!d || (d->dtype != BCQ_F16 && d->dtype != BCQ_BF16)) return false;
     if (d->count < 1 || d->max_rank < 1 || d->M < 1 || d->N < 1 || d->N % 8 || d->max_rank % 8) return false;
     *why = BCQ_ERR_UNSUPPORTED;
-    if (d->max_rank > BCQ_MAX_RANK || d->M > (1 << 24) || d->N > (1 << 24)) return false;
+    if (d->max_rank > BCQ_MAX_RANK || d->M > (1 << 23) || d->N > (1 << 23)) return false;
     *why = BCQ_OK;
     return true;
 }
