@@ -135,6 +135,18 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+_current_raw_stream = None
+
+
+def raw_stream(device_index):
+    """hipStream_t of torch's current stream of a device, as a number (see _stream)."""
+    global _current_raw_stream
+    if _current_raw_stream is None:
+        import torch
+        _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _current_raw_stream(device_index)
+
+
 def packed_bytes(desc):
     return int(lib().bcq_packed_bytes(ctypes.byref(desc)))
 

@@ -17,6 +17,7 @@ HIPCC_FLAGS = [
 
 
 TRACE_LIB = os.path.join(HERE, "libbcq_trace.so")
+SERVING_LIB = os.path.join(HERE, "_serving.so")
 
 
 def sources():
@@ -67,8 +68,24 @@ def kernel_resources(stderr_text):
     return res
 
 
+def build_serving(verbose=False):
+    """_serving.so: the objects of serving.py over torch tensors (host code only, against torch's headers)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    dirs = cpp_extension.library_paths()
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
+           "-I" + sysconfig.get_paths()["include"]] + ["-isystem" + d for d in cpp_extension.include_paths()] + \
+        [os.path.join(CSRC, "bcq_torch.cpp"), "-o", SERVING_LIB] + ["-L" + d for d in dirs] + ["-lc10", "-ltorch_cpu", "-ltorch_python"]
+    if verbose:
+        print(" ".join(cmd))
+    subprocess.run(cmd, check=True)
+    return SERVING_LIB
+
+
 def build(verbose=False, extra_flags=()):
-    """Compile every kernel for gfx950 and link libbcq.so.  Fails if a compute kernel (GEMV,
+    """Compile every kernel for gfx950 and link libbcq.so, then build _serving.so.  Fails if a compute kernel (GEMV,
     skinny GEMM) needs scratch memory or spills registers: those kernels are sized to keep
     everything in registers, and a spill would silently cost HBM traffic."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -106,6 +123,7 @@ def build(verbose=False, extra_flags=()):
     if verbose:
         for k, v in sorted(hot.items()):
             print(f"{k}: VGPRs {v.get('VGPRs')} AGPRs {v.get('AGPRs')} occupancy {v.get('Occupancy')}")
+    build_serving(verbose)
     return LIB
 
 
