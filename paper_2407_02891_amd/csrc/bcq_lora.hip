@@ -8,8 +8,8 @@
 //    the chip, leave their sums in binary32 side by side, and whoever reads them adds them in order.
 //  * Y = base + B v: a workgroup has a tile and a range of rows of B.  v (times the scale) is held as a sum of 16-bit numbers beside the 16-bit rows of B:
 //    two for binary16 (after a power of two for each token: 22 bits and more of its largest value), three for bfloat16 (24 bits).  The operand's 32
-//    places are 16 of v's first numbers and the same 16 of its second ones.  The rows of B are numbered so that a lane ends up with 16
-//    neighbouring outputs of a token.
+//    places are 16 of v's first numbers and the same 16 of its second ones.  The rows of B are numbered so that a lane ends up with eight
+//    neighbouring outputs of a token and four lanes with 32.
 #include "bcq_half.h"
 #include "bcq_internal.h"
 
@@ -86,8 +86,8 @@ __global__ __launch_bounds__(1024) void bcq_lora_plan_kernel(LoraParams p, int t
     __shared__ int scan_tokens[1024], scan_tiles[1024], few_cursors[kPlanGroups];
     const int tid = threadIdx.x, groups = p.a.desc.count + 1;
     int *const cursor = groups <= kPlanGroups ? few_cursors : p.cursor;
-    const auto all_see = [] {  // (the cursors may be in memory, whose atomics pass by the caches of loads and stores)
-        __threadfence();
+    const auto all_see = [&] {  // (cursors in memory: their atomics pass by the caches of loads and stores)
+        if (groups > kPlanGroups) __threadfence();
         __syncthreads();
     };
     for (int g = tid; g < groups; g += 1024) __hip_atomic_store(&cursor[g], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -223,8 +223,30 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
     const int M = p.a.desc.M, width = p.a.desc.max_rank, third = steps * NT * 64;
     const float scale = tile.adapter >= 0 && p.a.scale ? p.a.scale[tile.adapter] : 1.0f;
 
+    // ---- rows: lane (g, r16) ends up with outputs 8 g .. + 7 of each 32 of token r16: row r of tile q is output 32 (q / 2) + 8 (r / 4) + 4 (q mod 2) + r mod 4.
+    // What a group of 64 rows needs first, base and the first columns of B, is requested before v is made, and for the next group before this one's stores ----
+    const auto first_row = [&](int group) { return (int)((group * gridDim.y + blockIdx.y) * kWaves + wave) * 64; };  // (the workgroups' rows of one moment are neighbours)
+    const int widest = width > 8 ? 8 * (g & 1) : 0;  // (a row of B may have eight columns only; what is loaded twice is masked)
+    u32x4 out[NT][2], head[4];
+    const uint16_t *b[4];
+    const auto request = [&](int row0) {
+        if (row0 >= M) return;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            b[q] = p.a.B + ((long long)max(tile.adapter, 0) * M + min(row0 + 32 * (q >> 1) + 8 * (r16 >> 2) + 4 * (q & 1) + (r16 & 3), M - 1)) * width;
+            if (steps) head[q] = *reinterpret_cast<const u32x4 *>(b[q] + widest);
+        }
+        if (p.wide && row0 + 64 <= M) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    out[nt][h] = *reinterpret_cast<const u32x4 *>(p.a.base + (long long)members[16 * nt + r16] * p.a.ld_base + row0 + 32 * h + 8 * g);
+        }
+    };
     // ---- v ----
     float v[kItems][8];
+    request(first_row(0));
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
         const int item = threadIdx.x + k * 64 * kWaves, token = item % kTokens, j = item / kTokens * 8;
@@ -274,7 +296,6 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
     }
     __syncthreads();
 
-    // ---- rows: lane (g, r16) ends up with outputs row0 + 16 g .. + 15 of token r16; row r of tile q is output row0 + 16 (r / 4) + 4 q + r mod 4 ----
     u32x4 kept_last;  // of the last step: the columns that belong to the adapter
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -282,24 +303,24 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
         kept_last[i] = (j < rank ? 0xffffu : 0u) | (j + 1 < rank ? 0xffff0000u : 0u);
     }
     for (int group = 0; group < p.row_groups; ++group) {
-        const int row0 = ((blockIdx.y * p.row_groups + group) * kWaves + wave) * 64;
+        const int row0 = first_row(group);
         if (row0 >= M) break;
+        const bool vector = p.wide && row0 + 64 <= M;
         f32x4 acc[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int q = 0; q < 4; ++q) acc[nt][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        const uint16_t *b[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            b[q] = p.a.B + ((long long)max(tile.adapter, 0) * M + min(row0 + 16 * (r16 >> 2) + 4 * q + (r16 & 3), M - 1)) * width + 8 * (g & 1);
-#pragma unroll 2
+        u32x4 ahead[4];
         for (int s = 0; s < steps; ++s) {
             u32x4 rows[4];
-            // (a rank that ends in the first eight of a sixteen may be all that a row of B has)
-            const int at = 16 * s + (16 * s + 8 * (g & 1) < width ? 0 : -8);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) rows[q] = *reinterpret_cast<const u32x4 *>(b[q] + at);
+            for (int q = 0; q < 4; ++q) rows[q] = s ? ahead[q] : head[q];
+            if (s + 1 < steps) {
+                const int at = 16 * (s + 1) + 8 * (g & 1) < width ? 16 * (s + 1) + 8 * (g & 1) : 16 * (s + 1);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) ahead[q] = *reinterpret_cast<const u32x4 *>(b[q] + at);
+            }
             if (s == steps - 1) {
 #pragma unroll
                 for (int q = 0; q < 4; ++q) rows[q] &= kept_last;
@@ -316,33 +337,35 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
                 }
             }
         }
-        const int m = row0 + 16 * g;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int token = 16 * nt + r16;
-            if (token >= tile.count || m >= M) continue;
+            if (token >= tile.count) continue;
             const float unit = BF || steps == 0 ? 1.0f : ldexpf(1.0f, exponent(token));
-            const uint16_t *const base = p.a.base + (long long)members[token] * p.a.ld_base + m;
-            uint16_t *const y = p.a.Y + (long long)members[token] * p.a.ldy + m;
-            if (p.wide && m + 16 <= M) {
+            const uint16_t *const base = p.a.base + (long long)members[token] * p.a.ld_base;
+            uint16_t *const y = p.a.Y + (long long)members[token] * p.a.ldy;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    u32x4 pairs = *reinterpret_cast<const u32x4 *>(base + 8 * h);
+            for (int h = 0; h < 2; ++h) {
+                const int m = row0 + 32 * h + 8 * g;
+                if (vector) {
+                    u32x4 pairs = out[nt][h];
                     if (steps) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const f32x2 x = to_float2<BF>(pairs[i]);
-                            pairs[i] = from_float2<BF>(fmaf(acc[nt][2 * h + (i >> 1)][2 * (i & 1)], unit, x.x), fmaf(acc[nt][2 * h + (i >> 1)][2 * (i & 1) + 1], unit, x.y));
+                            const f32x4 a = acc[nt][2 * h + (i >> 1)];
+                            pairs[i] = from_float2<BF>(fmaf(a[2 * (i & 1)], unit, x.x), fmaf(a[2 * (i & 1) + 1], unit, x.y));
                         }
                     }
-                    *reinterpret_cast<u32x4 *>(y + 8 * h) = pairs;
-                }
-            } else {
+                    *reinterpret_cast<u32x4 *>(y + m) = pairs;
+                } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (m + i < M) y[i] = steps ? from_float<BF>(fmaf(acc[nt][i >> 2][i & 3], unit, to_float<BF>(base[i]))) : base[i];
+                    for (int i = 0; i < 8; ++i)
+                        if (m + i < M) y[m + i] = steps ? from_float<BF>(fmaf(acc[nt][2 * h + (i >> 2)][i & 3], unit, to_float<BF>(base[m + i]))) : base[m + i];
+                }
             }
         }
+        if (group + 1 < p.row_groups) request(first_row(group + 1));
     }
 }
 
@@ -373,10 +396,14 @@ LoraPlan lora_plan(const bcq_adapters &d, int tokens)
     const int likely = s.few ? (tokens < d.count ? tokens : d.count) : s.slots;  // tiles, if adapters are spread
     const int wanted = 2 * compute_units() / (likely * s.row_blocks), longest = (d.N + 511) / 512;
     s.slices = wanted < longest ? wanted : longest;
-    s.slices = s.slices < 1 ? 1 : s.slices > 16 ? 16 : s.slices;
+    // (with 64 tokens a tile there is work enough, and every workgroup of the second launch reads all slices: 4 slices 124 us, 13 134, 2 140 for 2048 tokens,
+    // rank 64, 7168 to 28672; one token, rank 64, 28672 to 7168: 16 slices 17 us, 8 23, 4 38)
+    const int cap = s.tiles == 4 ? 4 : 16;
+    s.slices = s.slices < 1 ? 1 : s.slices > cap ? cap : s.slices;
     const int blocks = (d.M + 64 * kWaves - 1) / (64 * kWaves);
-    const long long groups = (long long)blocks * likely / (4 * compute_units());
-    s.row_groups = (int)(groups < 1 ? 1 : groups > 8 ? 8 : groups);
+    // as many workgroups as the chip holds at once (registers: two to a compute unit with 64 tokens, four with 16), so that each makes v once
+    const long long resident = (s.tiles == 4 ? 2 : 4) * compute_units(), groups = ((long long)blocks * (s.few ? likely : tokens / (16 * s.tiles) + 1) + resident - 1) / resident;
+    s.row_groups = (int)(groups < 1 ? 1 : groups > 16 ? 16 : groups);
     s.part_bytes = whole((size_t)s.slices * tokens * d.max_rank * sizeof(float));
     s.order_bytes = s.few ? 0 : whole((size_t)tokens * sizeof(int));
     s.tile_bytes = s.few ? 0 : whole((size_t)(1 + 3 * s.slots) * sizeof(int));
