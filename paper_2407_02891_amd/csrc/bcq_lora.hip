@@ -19,14 +19,18 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kFewTokens = 64;     // that every wave sorts out by itself
+constexpr int kManyTokens = 64;    // a tile where adapters have many
 constexpr int kPlanGroups = 4096;  // adapters (and none) whose tokens are counted in LDS
 
 struct LoraParams {
     LoraArgs a;
     float *part;       // [slice][token][max_rank]
-    int *order;        // many tokens: by adapter
-    int *tiles;        // many tokens: {adapter or -1, first of order, count} each, their number in front
+    int *order;        // more than kFewTokens: tokens by tile; behind a tile's last one nothing
+    int *tiles;        // more than kFewTokens: {adapter or -1, tokens} each, their number in front
     int *cursor;       // many adapters: scratch, one per adapter and one for none
+    u32x4 *operands;   // many tokens of few adapters: v as matrix operands, by tile
+    float *units;      // and what they are to be multiplied by, [tile][64]
+    int operand_pieces;  // 16-byte pieces of sixteen tokens' operands
     int slices;
     int row_groups;    // expand: groups of 64 rows of B of a wave
     bool copy;         // Y is not base
@@ -69,10 +73,9 @@ __device__ __forceinline__ Tile find_tile(const LoraParams &p, int slot, int *me
         }
     } else {
         if (slot >= p.tiles[0]) return {-1, 0};
-        const int *const t = p.tiles + 1 + 3 * slot;
-        tile.adapter = t[0];
-        tile.count = t[2];
-        if (threadIdx.x < TOKENS) members[threadIdx.x] = p.order[t[1] + (threadIdx.x < tile.count ? threadIdx.x : 0)];
+        tile.adapter = p.tiles[2 + 2 * slot];
+        tile.count = p.tiles[3 + 2 * slot];
+        if (threadIdx.x < TOKENS) members[threadIdx.x] = p.order[slot * TOKENS + (threadIdx.x < tile.count ? threadIdx.x : 0)];
     }
     __syncthreads();
     return tile;
@@ -83,7 +86,7 @@ __device__ __forceinline__ Tile find_tile(const LoraParams &p, int slot, int *me
 // Many tokens: sorts them by adapter and lists the tiles.  One workgroup; which of an adapter's tokens share a tile has no part in the result.
 __global__ __launch_bounds__(1024) void bcq_lora_plan_kernel(LoraParams p, int tile_tokens)
 {
-    __shared__ int scan_tokens[1024], scan_tiles[1024], few_cursors[kPlanGroups];
+    __shared__ int scan[1024], few_cursors[kPlanGroups];
     const int tid = threadIdx.x, groups = p.a.desc.count + 1;
     int *const cursor = groups <= kPlanGroups ? few_cursors : p.cursor;
     const auto all_see = [&] {  // (cursors in memory: their atomics pass by the caches of loads and stores)
@@ -92,41 +95,171 @@ __global__ __launch_bounds__(1024) void bcq_lora_plan_kernel(LoraParams p, int t
     };
     for (int g = tid; g < groups; g += 1024) __hip_atomic_store(&cursor[g], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     all_see();
-    for (int t = tid; t < p.a.tokens; t += 1024) {
+    // this lane's place among all that add one to the same cursor: one atomic for each of a wave's adapters (a request's tokens are neighbours)
+    const auto next_of = [&](int g) {
+        int place = 0;
+        for (unsigned long long left = __ballot(g >= 0); left;) {
+            const int one = __builtin_amdgcn_readlane(g, __builtin_ctzll(left));
+            const unsigned long long same = __ballot(g == one);
+            int from = 0;
+            if ((threadIdx.x & 63) == (unsigned)__builtin_ctzll(left)) from = atomicAdd(&cursor[one], __popcll(same));
+            from = __builtin_amdgcn_readlane(from, __builtin_ctzll(left));
+            if (g == one) place = from + __popcll(same & ((1ull << (threadIdx.x & 63)) - 1));
+            left &= ~same;
+        }
+        return place;
+    };
+    const auto group_of = [&](int t) {
+        if (t >= p.a.tokens) return -1;
         const int id = adapter_of(p.a, t);
-        atomicAdd(&cursor[id < 0 ? groups - 1 : id], 1);
-    }
+        return id < 0 ? groups - 1 : id;
+    };
+    for (int t = 0; t < p.a.tokens; t += 1024) next_of(group_of(t + tid));
     all_see();
-    int token_base = 0, tile_base = 0;
+    int tile_base = 0;
     for (int g0 = 0; g0 < groups; g0 += 1024) {
         const int g = g0 + tid, count = g < groups ? __hip_atomic_load(&cursor[g], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
         const int tiles = (count + tile_tokens - 1) / tile_tokens;
-        scan_tokens[tid] = count, scan_tiles[tid] = tiles;
+        scan[tid] = tiles;
         __syncthreads();
         for (int step = 1; step < 1024 && step < groups; step <<= 1) {
-            const int a = tid >= step ? scan_tokens[tid - step] : 0, b = tid >= step ? scan_tiles[tid - step] : 0;
+            const int before = tid >= step ? scan[tid - step] : 0;
             __syncthreads();
-            scan_tokens[tid] += a, scan_tiles[tid] += b;
+            scan[tid] += before;
             __syncthreads();
         }
-        const int first = token_base + scan_tokens[tid] - count, first_tile = tile_base + scan_tiles[tid] - tiles;
+        const int first = tile_base + scan[tid] - tiles;
         for (int k = 0; k < tiles; ++k) {
-            int *const t = p.tiles + 1 + 3 * (first_tile + k);
-            t[0] = g == groups - 1 ? -1 : g;
-            t[1] = first + k * tile_tokens;
-            t[2] = min(tile_tokens, count - k * tile_tokens);
+            p.tiles[2 + 2 * (first + k)] = g == groups - 1 ? -1 : g;
+            p.tiles[3 + 2 * (first + k)] = min(tile_tokens, count - k * tile_tokens);
         }
-        if (g < groups) __hip_atomic_store(&cursor[g], first, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        const int last = min(groups - g0, 1024) - 1;
-        token_base += scan_tokens[last], tile_base += scan_tiles[last];
+        if (g < groups) __hip_atomic_store(&cursor[g], first * tile_tokens, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        tile_base += scan[min(groups - g0, 1024) - 1];
         __syncthreads();
     }
     if (tid == 0) p.tiles[0] = tile_base;
     all_see();
-    for (int t = tid; t < p.a.tokens; t += 1024) {
-        const int id = adapter_of(p.a, t);
-        p.order[atomicAdd(&cursor[id < 0 ? groups - 1 : id], 1)] = t;
+    for (int t = 0; t < p.a.tokens; t += 1024) {
+        const int place = next_of(group_of(t + tid));
+        if (t + tid < p.a.tokens) p.order[place] = t + tid;
     }
+}
+
+// Sums of the steps s0 .. s1 - 1 of 32 columns: RT sixteens of rows of A[adapter] from row0 on, times NT sixteens of tokens, those of this lane's columns in
+// `tokens`.  Rows behind the rank are copies of its last.
+template <bool BF, int NT, int RT>
+__device__ __forceinline__ void shrink_products(const LoraArgs &p, int adapter, const int (&tokens)[NT], int row0, int rank, int s0, int s1, int lane,
+                                                f32x4 (&acc)[NT][RT])
+{
+    const int r16 = lane & 15, g = lane >> 4, N = p.desc.N;
+    const uint16_t *x[NT], *a[RT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) x[nt] = p.X + (long long)tokens[nt] * p.ldx + 8 * g;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) a[rt] = p.A + ((long long)adapter * p.desc.max_rank + min(row0 + 16 * rt + r16, rank - 1)) * N + 8 * g;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[nt][rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    // Steps whose loads are under way together, and as many that are used meanwhile (the compiler would rather save the registers and load one at a time).
+    constexpr int kUnroll = NT + RT > 5 ? 2 : 4;
+    u32x4 xr[2][kUnroll][NT], ar[2][kUnroll][RT];
+    const auto load = [&](int s, int to) {
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) ar[to][k][rt] = *reinterpret_cast<const u32x4 *>(a[rt] + 32 * (s + k));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) xr[to][k][nt] = *reinterpret_cast<const u32x4 *>(x[nt] + 32 * (s + k));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto products = [&](int of) {
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) acc[nt][rt] = mfma16<BF>(ar[of][k][rt], xr[of][k][nt], acc[nt][rt]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const int batches = max(min(s1, N / 32) - s0, 0) / kUnroll;
+    int s = s0;
+    if (batches > 0) load(s, 0);
+    for (int i = 0; i < batches; i += 2) {
+        if (i + 1 < batches) load(s + kUnroll, 1);
+        products(0);
+        if (i + 1 < batches) {
+            if (i + 2 < batches) load(s + 2 * kUnroll, 0);
+            products(1);
+        }
+        s += 2 * kUnroll;
+    }
+    for (s = s0 + batches * kUnroll; s < s1; ++s) {  // what is left, the last columns among it
+        const bool inside = 32 * s + 8 * g < N;
+        u32x4 x1[NT], a1[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            a1[rt] = u32x4{0, 0, 0, 0};
+            if (inside) a1[rt] = *reinterpret_cast<const u32x4 *>(a[rt] + 32 * s);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            x1[nt] = u32x4{0, 0, 0, 0};
+            if (inside) x1[nt] = *reinterpret_cast<const u32x4 *>(x[nt] + 32 * s);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) acc[nt][rt] = mfma16<BF>(a1[rt], x1[nt], acc[nt][rt]);
+        }
+    }
+}
+
+// A product's row r of tile q is output 32 (q / 2) + 8 (r / 4) + 4 (q mod 2) + r mod 4 of a group of 64, so that lane (g, r16) ends up with the outputs
+// 8 g .. + 7 of each 32 of token r16.
+__device__ __forceinline__ int row_of(int r16, int q) { return 32 * (q >> 1) + 8 * (r16 >> 2) + 4 * (q & 1) + (r16 & 3); }
+
+// Y = base + unit * acc for a lane's outputs of a token.  `base` holds them already where `vector` (whole groups, 16-byte pieces); without an adapter
+// they are the base bit for bit.
+template <bool BF>
+__device__ __forceinline__ void store_rows(const LoraArgs &p, int token, int row0, int lane, bool vector, bool adapted, float unit, const u32x4 (&loaded)[2],
+                                           const f32x4 (&acc)[4])
+{
+    const uint16_t *const base = p.base + (long long)token * p.ld_base;
+    uint16_t *const y = p.Y + (long long)token * p.ldy;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int m = row0 + 32 * h + 8 * (lane >> 4);
+        if (vector) {
+            u32x4 pairs = loaded[h];
+            if (adapted) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f32x2 x = to_float2<BF>(pairs[i]);
+                    const f32x4 a = acc[2 * h + (i >> 1)];
+                    pairs[i] = from_float2<BF>(fmaf(a[2 * (i & 1)], unit, x.x), fmaf(a[2 * (i & 1) + 1], unit, x.y));
+                }
+            }
+            *reinterpret_cast<u32x4 *>(y + m) = pairs;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (m + i < p.desc.M) y[m + i] = adapted ? from_float<BF>(fmaf(acc[2 * h + (i >> 2)][i & 3], unit, to_float<BF>(base[m + i]))) : base[m + i];
+        }
+    }
+}
+
+// binary16: v's largest value is brought to 2^13 .. 2^14; its bits -> the power of two to divide by.
+__device__ __forceinline__ int power_of(uint32_t largest) { return min(max((int)(largest >> 23) - 127, -100), 100) - 13; }
+
+// Two values of v as sums of 16-bit numbers; nothing is left of an infinity or a NaN.
+template <bool BF>
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t &first, uint32_t &second, uint32_t &third)
+{
+    first = from_float2<BF>(a, b);
+    f32x2 kept = to_float2<BF>(first);
+    a = fabsf(kept.x) < INFINITY ? a - kept.x : 0.0f, b = fabsf(kept.y) < INFINITY ? b - kept.y : 0.0f;
+    second = from_float2<BF>(a, b);
+    kept = to_float2<BF>(second);
+    third = BF ? from_float2<BF>(a - kept.x, b - kept.y) : 0u;
 }
 
 // NT: tokens of a tile in sixteens.  RT: rows of A of a workgroup in sixteens.
@@ -139,55 +272,15 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_shrink_kernel(LoraParams
     const int rank = rank_of(p.a, tile.adapter), row0 = blockIdx.z * 16 * RT;
     if (tile.count == 0 || row0 >= rank) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
-    const int N = p.a.desc.N, width = p.a.desc.max_rank;
+    const int width = p.a.desc.max_rank;
     // steps of 32 columns, cut into slices and those among the waves
-    const int steps = (N + 31) / 32, pieces = p.slices * kWaves, piece = blockIdx.y * kWaves + wave;
+    const int steps = (p.a.desc.N + 31) / 32, pieces = p.slices * kWaves, piece = blockIdx.y * kWaves + wave;
     const int s0 = (int)((long long)steps * piece / pieces), s1 = (int)((long long)steps * (piece + 1) / pieces);
-    const uint16_t *x[NT], *a[RT];
+    int tokens[NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) x[nt] = p.a.X + (long long)members[16 * nt + r16] * p.a.ldx + 8 * g;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) a[rt] = p.a.A + ((long long)tile.adapter * width + min(row0 + 16 * rt + r16, rank - 1)) * N + 8 * g;
+    for (int nt = 0; nt < NT; ++nt) tokens[nt] = members[16 * nt + r16];
     f32x4 acc[NT][RT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[nt][rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const auto products = [&](const u32x4 (&xr)[NT], const u32x4 (&ar)[RT]) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) acc[nt][rt] = mfma16<BF>(ar[rt], xr[nt], acc[nt][rt]);
-    };
-    constexpr int kUnroll = NT * RT >= 8 ? 2 : 4;  // steps whose loads are under way together
-    int s = s0;
-    for (; s + kUnroll <= min(s1, N / 32); s += kUnroll) {
-        u32x4 xr[kUnroll][NT], ar[kUnroll][RT];
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) {
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) ar[k][rt] = *reinterpret_cast<const u32x4 *>(a[rt] + 32 * (s + k));
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) xr[k][nt] = *reinterpret_cast<const u32x4 *>(x[nt] + 32 * (s + k));
-        }
-#pragma unroll
-        for (int k = 0; k < kUnroll; ++k) products(xr[k], ar[k]);
-    }
-    for (; s < s1; ++s) {  // what is left, the last columns among it
-        const bool inside = 32 * s + 8 * g < N;
-        u32x4 xr[NT], ar[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            ar[rt] = u32x4{0, 0, 0, 0};
-            if (inside) ar[rt] = *reinterpret_cast<const u32x4 *>(a[rt] + 32 * s);
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            xr[nt] = u32x4{0, 0, 0, 0};
-            if (inside) xr[nt] = *reinterpret_cast<const u32x4 *>(x[nt] + 32 * s);
-        }
-        products(xr, ar);
-    }
+    shrink_products<BF, NT, RT>(p.a, tile.adapter, tokens, row0, rank, s0, s1, lane, acc);
     // lane (g, r16) has of token r16 the rows 4 g .. 4 g + 3
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -204,52 +297,21 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_shrink_kernel(LoraParams
     }
 }
 
-// v of a tile as matrix operands in LDS: [part][step of 16][tokens in sixteens][lane] 16 bytes; part 1 (bfloat16 only) the third numbers.
-constexpr size_t expand_lds_bytes(bool bf, int tiles, int steps) { return (size_t)(bf ? 2 : 1) * steps * tiles * 1024; }
+// v of sixteen tokens as matrix operands: [part][step of 16][lane] 16 bytes; part 1 (bfloat16 only) the third numbers.
+constexpr size_t operand_bytes(bool bf, int steps) { return (size_t)(bf ? 2 : 1) * steps * 1024; }
 
-template <bool BF, int NT, bool FEW>
-__global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams p)
+// Adds up the slices of v of sixteen tokens and turns it into operands.  binary16: largest[] (zeros before) becomes each token's largest value's bits, of
+// which power_of() is what it was divided by.  For all of a workgroup's threads.
+template <bool BF>
+__device__ __forceinline__ void make_operands(const LoraParams &p, int adapter, int rank, const int *members, uint32_t *largest, u32x4 *operands)
 {
-    constexpr int kTokens = 16 * NT, kItems = NT == 1 ? 2 : 4;  // eights of v that a thread prepares
-    extern __shared__ __attribute__((aligned(16))) u32x4 operand[];
-    __shared__ int members[kTokens];
-    __shared__ uint32_t largest[kTokens];
-    if (threadIdx.x < kTokens) largest[threadIdx.x] = 0;
-    const Tile tile = find_tile<kTokens, FEW>(p, blockIdx.x, members);
-    if (tile.count == 0) return;
-    const int rank = rank_of(p.a, tile.adapter), steps = (rank + 15) / 16;
-    if (steps == 0 && !p.copy) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
-    const int M = p.a.desc.M, width = p.a.desc.max_rank, third = steps * NT * 64;
-    const float scale = tile.adapter >= 0 && p.a.scale ? p.a.scale[tile.adapter] : 1.0f;
-
-    // ---- rows: lane (g, r16) ends up with outputs 8 g .. + 7 of each 32 of token r16: row r of tile q is output 32 (q / 2) + 8 (r / 4) + 4 (q mod 2) + r mod 4.
-    // What a group of 64 rows needs first, base and the first columns of B, is requested before v is made, and for the next group before this one's stores ----
-    const auto first_row = [&](int group) { return (int)((group * gridDim.y + blockIdx.y) * kWaves + wave) * 64; };  // (the workgroups' rows of one moment are neighbours)
-    const int widest = width > 8 ? 8 * (g & 1) : 0;  // (a row of B may have eight columns only; what is loaded twice is masked)
-    u32x4 out[NT][2], head[4];
-    const uint16_t *b[4];
-    const auto request = [&](int row0) {
-        if (row0 >= M) return;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            b[q] = p.a.B + ((long long)max(tile.adapter, 0) * M + min(row0 + 32 * (q >> 1) + 8 * (r16 >> 2) + 4 * (q & 1) + (r16 & 3), M - 1)) * width;
-            if (steps) head[q] = *reinterpret_cast<const u32x4 *>(b[q] + widest);
-        }
-        if (p.wide && row0 + 64 <= M) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    out[nt][h] = *reinterpret_cast<const u32x4 *>(p.a.base + (long long)members[16 * nt + r16] * p.a.ld_base + row0 + 32 * h + 8 * g);
-        }
-    };
-    // ---- v ----
+    constexpr int kItems = 16 * BCQ_MAX_RANK / 8 / (64 * kWaves);  // eights of v of a thread
+    const int steps = (rank + 15) / 16, width = p.a.desc.max_rank;
+    const float scale = p.a.scale && adapter >= 0 ? p.a.scale[adapter] : 1.0f;
     float v[kItems][8];
-    request(first_row(0));
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-        const int item = threadIdx.x + k * 64 * kWaves, token = item % kTokens, j = item / kTokens * 8;
+        const int item = threadIdx.x + k * 64 * kWaves, token = item % 16, j = item / 16 * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[k][i] = 0.0f;
         if (j >= rank) continue;
@@ -268,32 +330,59 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
         }
         if (!BF) atomicMax(&largest[token], __builtin_bit_cast(uint32_t, most));
     }
-    // binary16: the token's largest value is brought to 2^13 .. 2^14
-    const auto exponent = [&](int token) { return min(max((int)(largest[token] >> 23) - 127, -100), 100) - 13; };
     if (!BF) __syncthreads();
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-        const int item = threadIdx.x + k * 64 * kWaves, token = item % kTokens, eight = item / kTokens;
+        const int item = threadIdx.x + k * 64 * kWaves, token = item % 16, eight = item / 16;
         if (eight >= 2 * steps) continue;
+        const int power = BF ? 0 : power_of(largest[token]);
         u32x4 first, second, rest;
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            float a = v[k][i], b = v[k][i + 1];
-            if (!BF) a = ldexpf(a, -exponent(token)), b = ldexpf(b, -exponent(token));
-            uint32_t pair = from_float2<BF>(a, b);
-            first[i / 2] = pair;
-            f32x2 kept = to_float2<BF>(pair);
-            a = fabsf(kept.x) < INFINITY ? a - kept.x : 0.0f, b = fabsf(kept.y) < INFINITY ? b - kept.y : 0.0f;
-            second[i / 2] = pair = from_float2<BF>(a, b);
-            if (BF) {
-                kept = to_float2<BF>(pair);
-                rest[i / 2] = from_float2<BF>(a - kept.x, b - kept.y);
-            }
+            uint32_t x, y, z;
+            split_pair<BF>(BF ? v[k][i] : ldexpf(v[k][i], -power), BF ? v[k][i + 1] : ldexpf(v[k][i + 1], -power), x, y, z);
+            first[i / 2] = x, second[i / 2] = y, rest[i / 2] = z;
         }
-        u32x4 *const at = operand + ((eight >> 1) * NT + (token >> 4)) * 64 + (token & 15) + 16 * (eight & 1);
+        u32x4 *const at = operands + (eight >> 1) * 64 + token + 16 * (eight & 1);
         at[0] = first, at[32] = second;
-        if (BF) at[third] = rest, at[third + 32] = u32x4{0, 0, 0, 0};
+        if (BF) at[64 * steps] = rest, at[64 * steps + 32] = u32x4{0, 0, 0, 0};
     }
+}
+
+template <bool BF, bool FEW>
+__global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams p)
+{
+    constexpr int kTokens = 16;
+    extern __shared__ __attribute__((aligned(16))) u32x4 operand[];
+    __shared__ int members[kTokens];
+    __shared__ uint32_t largest[kTokens];
+    if (threadIdx.x < kTokens) largest[threadIdx.x] = 0;
+    const Tile tile = find_tile<kTokens, FEW>(p, blockIdx.x, members);
+    if (tile.count == 0) return;
+    const int rank = rank_of(p.a, tile.adapter), steps = (rank + 15) / 16;
+    if (steps == 0 && !p.copy) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+    const int M = p.a.desc.M, width = p.a.desc.max_rank, third = steps * 64;
+    // What a group of 64 rows needs first, base and the first columns of B, is requested before v is made, and for the next group before this one's stores.
+    const auto first_row = [&](int group) { return (int)((group * gridDim.y + blockIdx.y) * kWaves + wave) * 64; };  // (the workgroups' rows of one moment are neighbours)
+    const int widest = width > 8 ? 8 * (g & 1) : 0;  // (a row of B may have eight columns only; what is loaded twice is masked)
+    u32x4 out[2], head[4];
+    const uint16_t *b[4];
+    const auto request = [&](int row0) {
+        if (row0 >= M) return;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            b[q] = p.a.B + ((long long)max(tile.adapter, 0) * M + min(row0 + row_of(r16, q), M - 1)) * width;
+            if (steps) head[q] = *reinterpret_cast<const u32x4 *>(b[q] + widest);
+        }
+        if (p.wide && row0 + 64 <= M) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                out[h] = *reinterpret_cast<const u32x4 *>(p.a.base + (long long)members[r16] * p.a.ld_base + row0 + 32 * h + 8 * g);
+        }
+    };
+    request(first_row(0));
+    make_operands<BF>(p, tile.adapter, rank, members, largest, operand);
     __syncthreads();
 
     u32x4 kept_last;  // of the last step: the columns that belong to the adapter
@@ -306,11 +395,9 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
         const int row0 = first_row(group);
         if (row0 >= M) break;
         const bool vector = p.wide && row0 + 64 <= M;
-        f32x4 acc[NT][4];
+        f32x4 acc[4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[nt][q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int q = 0; q < 4; ++q) acc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         u32x4 ahead[4];
         for (int s = 0; s < steps; ++s) {
             u32x4 rows[4];
@@ -325,112 +412,232 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
 #pragma unroll
                 for (int q = 0; q < 4; ++q) rows[q] &= kept_last;
             }
+            const u32x4 o = operand[s * 64 + lane];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const u32x4 o = operand[(s * NT + nt) * 64 + lane];
+            for (int q = 0; q < 4; ++q) acc[q] = mfma16<BF>(rows[q], o, acc[q]);
+            if (BF) {
+                const u32x4 o3 = operand[third + s * 64 + lane];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) acc[nt][q] = mfma16<BF>(rows[q], o, acc[nt][q]);
-                if (BF) {
-                    const u32x4 o3 = operand[third + (s * NT + nt) * 64 + lane];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[nt][q] = mfma16<BF>(rows[q], o3, acc[nt][q]);
-                }
+                for (int q = 0; q < 4; ++q) acc[q] = mfma16<BF>(rows[q], o3, acc[q]);
             }
         }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int token = 16 * nt + r16;
-            if (token >= tile.count) continue;
-            const float unit = BF || steps == 0 ? 1.0f : ldexpf(1.0f, exponent(token));
-            const uint16_t *const base = p.a.base + (long long)members[token] * p.a.ld_base;
-            uint16_t *const y = p.a.Y + (long long)members[token] * p.a.ldy;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int m = row0 + 32 * h + 8 * g;
-                if (vector) {
-                    u32x4 pairs = out[nt][h];
-                    if (steps) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const f32x2 x = to_float2<BF>(pairs[i]);
-                            const f32x4 a = acc[nt][2 * h + (i >> 1)];
-                            pairs[i] = from_float2<BF>(fmaf(a[2 * (i & 1)], unit, x.x), fmaf(a[2 * (i & 1) + 1], unit, x.y));
-                        }
-                    }
-                    *reinterpret_cast<u32x4 *>(y + m) = pairs;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (m + i < M) y[m + i] = steps ? from_float<BF>(fmaf(acc[nt][2 * h + (i >> 2)][i & 3], unit, to_float<BF>(base[m + i]))) : base[m + i];
-                }
-            }
+        if (r16 < tile.count) {
+            const float unit = BF || steps == 0 ? 1.0f : ldexpf(1.0f, power_of(largest[r16]));
+            store_rows<BF>(p.a, members[r16], row0, lane, vector, steps != 0, unit, out, acc);
         }
         if (group + 1 < p.row_groups) request(first_row(group + 1));
+    }
+}
+
+// ---- many tokens: v is turned into operands once, and waves that share nothing but the caches go by the rows of B ----
+
+template <bool BF>
+__global__ __launch_bounds__(64 * kWaves) void bcq_lora_pack_kernel(LoraParams p)
+{
+    __shared__ int members[kManyTokens];
+    __shared__ uint32_t largest[16];
+    if (threadIdx.x < 16) largest[threadIdx.x] = 0;
+    const Tile tile = find_tile<kManyTokens, false>(p, blockIdx.x, members);
+    const int rank = rank_of(p.a, tile.adapter), sixteen = blockIdx.y;
+    if (rank == 0 || 16 * sixteen >= tile.count) return;
+    make_operands<BF>(p, tile.adapter, rank, members + 16 * sixteen, largest, p.operands + (size_t)(blockIdx.x * (kManyTokens / 16) + sixteen) * p.operand_pieces);
+    if (!BF) {
+        __syncthreads();
+        if (threadIdx.x < 16) p.units[blockIdx.x * kManyTokens + 16 * sixteen + threadIdx.x] = ldexpf(1.0f, power_of(largest[threadIdx.x]));
+    }
+}
+
+// A workgroup has a tile, 16 tokens a wave, whose operands stay in registers, and walks row_groups groups of 64 rows of B.  These come through LDS (two buffers, a
+// row 16 bytes longer than it is, so that 16 rows' pieces of one column meet 16 different banks): read in the operand's layout from memory, sixteen rows' 32 bytes each, a
+// load costs four times a contiguous one, and there would be four times as many.  Rows of the next group and base of the next two are on
+// their way during this one.
+// ST: steps that the operands have at most.
+template <bool BF, int ST>
+__global__ __launch_bounds__(64 * kWaves, ST == 8 ? 2 : 3) void bcq_lora_many_kernel(LoraParams p)
+{
+    constexpr int kParts = BF ? 2 : 1, kOwn = (64 * 2 * ST + 64 * kWaves - 1) / (64 * kWaves);  // 16-byte pieces of a group's rows that a thread brings
+    __shared__ u32x4 rows_lds[2][64 * (2 * ST + 1)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+    const int slot = blockIdx.y, M = p.a.desc.M, width = p.a.desc.max_rank;
+    if (slot >= p.tiles[0]) return;
+    const int adapter = p.tiles[2 + 2 * slot], count = p.tiles[3 + 2 * slot] - 16 * wave;
+    const int rank = rank_of(p.a, adapter), steps = (rank + 15) / 16;
+    if (steps == 0 && !p.copy) return;
+    const int token = p.order[slot * kManyTokens + (r16 < count ? 16 * wave + r16 : 0)];
+    const float unit = BF ? 1.0f : p.units[slot * kManyTokens + 16 * wave + r16];
+    u32x4 v[kParts][ST];
+    const u32x4 *const operands = p.operands + (size_t)(slot * (kManyTokens / 16) + wave) * p.operand_pieces;
+#pragma unroll
+    for (int part = 0; part < kParts; ++part)
+#pragma unroll
+        for (int s = 0; s < ST; ++s)
+            if (s < steps) v[part][s] = operands[(part * steps + s) * 64 + lane];
+    u32x4 kept_last;  // of the last step: the columns that belong to the adapter
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = 16 * (steps - 1) + 8 * (g & 1) + 2 * i;
+        kept_last[i] = (j < rank ? 0xffffu : 0u) | (j + 1 < rank ? 0xffff0000u : 0u);
+    }
+    // pieces of a row, and which of a group's this thread brings
+    const int pieces = width >> 3;
+    int from_row[kOwn], from_piece[kOwn];
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+        const int n = threadIdx.x + i * 64 * kWaves;
+        from_row[i] = n / pieces;
+        from_piece[i] = n - from_row[i] * pieces;
+    }
+    const uint16_t *const b = p.a.B + (long long)max(adapter, 0) * M * width;
+    u32x4 own[kOwn], base[2], next_base[2], later_base[2];  // base two groups ahead: a load takes longer than a group
+    const auto first_row = [&](int group) { return (int)(group * gridDim.x + blockIdx.x) * 64; };
+    const auto fetch = [&](int row0) {
+        if (steps == 0) return;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+            if (from_row[i] < 64) own[i] = *reinterpret_cast<const u32x4 *>(b + (long long)min(row0 + from_row[i], M - 1) * width + 8 * from_piece[i]);
+    };
+    const auto put = [&](u32x4 *to) {
+        if (steps == 0) return;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i)
+            if (from_row[i] < 64) to[from_row[i] * (pieces + 1) + from_piece[i]] = own[i];
+    };
+    const auto request = [&](int row0, u32x4 (&to)[2]) {
+        if (!p.wide || row0 + 64 > M) return;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) to[h] = *reinterpret_cast<const u32x4 *>(p.a.base + (long long)token * p.a.ld_base + row0 + 32 * h + 8 * g);
+    };
+    int groups = p.row_groups;  // those that exist
+    while (groups > 0 && first_row(groups - 1) >= M) --groups;
+    if (groups == 0) return;
+    fetch(first_row(0));
+    request(first_row(0), base);
+    if (groups > 1) request(first_row(1), next_base);
+    put(rows_lds[0]);
+    if (groups > 1) fetch(first_row(1));
+    __syncthreads();
+    for (int group = 0; group < groups; ++group) {
+        const int row0 = first_row(group);
+        if (group + 2 < groups) request(first_row(group + 2), later_base);
+        f32x4 acc[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (count > 0) {
+            const u32x4 *const at = rows_lds[group & 1];
+#pragma unroll
+            for (int s = 0; s < ST; ++s) {
+                if (s >= steps) break;
+                const int piece = min(2 * s + (g & 1), pieces - 1);  // (a row may end in the first eight of a sixteen: the second are masked)
+                u32x4 rows[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    rows[q] = at[row_of(r16, q) * (pieces + 1) + piece];
+                    if (s == steps - 1) rows[q] &= kept_last;
+                }
+#pragma unroll
+                for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[q] = mfma16<BF>(rows[q], v[part][s], acc[q]);
+            }
+        }
+        if (group + 1 < groups) put(rows_lds[(group + 1) & 1]);
+        if (group + 2 < groups) fetch(first_row(group + 2));
+        if (r16 < count) store_rows<BF>(p.a, token, row0, lane, p.wide && row0 + 64 <= M, steps != 0, unit, base, acc);
+        base[0] = next_base[0], base[1] = next_base[1];
+        next_base[0] = later_base[0], next_base[1] = later_base[1];
+        // (LDS alone: the stores need not have arrived)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     }
 }
 
 namespace {
 
 struct LoraPlan {
-    int tiles;          // tokens of a tile in sixteens
+    bool few, many;     // at most kFewTokens; many tokens of few adapters
     int slots;          // most tiles there can be
     int row_tiles, row_blocks;  // shrink: rows of A of a workgroup in sixteens, and how many such blocks
     int slices, row_groups;
-    bool few;
-    size_t part_bytes, order_bytes, tile_bytes, cursor_bytes;
+    size_t part_bytes, order_bytes, tile_bytes, cursor_bytes, operand_bytes, unit_bytes;
 };
 
 size_t whole(size_t bytes) { return (bytes + 15) & ~(size_t)15; }
+
+int steps_up_to(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ? 4 : 8; }
 
 LoraPlan lora_plan(const bcq_adapters &d, int tokens)
 {
     LoraPlan s;
     s.few = tokens <= kFewTokens;
-    // 64 tokens a tile where adapters have 32 or more on average (and their operands leave LDS for three workgroups)
-    const int steps = (d.max_rank + 15) / 16;
-    s.tiles = !s.few && d.max_rank <= 128 && expand_lds_bytes(d.dtype == BCQ_BF16, 4, steps) <= 48 * 1024 && tokens >= 32LL * d.count ? 4 : 1;
     const int most = tokens < d.count + 1 ? tokens : d.count + 1;
-    s.slots = s.few ? tokens : tokens / (16 * s.tiles) + most;
+    // Operands made in a launch of their own pay from about 1024 tokens of rank 64 on, if adapters have 16 tokens and more (4 adapters, 8192 to 10240, bfloat16; each
+    // workgroup for itself / once: 512 tokens of rank 64 39.0 / 36.3 us, 1024 52.6 / 42.8, 2048 98.8 / 59.8; 8 adapters of rank 16: 1024 29.2 / 31.3, 2048 47.9 / 50.0).
+    s.many = (long long)tokens * d.max_rank >= 64 * 1024 && d.max_rank <= 128 && tokens >= 16LL * d.count &&
+             tokens / kManyTokens + most <= 65535;  // (a grid's second number)
+    s.slots = s.few ? tokens : tokens / (s.many ? kManyTokens : 16) + most;
     s.row_tiles = d.max_rank <= 16 ? 1 : d.max_rank <= 32 ? 2 : 4;
     s.row_blocks = (d.max_rank + 16 * s.row_tiles - 1) / (16 * s.row_tiles);
     const int likely = s.few ? (tokens < d.count ? tokens : d.count) : s.slots;  // tiles, if adapters are spread
+    // (one token, rank 64, 28672 to 7168: 16 slices 17 us, 8 23, 4 38)
     const int wanted = 2 * compute_units() / (likely * s.row_blocks), longest = (d.N + 511) / 512;
     s.slices = wanted < longest ? wanted : longest;
-    // (with 64 tokens a tile there is work enough, and every workgroup of the second launch reads all slices: 4 slices 124 us, 13 134, 2 140 for 2048 tokens,
-    // rank 64, 7168 to 28672; one token, rank 64, 28672 to 7168: 16 slices 17 us, 8 23, 4 38)
-    const int cap = s.tiles == 4 ? 4 : 16;
-    s.slices = s.slices < 1 ? 1 : s.slices > cap ? cap : s.slices;
+    s.slices = s.slices < 1 ? 1 : s.slices > 16 ? 16 : s.slices;
+    // as many workgroups as the chip holds at once, four to a compute unit, so that each makes v once
     const int blocks = (d.M + 64 * kWaves - 1) / (64 * kWaves);
-    // as many workgroups as the chip holds at once (registers: two to a compute unit with 64 tokens, four with 16), so that each makes v once
-    const long long resident = (s.tiles == 4 ? 2 : 4) * compute_units(), groups = ((long long)blocks * (s.few ? likely : tokens / (16 * s.tiles) + 1) + resident - 1) / resident;
+    const long long resident = 4 * compute_units(), groups = ((long long)blocks * likely + resident - 1) / resident;
     s.row_groups = (int)(groups < 1 ? 1 : groups > 16 ? 16 : groups);
+    const bool bf = d.dtype == BCQ_BF16;
     s.part_bytes = whole((size_t)s.slices * tokens * d.max_rank * sizeof(float));
-    s.order_bytes = s.few ? 0 : whole((size_t)tokens * sizeof(int));
-    s.tile_bytes = s.few ? 0 : whole((size_t)(1 + 3 * s.slots) * sizeof(int));
+    s.order_bytes = s.few ? 0 : whole((size_t)s.slots * (s.many ? kManyTokens : 16) * sizeof(int));
+    s.tile_bytes = s.few ? 0 : whole((size_t)(2 + 2 * s.slots) * sizeof(int));
     s.cursor_bytes = s.few || d.count + 1 <= kPlanGroups ? 0 : whole((size_t)(d.count + 1) * sizeof(int));
+    s.operand_bytes = s.many ? (size_t)s.slots * (kManyTokens / 16) * operand_bytes(bf, (d.max_rank + 15) / 16) : 0;
+    s.unit_bytes = s.many ? whole((size_t)s.slots * kManyTokens * sizeof(float)) : 0;
     return s;
 }
 
 template <bool BF, int NT, bool FEW>
-hipError_t launch(const LoraParams &p, const LoraPlan &s, hipStream_t stream)
+void launch_shrink(const LoraParams &p, const LoraPlan &s, hipStream_t stream)
 {
     const dim3 shrink(s.slots, s.slices, s.row_blocks);
     if (s.row_tiles == 1) bcq_lora_shrink_kernel<BF, NT, 1, FEW><<<shrink, 64 * kWaves, 0, stream>>>(p);
     else if (s.row_tiles == 2) bcq_lora_shrink_kernel<BF, NT, 2, FEW><<<shrink, 64 * kWaves, 0, stream>>>(p);
     else bcq_lora_shrink_kernel<BF, NT, 4, FEW><<<shrink, 64 * kWaves, 0, stream>>>(p);
+}
+
+template <bool BF, bool FEW>
+void launch(const LoraParams &p, const LoraPlan &s, hipStream_t stream)
+{
+    launch_shrink<BF, 1, FEW>(p, s, stream);
     const int rows = 64 * kWaves * s.row_groups;
     const dim3 expand(s.slots, (p.a.desc.M + rows - 1) / rows);
-    const size_t lds = expand_lds_bytes(BF, NT, (p.a.desc.max_rank + 15) / 16);
-    bcq_lora_expand_kernel<BF, NT, FEW><<<expand, 64 * kWaves, lds, stream>>>(p);
-    return hipGetLastError();
+    bcq_lora_expand_kernel<BF, FEW><<<expand, 64 * kWaves, operand_bytes(BF, (p.a.desc.max_rank + 15) / 16), stream>>>(p);
 }
 
 template <bool BF>
-hipError_t by_plan(const LoraParams &p, const LoraPlan &s, hipStream_t stream)
+void launch_many(LoraParams p, const LoraPlan &s, hipStream_t stream)
 {
-    if (s.few) return launch<BF, 1, true>(p, s, stream);
-    bcq_lora_plan_kernel<<<1, 1024, 0, stream>>>(p, 16 * s.tiles);
-    return s.tiles == 4 ? launch<BF, 4, false>(p, s, stream) : launch<BF, 1, false>(p, s, stream);
+    launch_shrink<BF, kManyTokens / 16, false>(p, s, stream);
+    p.operand_pieces = (int)(operand_bytes(BF, (p.a.desc.max_rank + 15) / 16) / 16);
+    bcq_lora_pack_kernel<BF><<<dim3(s.slots, kManyTokens / 16), 64 * kWaves, 0, stream>>>(p);
+    const int blocks = (p.a.desc.M + 63) / 64;
+    p.row_groups = blocks >= 64 ? 8 : 1 + blocks / 16;
+    const dim3 grid((blocks + p.row_groups - 1) / p.row_groups, s.slots);
+    switch (steps_up_to(p.a.desc.max_rank)) {
+        case 1: bcq_lora_many_kernel<BF, 1><<<grid, 64 * kWaves, 0, stream>>>(p); break;
+        case 2: bcq_lora_many_kernel<BF, 2><<<grid, 64 * kWaves, 0, stream>>>(p); break;
+        case 4: bcq_lora_many_kernel<BF, 4><<<grid, 64 * kWaves, 0, stream>>>(p); break;
+        default: bcq_lora_many_kernel<BF, 8><<<grid, 64 * kWaves, 0, stream>>>(p);
+    }
+}
+
+template <bool BF>
+void by_plan(const LoraParams &p, const LoraPlan &s, hipStream_t stream)
+{
+    if (s.few) return launch<BF, true>(p, s, stream);
+    bcq_lora_plan_kernel<<<1, 1024, 0, stream>>>(p, s.many ? kManyTokens : 16);
+    s.many ? launch_many<BF>(p, s, stream) : launch<BF, false>(p, s, stream);
 }
 
 }  // namespace
@@ -438,7 +645,7 @@ hipError_t by_plan(const LoraParams &p, const LoraPlan &s, hipStream_t stream)
 size_t lora_workspace_bytes(const bcq_adapters &d, int tokens)
 {
     const LoraPlan s = lora_plan(d, tokens);
-    return s.part_bytes + s.order_bytes + s.tile_bytes + s.cursor_bytes;
+    return s.part_bytes + s.order_bytes + s.tile_bytes + s.cursor_bytes + s.operand_bytes + s.unit_bytes;
 }
 
 hipError_t launch_lora(const LoraArgs &a, hipStream_t stream)
@@ -447,15 +654,24 @@ hipError_t launch_lora(const LoraArgs &a, hipStream_t stream)
     LoraParams p;
     p.a = a;
     char *at = static_cast<char *>(a.workspace);
-    p.part = reinterpret_cast<float *>(at);
-    p.order = reinterpret_cast<int *>(at += s.part_bytes);
-    p.tiles = reinterpret_cast<int *>(at += s.order_bytes);
-    p.cursor = reinterpret_cast<int *>(at + s.tile_bytes);
+    const auto take = [&](size_t bytes) {
+        char *const here = at;
+        at += bytes;
+        return here;
+    };
+    p.part = reinterpret_cast<float *>(take(s.part_bytes));
+    p.order = reinterpret_cast<int *>(take(s.order_bytes));
+    p.tiles = reinterpret_cast<int *>(take(s.tile_bytes));
+    p.cursor = reinterpret_cast<int *>(take(s.cursor_bytes));
+    p.operands = reinterpret_cast<u32x4 *>(take(s.operand_bytes));
+    p.units = reinterpret_cast<float *>(take(s.unit_bytes));
     p.slices = s.slices;
     p.row_groups = s.row_groups;
     p.copy = a.Y != a.base;
     p.wide = a.ld_base % 8 == 0 && a.ldy % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.base) | reinterpret_cast<uintptr_t>(a.Y)) & 15) == 0;
-    return a.desc.dtype == BCQ_BF16 ? by_plan<true>(p, s, stream) : by_plan<false>(p, s, stream);
+    if (a.desc.dtype == BCQ_BF16) by_plan<true>(p, s, stream);
+    else by_plan<false>(p, s, stream);
+    return hipGetLastError();
 }
 
 }  // namespace bcq

@@ -357,6 +357,30 @@ def test_lora(dtype, T, N, M, C, width):
         assert_close(got, ref, bound, f"ranks {ranks}")
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,N,M,C,width", [(1100, 264, 333, 3, 64), (520, 136, 1025, 5, 128), (4200, 72, 130, 2, 16), (2200, 520, 192, 30, 32), (1400, 1032, 64, 1, 56),
+                                           (1030, 96, 640, 4, 72)])
+def test_lora_many_tokens(dtype, T, N, M, C, width):
+    """Enough tokens of an adapter that v is turned into operands in a launch of its own; sorted by adapter, in runs, and mixed."""
+    for ranks, runs in ((None, True), ([width, 1, width - 3, 0, 9], False)):
+        X, A, Bm, scale, rank, adapter, base = _lora_case(T, N, M, C, width, dtype, seed=T, ranks=ranks)
+        if runs:
+            adapter = adapter.sort().values.contiguous()
+        got = bcq.Adapters(A, Bm, scale, rank).add(X, adapter, base)
+        ref, bound = lora_ref(X, A, Bm, scale, rank, adapter, base)
+        assert_close(got, ref, bound, f"ranks {ranks}")
+        assert bcq.Adapters(A, Bm, scale, rank).add(X, adapter, base, out=base) is base
+        assert torch.equal(base, got)
+
+
+def test_lora_very_many_adapters():
+    """More adapters than the sorting launch counts in LDS."""
+    X, A, Bm, scale, rank, adapter, base = _lora_case(900, 64, 40, 5000, 8, "f16", bare=True)
+    got = bcq.Adapters(A, Bm, scale).add(X, adapter, base)
+    ref, bound = lora_ref(X, A, Bm, scale, None, adapter, base)
+    assert_close(got, ref, bound)
+
+
 @pytest.mark.parametrize("T", [5, 150])
 def test_lora_in_place_with_strides_and_defaults(T):
     X, A, Bm, _, _, adapter, base = _lora_case(T, 256, 200, 3, 16, "f16", strides=(24, 7))
@@ -384,7 +408,7 @@ def test_lora_ids_outside_the_range_leave_the_base():
     assert bcq.Adapters(A, Bm, scale).add(X[:0], adapter[:0], base[:0]).shape == (0, 96)
 
 
-@pytest.mark.parametrize("T", [4, 200])
+@pytest.mark.parametrize("T", [4, 200, 4200])
 def test_lora_wide_ranges_of_activations(T):
     """A x beyond binary16, and tokens whose A x differ by 2^20 beside each other."""
     X, A, Bm, scale, rank, adapter, base = _lora_case(T, 512, 96, 2, 16, "f16", bare=False)
@@ -397,7 +421,7 @@ def test_lora_wide_ranges_of_activations(T):
     assert_close(got, ref, bound)
 
 
-@pytest.mark.parametrize("T,M", [(6, 512), (200, 1024)])
+@pytest.mark.parametrize("T,M", [(6, 512), (200, 1024), (2100, 320)])
 def test_lora_repeats_bit_for_bit_on_any_stream_and_in_graphs(T, M):
     X, A, Bm, scale, rank, adapter, base = _lora_case(T, 2048, M, 4, 32, "f16", ranks=[32, 7])
     ad = bcq.Adapters(A, Bm, scale, rank)
