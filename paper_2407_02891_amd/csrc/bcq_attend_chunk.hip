@@ -85,45 +85,52 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
     const int b0 = block0 + (int)((long long)blocks * part / p.parts), b1 = block0 + (int)((long long)blocks * (part + 1) / p.parts);
 
     // ---- K and V of a block to LDS ----
+    // A wave brings KB / 4 neighbouring keys, which lie in one page of 16 slots or more.
     const int piece = lane % kPieces, in_rows = lane / kPieces;
     const uint16_t *const k_head = p.k + head * p.head_stride, *const v_head = p.v + head * p.head_stride;
     const int last = max(q.len - 1, 0);
-    int id[kTransfers];
-    const auto key_of = [&](int key0, int i) { return key0 + (i * kWaves + wave) * kRows; };   // first key of a transfer; all in one sixteen
+    constexpr int kOwn = KB / kWaves;
+    int id[ANY ? kTransfers : 1];
     const auto find_pages = [&](int key0) {
+        if (ANY) {
 #pragma unroll
-        for (int i = 0; i < kTransfers; ++i) id[i] = page_of(p, r, min(key_of(key0, i) + (ANY ? in_rows : 0), last));
+            for (int i = 0; i < kTransfers; ++i) id[i] = page_of(p, r, min(key0 + kOwn * wave + i * kRows + in_rows, last));
+        } else {
+            id[0] = page_of(p, r, min(key0 + kOwn * wave, last));
+        }
     };
+    // the 16-element unit of a row of V that unit 0 is exchanged with: four keys' pairs of units, which are read together, fill all banks
+    const auto v_turn = [](int key) { return DT == 64 ? (key & 2) | (key >> 2 & 1) : (key & 3) << 1 | (key >> 2 & 1); };
+    const auto k_turn = [](int key) { return key & (DT == 64 ? 7 : 15); };
+    const int row_off = in_rows * p.slot_stride;
     const auto request = [&](int key0, uint16_t *to_k, uint16_t *to_v) {
         int dim = p.head_dim;
         if (ANY) asm volatile("" : "+v"(dim));  // (compared here, not held as masks through the loop)
+        const int first = min(key0 + kOwn * wave, last & -kOwn);         // keys behind the last are the last's copies, and masked
+        const long long base = ANY ? 0 : __builtin_amdgcn_readfirstlane(id[0]) * p.page_stride + (long long)((first & ((1 << p.page_shift) - 1)) * p.slot_stride);
+        const int most = (last - first) * p.slot_stride;
 #pragma unroll
         for (int i = 0; i < kTransfers; ++i) {
-            const int in_lds = (i * kWaves + wave) * kRows + in_rows;
-            const int k_d = 8 * (piece ^ (in_lds & (DT == 64 ? 7 : 15)));
-            const int v_d = 8 * (((piece >> 1 ^ (in_lds & (DT == 64 ? 3 : 7))) << 1) + (piece & 1));
+            const int in_lds = kOwn * wave + i * kRows + in_rows;
+            const int k_d = 8 * (piece ^ k_turn(in_lds)), v_d = 8 * (piece ^ v_turn(in_lds) << 1);
             const uint16_t *k, *v;
             if (ANY) {
-                const int key = min(key_of(key0, i) + in_rows, last);     // keys behind the last are the last's copies, and masked
+                const int key = min(key0 + in_lds, last);
                 const long long at = id[i] * p.page_stride + (long long)((key & ((1 << p.page_shift) - 1)) * p.slot_stride);
                 k = k_d < dim ? k_head + at + k_d : g_zeros;
                 v = v_d < dim ? v_head + at + v_d : g_zeros;
             } else {
-                const int tile = min(key_of(key0, i), last) & ~15;
-                const long long base = __builtin_amdgcn_readfirstlane(id[i]) * p.page_stride + (long long)((tile & ((1 << p.page_shift) - 1)) * p.slot_stride);
-                const unsigned row = (unsigned)((min(key_of(key0, i) + in_rows, last) - tile) * p.slot_stride);
+                const unsigned row = (unsigned)min(row_off + i * kRows * p.slot_stride, most);
                 k = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(k_head + base) + 2u * (row + k_d));
                 v = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(v_head + base) + 2u * (row + v_d));
             }
-            load_to_lds(k, to_k + (i * kWaves + wave) * kRows * DT);
-            load_to_lds(v, to_v + (i * kWaves + wave) * kRows * DT);
+            load_to_lds(k, to_k + (kOwn * wave + i * kRows) * DT);
+            load_to_lds(v, to_v + (kOwn * wave + i * kRows) * DT);
         }
     };
     // element d of key j
-    const auto k_at = [&](const uint16_t *buffer, int key, int d) { return buffer + key * DT + ((d >> 3 ^ (key & (DT == 64 ? 7 : 15))) << 3); };
-    const auto v_at = [&](const uint16_t *buffer, int key, int d) {
-        return buffer + key * DT + ((d >> 4 ^ (key & (DT == 64 ? 3 : 7))) << 4) + (d & 15);
-    };
+    const auto k_at = [&](const uint16_t *buffer, int key, int d) { return buffer + key * DT + ((d >> 3 ^ k_turn(key)) << 3); };
+    const auto v_at = [&](const uint16_t *buffer, int key, int d) { return buffer + key * DT + ((d >> 4 ^ v_turn(key)) << 4) + (d & 15); };
 
     // ---- Q: lane (h, r32) has of row r32 the elements 16 c + 8 h .. ----
     u32x4 qr[C];
@@ -219,14 +226,20 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
         if (work) {
             f32x16 s[KT];
 #pragma unroll
-            for (int t = 0; t < KT; ++t) {
+            for (int t = 0; t < KT; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
+            // (a few pieces of K ahead of their use: the compiler would wait for each)
+            constexpr int kAhead = 4, kSteps = KT * C;
+            u32x4 a[kAhead];
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const u32x4 a = *reinterpret_cast<const u32x4 *>(k_at(kb, 32 * t + r32, 16 * c + 8 * h));
-                    s[t] = mfma32<BF>(a, qr[c], s[t]);
-                }
+            for (int n = 0; n < kAhead; ++n) a[n] = *reinterpret_cast<const u32x4 *>(k_at(kb, 32 * (n / C) + r32, 16 * (n % C) + 8 * h));
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < kSteps; ++n) {
+                s[n / C] = mfma32<BF>(a[n % kAhead], qr[n % C], s[n / C]);
+                if (n + kAhead < kSteps) a[n % kAhead] = *reinterpret_cast<const u32x4 *>(k_at(kb, 32 * ((n + kAhead) / C) + r32, 16 * ((n + kAhead) % C) + 8 * h));
+                __builtin_amdgcn_sched_barrier(0);
             }
             // number 16 t + 4 u + i of a lane is key 32 t + 8 u + 4 h + i
             float x[16 * KT];
@@ -234,9 +247,10 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
             for (int e = 0; e < 16 * KT; ++e) x[e] = s[e >> 4][e & 15];
             if (key0 + KB > all_to || key0 < all_from) {
                 const unsigned span = max(to - from, 0);
+                int key = key0 + 4 * h - from;
+                asm volatile("" : "+v"(key));  // (or 32 sums of it would take registers over the loop)
 #pragma unroll
-                for (int e = 0; e < 16 * KT; ++e)
-                    x[e] = (unsigned)(key0 + 32 * (e >> 4) + 8 * (e >> 2 & 3) + 4 * h + (e & 3) - from) < span ? x[e] : -INFINITY;
+                for (int e = 0; e < 16 * KT; ++e) x[e] = (unsigned)(key + 32 * (e >> 4) + 8 * (e >> 2 & 3) + (e & 3)) < span ? x[e] : -INFINITY;
             }
             float high = x[0];
 #pragma unroll
@@ -260,10 +274,17 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
             }
         }
         if (work) {
+            constexpr int kAhead = 4, kSteps = KB / 16 * DV;
+            u32x4 a[kAhead];
 #pragma unroll
-            for (int u = 0; u < KB / 16; ++u)
+            for (int n = 0; n < kAhead; ++n) a[n] = column(n / DV, n % DV, lane);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int d = 0; d < DV; ++d) o[d] = mfma32<BF>(column(u, d, lane), weight[u], o[d]);
+            for (int n = 0; n < kSteps; ++n) {
+                o[n % DV] = mfma32<BF>(a[n % kAhead], weight[n / DV], o[n % DV]);
+                if (n + kAhead < kSteps) a[n % kAhead] = column((n + kAhead) / DV, (n + kAhead) % DV, lane);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
     if (b0 < b1) {
