@@ -19,6 +19,7 @@ struct AttendParams {
     float scale;       // times log2 e
     int rows;          // requests of at most this many rows (new tokens times group) are the stream kernel's
     int workers;       // stream kernel: waves per kv head
+    int join_rows;     // its join: rows of a workgroup
     int parts;         // chunk kernel: pieces that a tile's keys are cut into
 };
 

@@ -24,9 +24,10 @@ constexpr int kBlock = 32;  // keys of a step
 constexpr int kWaves = 4;
 constexpr float kGrow = 8.0f;
 constexpr int kStreamRows = 16;
+constexpr long long kPassingBytes = 128ll << 20;  // half of what the last level holds
 
 // Waves per SIMD: what the registers allow.
-constexpr int stream_occupancy(int dim, bool any) { return dim == 64 ? (any ? 3 : 4) : dim == 128 ? 2 : 1; }
+constexpr int stream_occupancy(int dim, bool any) { return dim == 64 ? 3 : dim == 128 ? 2 : 1; }
 
 // Blocks of a request in the line; a request whose rows see nothing has one, which writes its zeros.
 __device__ __forceinline__ int blocks_of(const AttendParams &p, const Request &q)
@@ -74,21 +75,22 @@ struct Segment {
 
 }  // namespace
 
-// DT: head_dim, or what it is padded to.  ANY: head_dim < DT, or pages of fewer than 16 slots.
-template <int DT, bool BF, bool ANY>
+// DT: head_dim, or what it is padded to.  ANY: head_dim < DT, or pages of fewer than 16 slots.  PASSING: K and V leave nothing in the caches.
+template <int DT, bool BF, bool ANY, bool PASSING>
 __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_attend_stream_kernel(AttendParams p)
 {
     constexpr int C = DT / 32, DV = DT / 16;     // matrix steps over head_dim; tiles of O
-    constexpr int kRowLanes = DT / 8, kRows = 64 / kRowLanes;  // a load of V covers kRows keys
-    __shared__ __attribute__((aligned(16))) uint16_t v_lds[kWaves][kBlock * DT];
+    constexpr int kRowLanes = DT / 8, kRows = 64 / kRowLanes;  // a load covers kRows keys
+    __shared__ __attribute__((aligned(16))) uint16_t lds[kWaves][2 * kBlock * DT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4;
     const int index = blockIdx.x * kWaves + wave;
     const int head = index % p.kv_heads, worker = index / p.kv_heads;
     int first_head = head * p.group;  // (of q)
     if (ANY) asm("" : "+v"(first_head));
-    uint16_t *const vs = v_lds[wave];
-    // element d of key j in LDS: 16-element units of a row exchanged by the key, so that eight keys' units of one number fill all banks
+    uint16_t *const ks = lds[wave], *const vs = ks + kBlock * DT;
+    // element d of key j in LDS: units of a row (8 elements of K, 16 of V) exchanged by the key, so that the units of one number fill all banks
+    const auto k_at = [&](int key, int d) { return ks + key * DT + ((d >> 3 ^ (DT == 64 ? key >> 1 & 7 : key & 15)) << 3); };
     const auto v_at = [&](int key, int d) {
         const int turn = DT == 64 ? key >> 1 & 3 : key & 7;
         return vs + key * DT + ((d >> 4 ^ turn) << 4) + (d & 15);
@@ -122,7 +124,8 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
         return e;
     };
 
-    // ---- requests to memory: lane (g, r16) has of K the elements 32 c + 8 g .. of keys r16 and 16 + r16 ----
+    // ---- requests to memory: whole rows, kRows of them at a time ----
+    const int in_rows = lane / kRowLanes, d_own = 8 * (lane % kRowLanes);
     u32x4 kr[2][C], vr[2][C];
     long long page_stride = p.page_stride, head_offset = head * p.head_stride;
     int slot_stride = p.slot_stride, last_page = p.num_pages - 1;
@@ -145,13 +148,12 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
                 const long long base = __builtin_amdgcn_readfirstlane(id[t]) * page_stride + head_offset +
                                        (long long)((key & ((1 << p.page_shift) - 1)) * p.slot_stride);
                 const char *const kp = reinterpret_cast<const char *>(p.k + base), *const vp = reinterpret_cast<const char *>(p.v + base);
-                const unsigned k_off = 2 * (unsigned)(min(r16, last - key) * p.slot_stride + 8 * g);
-#pragma unroll
-                for (int c = 0; c < C; ++c) kr[t][c] = *reinterpret_cast<const u32x4 *>(kp + k_off + 64 * c);
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
-                    const unsigned v_off = 2 * (unsigned)(min(c * kRows + lane / kRowLanes, last - key) * p.slot_stride + 8 * (lane % kRowLanes));
-                    vr[t][c] = *reinterpret_cast<const u32x4 *>(vp + v_off);
+                    const unsigned off = 2 * (unsigned)(min(c * kRows + in_rows, last - key) * p.slot_stride + d_own);
+                    const u32x4 *const ka = reinterpret_cast<const u32x4 *>(kp + off), *const va = reinterpret_cast<const u32x4 *>(vp + off);
+                    if (PASSING) kr[t][c] = __builtin_nontemporal_load(ka), vr[t][c] = __builtin_nontemporal_load(va);
+                    else kr[t][c] = *ka, vr[t][c] = *va;
                 }
             } else {
                 const auto place = [&](int row) {
@@ -159,12 +161,12 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
                     const int page = min(max(p.pages[(long long)r * p.max_pages + (j >> p.page_shift)], 0), last_page);
                     return page * page_stride + head_offset + (long long)((j & ((1 << p.page_shift) - 1)) * slot_stride);
                 };
-                const auto load = [&](const uint16_t *row, int d) { return *reinterpret_cast<const u32x4 *>(d < dim ? row + d : g_zeros); };
-                const uint16_t *const kp = p.k + place(r16);
 #pragma unroll
-                for (int c = 0; c < C; ++c) kr[t][c] = load(kp, 32 * c + 8 * g);
-#pragma unroll
-                for (int c = 0; c < C; ++c) vr[t][c] = load(p.v + place(c * kRows + lane / kRowLanes), 8 * (lane % kRowLanes));
+                for (int c = 0; c < C; ++c) {
+                    const long long at = place(c * kRows + in_rows);
+                    kr[t][c] = *reinterpret_cast<const u32x4 *>(d_own < dim ? p.k + at + d_own : g_zeros);
+                    vr[t][c] = *reinterpret_cast<const u32x4 *>(d_own < dim ? p.v + at + d_own : g_zeros);
+                }
             }
         }
     };
@@ -201,7 +203,7 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
     begin_request(now);
 
     while (true) {
-        // V to LDS, scores
+        // K and V to LDS, scores
         const int key0 = now.key;
         const bool masked = key0 + kBlock > all_to || key0 < all_from;
         // Infinities or NaN among values that not every row sees: zero times them must not reach the rows that do not.  They are replaced by
@@ -219,15 +221,10 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-                *reinterpret_cast<u32x4 *>(v_at(16 * t + c * kRows + lane / kRowLanes, 8 * (lane % kRowLanes))) = vr[t][c];
-        f32x4 s[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int c = 0; c < C; ++c) s[t] = mfma16<BF>(kr[t][c], q[c], s[t]);
-        }
+            for (int c = 0; c < C; ++c) {
+                *reinterpret_cast<u32x4 *>(k_at(16 * t + c * kRows + in_rows, d_own)) = kr[t][c];
+                *reinterpret_cast<u32x4 *>(v_at(16 * t + c * kRows + in_rows, d_own)) = vr[t][c];
+            }
         now.key += kBlock;
         --now.blocks;
         ++at;
@@ -239,6 +236,14 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
             }
             request(next.r, next.len, next.key);
             if (next.blocks > 1) find_pages(next.r, next.len, next.key + kBlock);
+        }
+        f32x4 s[2];
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < C; ++c) s[t] = mfma16<BF>(*reinterpret_cast<const u32x4 *>(k_at(16 * t + r16, 32 * c + 8 * g)), q[c], s[t]);
         }
         // weights: number 4 t + i of a lane is key 16 t + 4 g + i
         float x[8];
@@ -300,7 +305,7 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
-                    u32x4 *const mine = reinterpret_cast<u32x4 *>(v_at(16 * t + c * kRows + lane / kRowLanes, 8 * (lane % kRowLanes)));
+                    u32x4 *const mine = reinterpret_cast<u32x4 *>(v_at(16 * t + c * kRows + in_rows, d_own));
                     u32x4 x = *mine;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) x[i] = finite_only<BF>(x[i]);
@@ -340,17 +345,19 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
     }
 }
 
-// Joins what the waves left of a request: a workgroup per (request, kv head, row), its waves share the pieces.
+// Joins what the waves left of a request.  A workgroup has p.join_rows rows of a (request, kv head): a wave has a row to itself where the
+// pieces are few, else all waves share the pieces of each row in turn.
 template <int DT, bool BF>
 __global__ __launch_bounds__(64 * kWaves) void bcq_attend_join_kernel(AttendParams p)
 {
     constexpr int E = DT / 64;  // elements of a lane
+    constexpr int kAhead = 8;   // pieces requested together
     __shared__ float shared[kWaves][DT + 2];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r = blockIdx.x, head = blockIdx.y, row = blockIdx.z;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = blockIdx.x, head = blockIdx.y, first_row = blockIdx.z * p.join_rows;
     const Request q = load_request(p, r);
-    const int own = blocks_of(p, q);
-    if (own == 0 || row >= q.todo * p.group) return;
+    const int own = blocks_of(p, q), rows = min(q.todo * p.group - first_row, p.join_rows);
+    if (own == 0 || rows <= 0) return;
     int total = 0, upto = 0;
     for (int c = 0; c < p.requests; c += 64) {
         Window w;
@@ -361,43 +368,78 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_attend_join_kernel(AttendPara
     const int workers = workers_of(p, total);
     const int w0 = worker_of(upto - own, workers, total), w1 = worker_of(upto - 1, workers, total);
     if (w0 == w1) return;  // finished by its one wave
-    const auto slot = [&](int w) { return ((long long)(w + r) * p.kv_heads + head) * kStreamRows + row; };
-    float most = -INFINITY;
-    for (int w = w0 + lane; w <= w1; w += 64) most = fmaxf(most, p.stat[slot(w)].x);
+    const auto slot = [&](int w, int row) { return ((long long)(w + r) * p.kv_heads + head) * kStreamRows + row; };
+    const auto finish = [&](int row, const float (&y)[E], float weight) {
+        int from, to;
+        visible_keys(p, q.n, q.len, row / p.group, from, to);
+        uint16_t *const dst = p.out + (long long)(q.start + row / p.group) * p.ld_out + (head * p.group + row % p.group) * p.head_dim;
 #pragma unroll
-    for (int step = 32; step > 0; step >>= 1) most = fmaxf(most, __shfl_xor(most, step));
-    const float base = most == -INFINITY ? 0.0f : most;
-    float weight = 0.0f, y[E] = {};
-#pragma unroll 4
-    for (int w = w0 + wave; w <= w1; w += kWaves) {
-        const long long s = slot(w);
-        const f32x2 stat = p.stat[s];
-        const float scale = exp2_fast(stat.x - base);
-        weight = fmaf(stat.y, scale, weight);
+        for (int e = 0; e < E; ++e)
+            if (lane * E + e < p.head_dim) dst[lane * E + e] = from_float<BF>(to > from ? y[e] / weight : 0.0f);
+    };
+    // sums over pieces begin, begin + step, .., 64 at a time: their statistics are a lane's each
+    const auto gather = [&](int row, int begin, int step, float base, float (&y)[E], float &weight) {
+        weight = 0.0f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = fmaf(p.part[s * DT + lane * E + e], scale, y[e]);
+        for (int e = 0; e < E; ++e) y[e] = 0.0f;
+        for (int c = begin; c <= w1; c += 64 * step) {
+            const int mine = c + lane * step;
+            const f32x2 stat = p.stat[slot(min(mine, w1), row)];
+            const float scale = exp2_fast(stat.x - base);
+            if (mine <= w1) weight = fmaf(stat.y, scale, weight);
+            const int n = min((w1 - c) / step + 1, 64);
+            for (int i = 0; i < n; i += kAhead) {
+                float part[kAhead][E];
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) part[j][e] = p.part[slot(c + min(i + j, n - 1) * step, row) * DT + lane * E + e];
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) {
+                    const float times = i + j < n ? __shfl(scale, (i + j) & 63) : 0.0f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) y[e] = i + j < n ? fmaf(part[j][e], times, y[e]) : y[e];
+                }
+            }
+        }
+#pragma unroll
+        for (int step = 32; step > 0; step >>= 1) weight += __shfl_xor(weight, step);
+    };
+    const auto base_of = [&](int row) {
+        float most = -INFINITY;
+        for (int w = w0 + lane; w <= w1; w += 64) most = fmaxf(most, p.stat[slot(w, row)].x);
+#pragma unroll
+        for (int step = 32; step > 0; step >>= 1) most = fmaxf(most, __shfl_xor(most, step));
+        return most == -INFINITY ? 0.0f : most;
+    };
+    float y[E], weight;
+    if (p.join_rows == kWaves && w1 - w0 < 2 * kAhead) {
+        if (wave >= rows) return;
+        const int row = first_row + wave;
+        gather(row, w0, 1, base_of(row), y, weight);
+        finish(row, y, weight);
+        return;
     }
+    for (int row = first_row; row < first_row + rows; ++row) {
+        gather(row, w0 + wave, kWaves, base_of(row), y, weight);
 #pragma unroll
-    for (int e = 0; e < E; ++e) shared[wave][lane * E + e] = y[e];
-    if (lane == 0) shared[wave][DT] = weight;
-    __syncthreads();
-    if (wave != 0) return;
-    float all = 0.0f;
+        for (int e = 0; e < E; ++e) shared[wave][lane * E + e] = y[e];
+        if (lane == 0) shared[wave][DT] = weight;
+        __syncthreads();
+        if (wave == 0) {
+            weight = 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) y[e] = 0.0f;
+            for (int e = 0; e < E; ++e) y[e] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        all += shared[w][DT];
+            for (int w = 0; w < kWaves; ++w) {
+                weight += shared[w][DT];
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] += shared[w][lane * E + e];
+                for (int e = 0; e < E; ++e) y[e] += shared[w][lane * E + e];
+            }
+            finish(row, y, weight);
+        }
+        __syncthreads();
     }
-    const int token = row / p.group;
-    int from, to;
-    visible_keys(p, q.n, q.len, token, from, to);
-    uint16_t *const dst = p.out + (long long)(q.start + token) * p.ld_out + (head * p.group + row % p.group) * p.head_dim;
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-        if (lane * E + e < p.head_dim) dst[lane * E + e] = from_float<BF>(to > from ? y[e] / all : 0.0f);
 }
 
 namespace {
@@ -414,29 +456,34 @@ StreamPlan stream_plan(const bcq_cache &c, int requests)
     StreamPlan s;
     s.dim = padded_dim(c.head_dim);
     s.any = c.head_dim != s.dim || c.page_size < 16;
-    s.workers = (compute_units() * kWaves * stream_occupancy(s.dim, s.any) + c.kv_heads - 1) / c.kv_heads;  // as many waves as the chip holds
+    // As many waves as the chip holds: one workgroup more would start when the others end.
+    s.workers = compute_units() * kWaves * stream_occupancy(s.dim, s.any) / c.kv_heads;
+    if (s.workers < 1) s.workers = 1;
     s.slots = (size_t)(s.workers + requests) * c.kv_heads * kStreamRows;
     s.part_bytes = s.slots * s.dim * sizeof(float);
     return s;
 }
 
 template <int DT, bool BF>
-void stream_and_join(const AttendParams &p, bool any, hipStream_t s)
+void stream_and_join(const AttendParams &p, bool any, bool passing, hipStream_t s)
 {
     const int groups = (p.workers * p.kv_heads + kWaves - 1) / kWaves;
-    if (any) bcq_attend_stream_kernel<DT, BF, true><<<groups, 64 * kWaves, 0, s>>>(p);
-    else bcq_attend_stream_kernel<DT, BF, false><<<groups, 64 * kWaves, 0, s>>>(p);
+    if (any) bcq_attend_stream_kernel<DT, BF, true, false><<<groups, 64 * kWaves, 0, s>>>(p);
+    else if (passing) bcq_attend_stream_kernel<DT, BF, false, true><<<groups, 64 * kWaves, 0, s>>>(p);
+    else bcq_attend_stream_kernel<DT, BF, false, false><<<groups, 64 * kWaves, 0, s>>>(p);
     const long long most = (long long)p.max_new * p.group;
-    const dim3 grid(p.requests, p.kv_heads, (unsigned)(most < kStreamRows ? most : kStreamRows));
-    bcq_attend_join_kernel<DT, BF><<<grid, 64 * kWaves, 0, s>>>(p);
+    const int rows = (int)(most < kStreamRows ? most : kStreamRows);
+    AttendParams j = p;
+    j.join_rows = (long long)p.requests * p.kv_heads * rows >= 2 * kWaves * compute_units() ? kWaves : 1;
+    bcq_attend_join_kernel<DT, BF><<<dim3(p.requests, p.kv_heads, (rows + j.join_rows - 1) / j.join_rows), 64 * kWaves, 0, s>>>(j);
 }
 
 template <bool BF>
-void by_dim(const AttendParams &p, int dim, bool any, hipStream_t s)
+void by_dim(const AttendParams &p, int dim, bool any, bool passing, hipStream_t s)
 {
-    if (dim == 64) stream_and_join<64, BF>(p, any, s);
-    else if (dim == 128) stream_and_join<128, BF>(p, any, s);
-    else stream_and_join<256, BF>(p, any, s);
+    if (dim == 64) stream_and_join<64, BF>(p, any, passing, s);
+    else if (dim == 128) stream_and_join<128, BF>(p, any, passing, s);
+    else stream_and_join<256, BF>(p, any, passing, s);
 }
 
 // Which kernels a call needs: the stream kernel has the requests of up to kStreamRows rows, the chunk kernel the others.  The host knows tokens,
@@ -484,9 +531,13 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t stream)
     const Split which = split(a.tokens, a.requests, p.group, a.max_new);
     if (which.stream) {
         p.rows = kStreamRows, p.workers = plan.workers;
+        // Every byte of K and V is read by one wave.  Loads that leave nothing behind for others are faster (8 heads of 128, 1 GiB: 177 us against
+        // 199), unless the cache is so small that it may still be in the last level from the call before (32 x 2000 keys of 4 heads of 64,
+        // 66 MB: 24.5 us against 22).
+        const bool passing = 4 * (long long)c.num_pages * c.page_stride >= kPassingBytes;
         p.stat = reinterpret_cast<f32x2 *>(static_cast<char *>(a.workspace) + plan.part_bytes);
-        if (c.dtype == BCQ_BF16) by_dim<true>(p, plan.dim, plan.any, stream);
-        else by_dim<false>(p, plan.dim, plan.any, stream);
+        if (c.dtype == BCQ_BF16) by_dim<true>(p, plan.dim, plan.any, passing, stream);
+        else by_dim<false>(p, plan.dim, plan.any, passing, stream);
     }
     if (which.chunk) {
         p.rows = which.stream ? kStreamRows : 0;
