@@ -52,6 +52,20 @@ __device__ __forceinline__ void visible_keys(const AttendParams &p, const int n,
     begin = p.window ? max(position + 1 - p.window, 0) : 0;
 }
 
+// The last request of which begins(r) holds, all lanes together (begins(0) is taken to hold, and begins is never true again once it is false).
+template <class F>
+__device__ __forceinline__ int last_request(const AttendParams &p, int lane, F begins)
+{
+    int r = 0;
+    for (int high = p.requests; high - r > 1;) {
+        const int stride = (high - r + 63) / 64, probe = r + lane * stride;
+        const int count = __popcll(__ballot(probe < high && begins(probe)));
+        r += max(count - 1, 0) * stride;
+        high = min(high, r + stride);
+    }
+    return r;
+}
+
 __device__ __forceinline__ int page_of(const AttendParams &p, int r, int key)
 {
     return min(max(p.pages[(long long)r * p.max_pages + (key >> p.page_shift)], 0), p.num_pages - 1);
@@ -62,8 +76,51 @@ static __device__ __attribute__((aligned(16))) const uint16_t g_zeros[8] = {};
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Joining the pieces of a row: piece i has its sums in part and its (maximum, weight) in stat at first + i * step.
+struct Slots {
+    long long first, step;
+    __device__ __forceinline__ long long operator()(int i) const { return first + i * step; }
+};
+constexpr int kJoinAhead = 8;  // pieces requested together
+
+// y, weight: sums over the pieces from + share, from + share + STRIDE, .. < end, relative to the maximum over all pieces from .. end - 1.
+template <int DT, int STRIDE>
+__device__ __forceinline__ void join_pieces(const AttendParams &p, Slots at, int from, int end, int share, int lane, float (&y)[DT / 64], float &weight)
+{
+    constexpr int E = DT / 64;  // elements of a lane
+    float most = -INFINITY;
+    for (int i = from + lane; i < end; i += 64) most = fmaxf(most, p.stat[at(i)].x);
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
+    const float base = most == -INFINITY ? 0.0f : most;
+    weight = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) y[e] = 0.0f;
+    for (int c = from + share; c < end; c += 64 * STRIDE) {  // sixty-four pieces, a lane has the statistics of one
+        const int mine = c + lane * STRIDE, n = min((end - 1 - c) / STRIDE + 1, 64);
+        const f32x2 stat = p.stat[at(min(mine, end - 1))];
+        const float scale = exp2_fast(stat.x - base);
+        if (mine < end) weight = fmaf(stat.y, scale, weight);
+        for (int i = 0; i < n; i += kJoinAhead) {
+            float part[kJoinAhead][E];
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j)
+#pragma unroll
+                for (int e = 0; e < E; ++e) part[j][e] = p.part[at(c + min(i + j, n - 1) * STRIDE) * DT + lane * E + e];
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j) {
+                const float times = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scale), min(i + j, n - 1)));
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[e] = i + j < n ? fmaf(part[j][e], times, y[e]) : y[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) weight += __shfl_xor(weight, s);
+}
+
 // The chunk kernel (bcq_attend_chunk.hip): requests of more than p.rows rows.  dim: the padded head_dim.
 int chunk_parts(int tokens, int group, int kv_heads, int dim, long long most_keys);
-void launch_chunks(const AttendParams &p, int dim, bool any, bool bf16, hipStream_t s);
+void launch_chunks(const AttendParams &p, int dim, bool any, bool passing, bool bf16, hipStream_t s);
 
 }  // namespace bcq

@@ -24,6 +24,8 @@ constexpr int kBlock = 32;  // keys of a step
 constexpr int kWaves = 4;
 constexpr float kGrow = 8.0f;
 constexpr int kStreamRows = 16;
+constexpr int kDirectKeys = 1024;
+constexpr int kMostRows = 128;  // of a tile of either kernel
 constexpr long long kPassingBytes = 128ll << 20;  // half of what the last level holds
 
 // Waves per SIMD: what the registers allow.
@@ -76,7 +78,8 @@ struct Segment {
 }  // namespace
 
 // DT: head_dim, or what it is padded to.  ANY: head_dim < DT, or pages of fewer than 16 slots.  PASSING: K and V leave nothing in the caches.
-template <int DT, bool BF, bool ANY, bool PASSING>
+// DIRECT: a workgroup has a request and kv head to itself, which its waves share and join.
+template <int DT, bool BF, bool ANY, bool PASSING, bool DIRECT>
 __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_attend_stream_kernel(AttendParams p)
 {
     constexpr int C = DT / 32, DV = DT / 16;     // matrix steps over head_dim; tiles of O
@@ -85,7 +88,7 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4;
     const int index = blockIdx.x * kWaves + wave;
-    const int head = index % p.kv_heads, worker = index / p.kv_heads;
+    const int head = DIRECT ? blockIdx.x % p.kv_heads : index % p.kv_heads, worker = index / p.kv_heads;
     int first_head = head * p.group;  // (of q)
     if (ANY) asm("" : "+v"(first_head));
     uint16_t *const ks = lds[wave], *const vs = ks + kBlock * DT;
@@ -96,18 +99,28 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
         return vs + key * DT + ((d >> 4 ^ turn) << 4) + (d & 15);
     };
 
-    // ---- this wave's piece of the line ----
+    // ---- this wave's piece of the line, or of the request ----
     Window w;
-    int total = 0, first = 0;
-    for (int c = 0; c < p.requests; c += 64) {
-        w.load(p, c, total, lane);
-        total = lane_of(w.upto, 63);
+    Segment now;
+    int total = 0, first = 0, at, stop;
+    if (DIRECT) {
+        const int r = blockIdx.x / p.kv_heads;
+        const Request own = load_request(p, r);
+        total = blocks_of(p, own);
+        if (total == 0) return;
+        at = total * wave / kWaves, stop = total * (wave + 1) / kWaves;
+        now = Segment{r, own.start, own.n, own.todo, own.len, (own.begin / kBlock + at) * kBlock, stop - at, false};
+    } else {
+        for (int c = 0; c < p.requests; c += 64) {
+            w.load(p, c, total, lane);
+            total = lane_of(w.upto, 63);
+        }
+        const int workers = workers_of(p, total);
+        if (worker >= workers || total == 0) return;
+        at = first_block(worker, workers, total);
+        stop = first_block(worker + 1, workers, total);
+        if (p.requests > 64) w.load(p, 0, 0, lane);
     }
-    const int workers = workers_of(p, total);
-    if (worker >= workers || total == 0) return;
-    int at = first_block(worker, workers, total);
-    const int stop = first_block(worker + 1, workers, total);
-    if (p.requests > 64) w.load(p, 0, 0, lane);
     const auto segment_at = [&](int place) {
         while (lane_of(w.upto, 63) <= place) w.load(p, first += 64, lane_of(w.upto, 63), lane);
         const int l = __builtin_ctzll(__ballot(w.upto > place));
@@ -171,9 +184,12 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
         }
     };
 
-    Segment now = segment_at(at);
-    find_pages(now.r, now.len, now.key);
-    request(now.r, now.len, now.key);
+    if (!DIRECT) now = segment_at(at);
+    const bool any_block = !DIRECT || now.blocks > 0;
+    if (any_block) {
+        find_pages(now.r, now.len, now.key);
+        request(now.r, now.len, now.key);
+    }
     if (now.blocks > 1) find_pages(now.r, now.len, now.key + kBlock);
 
     // ---- rows: column r16 is token r16 / group, query head r16 mod group ----
@@ -202,7 +218,7 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
     };
     begin_request(now);
 
-    while (true) {
+    while (any_block) {
         // K and V to LDS, scores
         const int key0 = now.key;
         const bool masked = key0 + kBlock > all_to || key0 < all_from;
@@ -230,7 +246,7 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
         ++at;
         Segment next = now;
         if (at < stop) {
-            if (!now.blocks) {
+            if (!DIRECT && !now.blocks) {
                 next = segment_at(at);
                 find_pages(next.r, next.len, next.key);
             }
@@ -320,6 +336,7 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
         }
         asm volatile("" ::: "memory");
         if (now.blocks) continue;
+        if (DIRECT) break;
         const float weight = sum_over_groups(sum), unit = 1.0f / weight;
         if (token < now.todo) {
             if (now.whole) {
@@ -343,6 +360,39 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
         now = next;
         begin_request(now);
     }
+    if (!DIRECT) return;
+
+    // ---- the waves' sums through LDS, each in its wave's own part; a row's are four banks from the next one's ----
+    constexpr int kStep = DT + 4;
+    static_assert(kStreamRows * kStep * sizeof(float) <= 2 * kBlock * DT * sizeof(uint16_t), "");
+    __shared__ f32x2 stat[DIRECT ? kWaves : 1][kStreamRows];
+    const auto sums = [&](int w) { return reinterpret_cast<float *>(lds[w]); };
+    const float part_weight = sum_over_groups(sum);
+#pragma unroll
+    for (int d = 0; d < DV; ++d) *reinterpret_cast<f32x4 *>(sums(wave) + r16 * kStep + 16 * d + 4 * g) = o[d];
+    if (g == 0) stat[wave][r16] = f32x2{most, part_weight};
+    __syncthreads();
+    const int rows = now.todo * p.group;
+    for (int i = threadIdx.x; i < rows * (DT / 4); i += 64 * kWaves) {
+        const int row = i / (DT / 4), d = 4 * (i % (DT / 4)), t = row / p.group;
+        if (ANY && d >= p.head_dim) continue;
+        float high = -INFINITY, all = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) high = fmaxf(high, stat[w][row].x);
+        if (high == -INFINITY) high = 0.0f;
+        f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float scale = exp2_fast(stat[w][row].x - high);
+            all = fmaf(stat[w][row].y, scale, all);
+            y += *reinterpret_cast<const f32x4 *>(sums(w) + row * kStep + d) * scale;
+        }
+        y *= 1.0f / all;
+        visible_keys(p, now.n, now.len, t, from, to);
+        if (to <= from) y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        uint16_t *const dst = p.out + (long long)(now.start + t) * p.ld_out + (head * p.group + row % p.group) * p.head_dim;
+        *reinterpret_cast<u32x2 *>(dst + d) = u32x2{from_float2<BF>(y[0], y[1]), from_float2<BF>(y[2], y[3])};
+    }
 }
 
 // Joins what the waves left of a request.  A workgroup has p.join_rows rows of a (request, kv head): a wave has a row to itself where the
@@ -351,7 +401,6 @@ template <int DT, bool BF>
 __global__ __launch_bounds__(64 * kWaves) void bcq_attend_join_kernel(AttendParams p)
 {
     constexpr int E = DT / 64;  // elements of a lane
-    constexpr int kAhead = 8;   // pieces requested together
     __shared__ float shared[kWaves][DT + 2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = blockIdx.x, head = blockIdx.y, first_row = blockIdx.z * p.join_rows;
@@ -368,7 +417,7 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_attend_join_kernel(AttendPara
     const int workers = workers_of(p, total);
     const int w0 = worker_of(upto - own, workers, total), w1 = worker_of(upto - 1, workers, total);
     if (w0 == w1) return;  // finished by its one wave
-    const auto slot = [&](int w, int row) { return ((long long)(w + r) * p.kv_heads + head) * kStreamRows + row; };
+    const auto slots = [&](int row) { return Slots{((long long)r * p.kv_heads + head) * kStreamRows + row, (long long)p.kv_heads * kStreamRows}; };
     const auto finish = [&](int row, const float (&y)[E], float weight) {
         int from, to;
         visible_keys(p, q.n, q.len, row / p.group, from, to);
@@ -377,51 +426,16 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_attend_join_kernel(AttendPara
         for (int e = 0; e < E; ++e)
             if (lane * E + e < p.head_dim) dst[lane * E + e] = from_float<BF>(to > from ? y[e] / weight : 0.0f);
     };
-    // sums over pieces begin, begin + step, .., 64 at a time: their statistics are a lane's each
-    const auto gather = [&](int row, int begin, int step, float base, float (&y)[E], float &weight) {
-        weight = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = 0.0f;
-        for (int c = begin; c <= w1; c += 64 * step) {
-            const int mine = c + lane * step;
-            const f32x2 stat = p.stat[slot(min(mine, w1), row)];
-            const float scale = exp2_fast(stat.x - base);
-            if (mine <= w1) weight = fmaf(stat.y, scale, weight);
-            const int n = min((w1 - c) / step + 1, 64);
-            for (int i = 0; i < n; i += kAhead) {
-                float part[kAhead][E];
-#pragma unroll
-                for (int j = 0; j < kAhead; ++j)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) part[j][e] = p.part[slot(c + min(i + j, n - 1) * step, row) * DT + lane * E + e];
-#pragma unroll
-                for (int j = 0; j < kAhead; ++j) {
-                    const float times = i + j < n ? __shfl(scale, (i + j) & 63) : 0.0f;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) y[e] = i + j < n ? fmaf(part[j][e], times, y[e]) : y[e];
-                }
-            }
-        }
-#pragma unroll
-        for (int step = 32; step > 0; step >>= 1) weight += __shfl_xor(weight, step);
-    };
-    const auto base_of = [&](int row) {
-        float most = -INFINITY;
-        for (int w = w0 + lane; w <= w1; w += 64) most = fmaxf(most, p.stat[slot(w, row)].x);
-#pragma unroll
-        for (int step = 32; step > 0; step >>= 1) most = fmaxf(most, __shfl_xor(most, step));
-        return most == -INFINITY ? 0.0f : most;
-    };
     float y[E], weight;
-    if (p.join_rows == kWaves && w1 - w0 < 2 * kAhead) {
+    if (p.join_rows == kWaves && w1 - w0 < 2 * kJoinAhead) {
         if (wave >= rows) return;
         const int row = first_row + wave;
-        gather(row, w0, 1, base_of(row), y, weight);
+        join_pieces<DT, 1>(p, slots(row), w0, w1 + 1, 0, lane, y, weight);
         finish(row, y, weight);
         return;
     }
     for (int row = first_row; row < first_row + rows; ++row) {
-        gather(row, w0 + wave, kWaves, base_of(row), y, weight);
+        join_pieces<DT, kWaves>(p, slots(row), w0, w1 + 1, wave, lane, y, weight);
 #pragma unroll
         for (int e = 0; e < E; ++e) shared[wave][lane * E + e] = y[e];
         if (lane == 0) shared[wave][DT] = weight;
@@ -467,10 +481,16 @@ StreamPlan stream_plan(const bcq_cache &c, int requests)
 template <int DT, bool BF>
 void stream_and_join(const AttendParams &p, bool any, bool passing, hipStream_t s)
 {
+    if (p.workers == 0) {  // no line: a workgroup per request and kv head
+        const unsigned groups = (unsigned)p.requests * p.kv_heads;
+        if (any) bcq_attend_stream_kernel<DT, BF, true, false, true><<<groups, 64 * kWaves, 0, s>>>(p);
+        else bcq_attend_stream_kernel<DT, BF, false, false, true><<<groups, 64 * kWaves, 0, s>>>(p);
+        return;
+    }
     const int groups = (p.workers * p.kv_heads + kWaves - 1) / kWaves;
-    if (any) bcq_attend_stream_kernel<DT, BF, true, false><<<groups, 64 * kWaves, 0, s>>>(p);
-    else if (passing) bcq_attend_stream_kernel<DT, BF, false, true><<<groups, 64 * kWaves, 0, s>>>(p);
-    else bcq_attend_stream_kernel<DT, BF, false, false><<<groups, 64 * kWaves, 0, s>>>(p);
+    if (any) bcq_attend_stream_kernel<DT, BF, true, false, false><<<groups, 64 * kWaves, 0, s>>>(p);
+    else if (passing) bcq_attend_stream_kernel<DT, BF, false, true, false><<<groups, 64 * kWaves, 0, s>>>(p);
+    else bcq_attend_stream_kernel<DT, BF, false, false, false><<<groups, 64 * kWaves, 0, s>>>(p);
     const long long most = (long long)p.max_new * p.group;
     const int rows = (int)(most < kStreamRows ? most : kStreamRows);
     AttendParams j = p;
@@ -527,23 +547,27 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t stream)
     p.tokens = a.tokens, p.requests = a.requests, p.kv_heads = c.kv_heads, p.group = a.q_heads / c.kv_heads;
     p.head_dim = c.head_dim, p.page_shift = __builtin_ctz(c.page_size), p.num_pages = c.num_pages, p.max_pages = a.max_pages;
     p.max_new = a.max_new, p.window = a.window, p.causal = a.causal;
+    // What the rows of a tile can see at most, as far as the host knows.
+    long long most_keys = (long long)a.max_pages * c.page_size;
+    const int tile_tokens = kMostRows / p.group + 2 < a.max_new ? kMostRows / p.group + 2 : a.max_new;
+    if (a.window && (long long)a.window + tile_tokens < most_keys) most_keys = (long long)a.window + tile_tokens;
     p.scale = (float)(a.scale * 1.4426950408889634);
     const Split which = split(a.tokens, a.requests, p.group, a.max_new);
+    // Where every byte of K and V is read once, loads that leave nothing behind for others are faster (8 heads of 128, 1 GiB: 177 us against
+    // 199), unless the cache is so small that it may still be in the last level from the call before (32 x 2000 keys of 4 heads of 64,
+    // 66 MB: 24.5 us against 22).
+    const bool passing = 4 * (long long)c.num_pages * c.page_stride >= kPassingBytes;
     if (which.stream) {
-        p.rows = kStreamRows, p.workers = plan.workers;
-        // Every byte of K and V is read by one wave.  Loads that leave nothing behind for others are faster (8 heads of 128, 1 GiB: 177 us against
-        // 199), unless the cache is so small that it may still be in the last level from the call before (32 x 2000 keys of 4 heads of 64,
-        // 66 MB: 24.5 us against 22).
-        const bool passing = 4 * (long long)c.num_pages * c.page_stride >= kPassingBytes;
+        p.rows = kStreamRows, p.workers = most_keys <= kDirectKeys && (long long)a.requests * c.kv_heads <= 1 << 23 ? 0 : plan.workers;
         p.stat = reinterpret_cast<f32x2 *>(static_cast<char *>(a.workspace) + plan.part_bytes);
         if (c.dtype == BCQ_BF16) by_dim<true>(p, plan.dim, plan.any, passing, stream);
         else by_dim<false>(p, plan.dim, plan.any, passing, stream);
     }
     if (which.chunk) {
         p.rows = which.stream ? kStreamRows : 0;
-        p.parts = chunk_parts(a.tokens, p.group, c.kv_heads, plan.dim, (long long)a.max_pages * c.page_size);
+        p.parts = chunk_parts(a.tokens, p.group, c.kv_heads, plan.dim, most_keys);
         p.stat = reinterpret_cast<f32x2 *>(static_cast<char *>(a.workspace) + chunk_part_bytes(p.parts, a.tokens, a.q_heads, plan.dim));
-        launch_chunks(p, plan.dim, plan.any, c.dtype == BCQ_BF16, stream);
+        launch_chunks(p, plan.dim, plan.any, passing, c.dtype == BCQ_BF16, stream);
     }
     return hipGetLastError();
 }

@@ -20,16 +20,18 @@ namespace {
 
 constexpr int kWaves = 4, kChunkRows = 32 * kWaves;
 constexpr float kGrow = 8.0f;
+constexpr int kFewParts = 8;
 constexpr int chunk_keys(int dim) { return dim == 256 ? 32 : 64; }  // a block
 constexpr int chunk_occupancy(int dim) { return dim == 256 ? 1 : 2; }
 
 typedef __attribute__((address_space(3))) void *lds_void;
 typedef const __attribute__((address_space(1))) void *global_void;
 
-// Sixteen bytes a lane from memory to LDS: lane l's to `to` (the wave's) + 16 l.
+// Sixteen bytes a lane from memory to LDS: lane l's to `to` (the wave's) + 16 l.  PASSING: nothing is left behind in the caches.
+template <bool PASSING>
 __device__ __forceinline__ void load_to_lds(const uint16_t *from, uint16_t *to)
 {
-    __builtin_amdgcn_global_load_lds((global_void)from, (lds_void)to, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((global_void)from, (lds_void)to, 16, 0, PASSING ? 2 : 0);
 }
 
 // This wave's transfers to LDS have arrived, and its reads of LDS have returned: what the barrier after it promises the other waves.
@@ -43,7 +45,7 @@ __device__ __forceinline__ int tile_slots_before(const AttendParams &p, int r)
 }  // namespace
 
 // DT: head_dim, or what it is padded to.  ANY: head_dim < DT, or pages of fewer than 16 slots.
-template <int DT, bool BF, bool ANY>
+template <int DT, bool BF, bool ANY, bool PASSING>
 __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_chunk_kernel(AttendParams p)
 {
     constexpr int KB = chunk_keys(DT), KT = KB / 32, C = DT / 16, DV = DT / 32;
@@ -57,12 +59,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
     // ---- which rows: the slots of a request's tiles begin at q_start * group / 128 + r, the last tiles (with the most keys) first ----
     const int head = blockIdx.x % p.kv_heads, part = blockIdx.y;
     const int slot = gridDim.x / p.kv_heads - 1 - blockIdx.x / p.kv_heads;
-    int r = 0;
-    for (int high = p.requests; high - r > 1;) {
-        const int middle = (r + high) >> 1;
-        if (tile_slots_before(p, middle) <= slot) r = middle;
-        else high = middle;
-    }
+    const int r = last_request(p, lane, [&](int i) { return tile_slots_before(p, i) <= slot; });
     const Request q = load_request(p, r);
     const int rows = q.todo * p.group, row0 = (slot - tile_slots_before(p, r)) * kChunkRows;
     if (rows <= p.rows || row0 < 0 || row0 >= rows) return;
@@ -124,8 +121,8 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
                 k = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(k_head + base) + 2u * (row + k_d));
                 v = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(v_head + base) + 2u * (row + v_d));
             }
-            load_to_lds(k, to_k + (kOwn * wave + i * kRows) * DT);
-            load_to_lds(v, to_v + (kOwn * wave + i * kRows) * DT);
+            load_to_lds<PASSING>(k, to_k + (kOwn * wave + i * kRows) * DT);
+            load_to_lds<PASSING>(v, to_v + (kOwn * wave + i * kRows) * DT);
         }
     };
     // element d of key j
@@ -326,35 +323,30 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
     }
 }
 
-// Joins the parts: a wave per row.
+// Joins many parts: a workgroup per row, whose waves share them.
 template <int DT, bool BF>
-__global__ __launch_bounds__(64) void bcq_attend_chunk_join_kernel(AttendParams p)
+__global__ __launch_bounds__(64 * kWaves) void bcq_attend_chunk_join_kernel(AttendParams p)
 {
     constexpr int E = DT / 64;
-    const int lane = threadIdx.x, token = blockIdx.x / p.group, member = blockIdx.x % p.group, head = blockIdx.y;
-    int r = 0;
-    for (int high = p.requests; high - r > 1;) {
-        const int middle = (r + high) >> 1;
-        if (p.q_start[middle] <= token) r = middle;
-        else high = middle;
-    }
-    const Request q = load_request(p, r);
+    __shared__ float shared[kWaves][DT + 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int token = blockIdx.x / p.group, member = blockIdx.x % p.group, head = blockIdx.y;
+    const Request q = load_request(p, last_request(p, lane, [&](int i) { return p.q_start[i] <= token; }));
     const int i = token - q.start;
     if (i < 0 || i >= q.todo || q.todo * p.group <= p.rows) return;
-    const long long step = (long long)p.kv_heads * p.tokens * p.group, at = (long long)head * p.tokens * p.group + blockIdx.x;
-    float most = -INFINITY;
-    for (int k = lane; k < p.parts; k += 64) most = fmaxf(most, p.stat[k * step + at].x);
+    const long long rows = (long long)p.tokens * p.group;
+    float y[E], weight;
+    join_pieces<DT, kWaves>(p, Slots{head * rows + blockIdx.x, p.kv_heads * rows}, 0, p.parts, wave, lane, y, weight);
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) most = fmaxf(most, __shfl_xor(most, s));
-    const float base = most == -INFINITY ? 0.0f : most;
-    float weight = 0.0f, y[E] = {};
-#pragma unroll 4
-    for (int k = 0; k < p.parts; ++k) {
-        const f32x2 stat = p.stat[k * step + at];
-        const float scale = exp2_fast(stat.x - base);
-        weight = fmaf(stat.y, scale, weight);
+    for (int e = 0; e < E; ++e) shared[wave][lane * E + e] = y[e];
+    if (lane == 0) shared[wave][DT] = weight;
+    __syncthreads();
+    if (wave != 0) return;
 #pragma unroll
-        for (int e = 0; e < E; ++e) y[e] = fmaf(p.part[(k * step + at) * DT + lane * E + e], scale, y[e]);
+    for (int w = 1; w < kWaves; ++w) {
+        weight += shared[w][DT];
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[e] += shared[w][lane * E + e];
     }
     int from, to;
     visible_keys(p, q.n, q.len, i, from, to);
@@ -362,6 +354,50 @@ __global__ __launch_bounds__(64) void bcq_attend_chunk_join_kernel(AttendParams 
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (lane * E + e < p.head_dim) dst[lane * E + e] = from_float<BF>(to > from ? y[e] / weight : 0.0f);
+}
+
+// Joins few parts: four elements of a row to a thread, which reads all parts of them at once.
+template <int DT, bool BF>
+__global__ __launch_bounds__(64 * kWaves) void bcq_attend_chunk_join_few_kernel(AttendParams p)
+{
+    constexpr int kLanes = DT / 4;  // of a row
+    const int lane = threadIdx.x & 63, first = (blockIdx.x * 64 * kWaves + (threadIdx.x & ~63)) / kLanes, rows = p.tokens * p.group;
+    const int row = min(first + lane / kLanes, rows - 1), d = 4 * (lane % kLanes), head = blockIdx.y;
+    const int token = row / p.group, member = row % p.group, first_token = min(first, rows - 1) / p.group;
+    int r = last_request(p, lane, [&](int i) { return p.q_start[i] <= first_token; });
+    while (r + 1 < p.requests && p.q_start[r + 1] <= token) ++r;
+    const Request q = load_request(p, r);
+    const int i = token - q.start;
+    if (first + lane / kLanes >= rows || i < 0 || i >= q.todo || q.todo * p.group <= p.rows || d >= p.head_dim) return;
+    const long long at = (long long)head * rows + row, step = (long long)p.kv_heads * rows;
+    f32x4 part[kFewParts], y = {0.0f, 0.0f, 0.0f, 0.0f};
+    f32x2 stat[kFewParts];
+    float most = -INFINITY, weight = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kFewParts; ++k)
+        if (k < p.parts) {
+            stat[k] = p.stat[k * step + at];
+            part[k] = *reinterpret_cast<const f32x4 *>(p.part + (k * step + at) * DT + d);
+        }
+#pragma unroll
+    for (int k = 0; k < kFewParts; ++k)
+        if (k < p.parts) most = fmaxf(most, stat[k].x);
+    const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+    for (int k = 0; k < kFewParts; ++k)
+        if (k < p.parts) {
+            const float scale = exp2_fast(stat[k].x - base);
+            weight = fmaf(stat[k].y, scale, weight);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = fmaf(part[k][e], scale, y[e]);
+        }
+    int from, to;
+    visible_keys(p, q.n, q.len, i, from, to);
+    const float unit = 1.0f / weight;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = to > from ? y[e] * unit : 0.0f;
+    *reinterpret_cast<u32x2 *>(p.out + (long long)token * p.ld_out + (head * p.group + member) * p.head_dim + d) =
+        u32x2{from_float2<BF>(y[0], y[1]), from_float2<BF>(y[2], y[3])};
 }
 
 // Pieces that the keys of a tile are cut into: enough workgroups for two on every compute unit, none with fewer than four blocks of the longest row of pages.
@@ -374,27 +410,31 @@ int chunk_parts(int tokens, int group, int kv_heads, int dim, long long most_key
 }
 
 template <int DT, bool BF>
-static void chunks(const AttendParams &p, bool any, hipStream_t s)
+static void chunks(const AttendParams &p, bool any, bool passing, hipStream_t s)
 {
     const long long slots = (long long)p.tokens * p.group / kChunkRows + p.requests;
     const dim3 grid((unsigned)(slots * p.kv_heads), p.parts);
-    if (any) bcq_attend_chunk_kernel<DT, BF, true><<<grid, 64 * kWaves, 0, s>>>(p);
-    else bcq_attend_chunk_kernel<DT, BF, false><<<grid, 64 * kWaves, 0, s>>>(p);
-    if (p.parts > 1) bcq_attend_chunk_join_kernel<DT, BF><<<dim3(p.tokens * p.group, p.kv_heads), 64, 0, s>>>(p);
+    // (where a request has one tile, each byte of K and V is read once)
+    if (any) bcq_attend_chunk_kernel<DT, BF, true, false><<<grid, 64 * kWaves, 0, s>>>(p);
+    else if (passing && (long long)p.max_new * p.group <= kChunkRows) bcq_attend_chunk_kernel<DT, BF, false, true><<<grid, 64 * kWaves, 0, s>>>(p);
+    else bcq_attend_chunk_kernel<DT, BF, false, false><<<grid, 64 * kWaves, 0, s>>>(p);
+    const int rows = p.tokens * p.group;
+    if (p.parts > kFewParts) bcq_attend_chunk_join_kernel<DT, BF><<<dim3(rows, p.kv_heads), 64 * kWaves, 0, s>>>(p);
+    else if (p.parts > 1) bcq_attend_chunk_join_few_kernel<DT, BF><<<dim3((rows + 1024 / DT - 1) / (1024 / DT), p.kv_heads), 64 * kWaves, 0, s>>>(p);
 }
 
 template <bool BF>
-static void by_dim(const AttendParams &p, int dim, bool any, hipStream_t s)
+static void by_dim(const AttendParams &p, int dim, bool any, bool passing, hipStream_t s)
 {
-    if (dim == 64) chunks<64, BF>(p, any, s);
-    else if (dim == 128) chunks<128, BF>(p, any, s);
-    else chunks<256, BF>(p, any, s);
+    if (dim == 64) chunks<64, BF>(p, any, passing, s);
+    else if (dim == 128) chunks<128, BF>(p, any, passing, s);
+    else chunks<256, BF>(p, any, passing, s);
 }
 
-void launch_chunks(const AttendParams &p, int dim, bool any, bool bf16, hipStream_t s)
+void launch_chunks(const AttendParams &p, int dim, bool any, bool passing, bool bf16, hipStream_t s)
 {
-    if (bf16) by_dim<true>(p, dim, any, s);
-    else by_dim<false>(p, dim, any, s);
+    if (bf16) by_dim<true>(p, dim, any, passing, s);
+    else by_dim<false>(p, dim, any, passing, s);
 }
 
 }  // namespace bcq
