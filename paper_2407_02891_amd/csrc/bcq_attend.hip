@@ -24,12 +24,14 @@ constexpr int kBlock = 32;  // keys of a step
 constexpr int kWaves = 4;
 constexpr float kGrow = 8.0f;
 constexpr int kStreamRows = 16;
-constexpr int kDirectKeys = 1024;
 constexpr int kMostRows = 128;  // of a tile of either kernel
 constexpr long long kPassingBytes = 128ll << 20;  // half of what the last level holds
 
 // Waves per SIMD: what the registers allow.
 constexpr int stream_occupancy(int dim, bool any) { return dim == 64 ? 3 : dim == 128 ? 2 : 1; }
+
+// Waves of a workgroup that has a request and kv head to itself, where there are fewer of them than compute units: what LDS holds a block for.
+constexpr int most_waves(int dim) { return 1024 / dim; }
 
 // Blocks of a request in the line; a request whose rows see nothing has one, which writes its zeros.
 __device__ __forceinline__ int blocks_of(const AttendParams &p, const Request &q)
@@ -78,16 +80,19 @@ struct Segment {
 }  // namespace
 
 // DT: head_dim, or what it is padded to.  ANY: head_dim < DT, or pages of fewer than 16 slots.  PASSING: K and V leave nothing in the caches.
-// DIRECT: a workgroup has a request and kv head to itself, which its waves share and join.
-template <int DT, bool BF, bool ANY, bool PASSING, bool DIRECT>
-__global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_attend_stream_kernel(AttendParams p)
+// OWN: 0, or the waves of a workgroup that has a request and kv head to itself; they share its blocks and join their sums.
+template <int DT, bool BF, bool ANY, bool PASSING, int OWN>
+__global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4 : stream_occupancy(DT, ANY)) void bcq_attend_stream_kernel(
+    AttendParams p)
 {
+    constexpr bool DIRECT = OWN > 0;
+    constexpr int W = DIRECT ? OWN : kWaves;
     constexpr int C = DT / 32, DV = DT / 16;     // matrix steps over head_dim; tiles of O
     constexpr int kRowLanes = DT / 8, kRows = 64 / kRowLanes;  // a load covers kRows keys
-    __shared__ __attribute__((aligned(16))) uint16_t lds[kWaves][2 * kBlock * DT];
+    __shared__ __attribute__((aligned(16))) uint16_t lds[W][2 * kBlock * DT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4;
-    const int index = blockIdx.x * kWaves + wave;
+    const int index = blockIdx.x * W + wave;
     const int head = DIRECT ? blockIdx.x % p.kv_heads : index % p.kv_heads, worker = index / p.kv_heads;
     int first_head = head * p.group;  // (of q)
     if (ANY) asm("" : "+v"(first_head));
@@ -108,7 +113,7 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
         const Request own = load_request(p, r);
         total = blocks_of(p, own);
         if (total == 0) return;
-        at = total * wave / kWaves, stop = total * (wave + 1) / kWaves;
+        at = total * wave / W, stop = total * (wave + 1) / W;
         now = Segment{r, own.start, own.n, own.todo, own.len, (own.begin / kBlock + at) * kBlock, stop - at, false};
     } else {
         for (int c = 0; c < p.requests; c += 64) {
@@ -365,7 +370,7 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
     // ---- the waves' sums through LDS, each in its wave's own part; a row's are four banks from the next one's ----
     constexpr int kStep = DT + 4;
     static_assert(kStreamRows * kStep * sizeof(float) <= 2 * kBlock * DT * sizeof(uint16_t), "");
-    __shared__ f32x2 stat[DIRECT ? kWaves : 1][kStreamRows];
+    __shared__ f32x2 stat[DIRECT ? W : 1][kStreamRows];
     const auto sums = [&](int w) { return reinterpret_cast<float *>(lds[w]); };
     const float part_weight = sum_over_groups(sum);
 #pragma unroll
@@ -373,16 +378,16 @@ __global__ __launch_bounds__(64 * kWaves, stream_occupancy(DT, ANY)) void bcq_at
     if (g == 0) stat[wave][r16] = f32x2{most, part_weight};
     __syncthreads();
     const int rows = now.todo * p.group;
-    for (int i = threadIdx.x; i < rows * (DT / 4); i += 64 * kWaves) {
+    for (int i = threadIdx.x; i < rows * (DT / 4); i += 64 * W) {
         const int row = i / (DT / 4), d = 4 * (i % (DT / 4)), t = row / p.group;
         if (ANY && d >= p.head_dim) continue;
         float high = -INFINITY, all = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) high = fmaxf(high, stat[w][row].x);
+        for (int w = 0; w < W; ++w) high = fmaxf(high, stat[w][row].x);
         if (high == -INFINITY) high = 0.0f;
         f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
             const float scale = exp2_fast(stat[w][row].x - high);
             all = fmaf(stat[w][row].y, scale, all);
             y += *reinterpret_cast<const f32x4 *>(sums(w) + row * kStep + d) * scale;
@@ -460,6 +465,16 @@ namespace {
 
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
+// One launch, in which a workgroup has a (request, kv head) to itself, or the line and its join?  The line balances and fills the chip with few
+// requests, but costs a launch more and its waves look at all requests first.  Measured with all requests of a length, heads of 128, 8 kv heads,
+// own against line: 16 requests of 1000 keys 15.9 and 23.0 us, 1 of 1000 11.9 and 11.8, 1 of 2000 18.2 and 12.8; with four waves 64 requests of
+// 200 keys 13.0 and 22.7, of 2000 99 and 99, of 4000 189 and 181.
+bool one_launch(long long pairs, int dim, long long most_keys)
+{
+    if (pairs > 1 << 23) return false;  // (threads of a grid)
+    return most_keys <= (pairs < compute_units() ? 5 * kBlock * most_waves(dim) : 2048);
+}
+
 struct StreamPlan {
     int dim, workers;
     bool any;
@@ -478,19 +493,26 @@ StreamPlan stream_plan(const bcq_cache &c, int requests)
     return s;
 }
 
+template <int DT, bool BF, int OWN>
+void stream_own(const AttendParams &p, bool any, unsigned pairs, hipStream_t s)
+{
+    if (any) bcq_attend_stream_kernel<DT, BF, true, false, OWN><<<pairs, 64 * OWN, 0, s>>>(p);
+    else bcq_attend_stream_kernel<DT, BF, false, false, OWN><<<pairs, 64 * OWN, 0, s>>>(p);
+}
+
 template <int DT, bool BF>
 void stream_and_join(const AttendParams &p, bool any, bool passing, hipStream_t s)
 {
     if (p.workers == 0) {  // no line: a workgroup per request and kv head
-        const unsigned groups = (unsigned)p.requests * p.kv_heads;
-        if (any) bcq_attend_stream_kernel<DT, BF, true, false, true><<<groups, 64 * kWaves, 0, s>>>(p);
-        else bcq_attend_stream_kernel<DT, BF, false, false, true><<<groups, 64 * kWaves, 0, s>>>(p);
+        const unsigned pairs = (unsigned)p.requests * p.kv_heads;
+        if (pairs < (unsigned)compute_units()) stream_own<DT, BF, most_waves(DT)>(p, any, pairs, s);
+        else stream_own<DT, BF, kWaves>(p, any, pairs, s);
         return;
     }
     const int groups = (p.workers * p.kv_heads + kWaves - 1) / kWaves;
-    if (any) bcq_attend_stream_kernel<DT, BF, true, false, false><<<groups, 64 * kWaves, 0, s>>>(p);
-    else if (passing) bcq_attend_stream_kernel<DT, BF, false, true, false><<<groups, 64 * kWaves, 0, s>>>(p);
-    else bcq_attend_stream_kernel<DT, BF, false, false, false><<<groups, 64 * kWaves, 0, s>>>(p);
+    if (any) bcq_attend_stream_kernel<DT, BF, true, false, 0><<<groups, 64 * kWaves, 0, s>>>(p);
+    else if (passing) bcq_attend_stream_kernel<DT, BF, false, true, 0><<<groups, 64 * kWaves, 0, s>>>(p);
+    else bcq_attend_stream_kernel<DT, BF, false, false, 0><<<groups, 64 * kWaves, 0, s>>>(p);
     const long long most = (long long)p.max_new * p.group;
     const int rows = (int)(most < kStreamRows ? most : kStreamRows);
     AttendParams j = p;
@@ -558,7 +580,7 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t stream)
     // 66 MB: 24.5 us against 22).
     const bool passing = 4 * (long long)c.num_pages * c.page_stride >= kPassingBytes;
     if (which.stream) {
-        p.rows = kStreamRows, p.workers = most_keys <= kDirectKeys && (long long)a.requests * c.kv_heads <= 1 << 23 ? 0 : plan.workers;
+        p.rows = kStreamRows, p.workers = one_launch((long long)a.requests * c.kv_heads, plan.dim, most_keys) ? 0 : plan.workers;
         p.stat = reinterpret_cast<f32x2 *>(static_cast<char *>(a.workspace) + plan.part_bytes);
         if (c.dtype == BCQ_BF16) by_dim<true>(p, plan.dim, plan.any, passing, stream);
         else by_dim<false>(p, plan.dim, plan.any, passing, stream);
