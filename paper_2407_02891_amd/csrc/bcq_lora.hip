@@ -20,6 +20,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kFewTokens = 64;     // that every wave sorts out by itself
 constexpr int kManyTokens = 64;    // a tile where adapters have many
+constexpr long long kOneElements = 128 * 1024;  // of an adapter's A that every workgroup may read for itself
 constexpr int kPlanGroups = 4096;  // adapters (and none) whose tokens are counted in LDS
 
 struct LoraParams {
@@ -429,6 +430,110 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
     }
 }
 
+// ---- one token of a small adapter: one launch, in which every workgroup makes v for itself ----
+
+constexpr int kOneWaves = 8;
+
+// acc + the dot product of eight pairs, in binary32.
+template <bool BF>
+__device__ __forceinline__ float dot8(u32x4 a, u32x4 x, float acc)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 p = to_float2<BF>(a[i]), q = to_float2<BF>(x[i]);
+        acc = fmaf(p.y, q.y, fmaf(p.x, q.x, acc));
+    }
+    return acc;
+}
+
+// The sums over a wave's lanes of COUNT values each (a power of two up to 64): lane l gets that of value l / (64 / COUNT).
+template <int COUNT, int STEP = 32>
+__device__ __forceinline__ float sum_over_lanes(const float (&v)[COUNT], int lane)
+{
+    constexpr int kHalf = COUNT > 1 ? COUNT / 2 : 1;
+    float half[kHalf];
+    if (COUNT > 1) {
+        const bool upper = (lane & STEP) != 0;
+#pragma unroll
+        for (int i = 0; i < kHalf; ++i) {
+            const float low = v[i], high = v[COUNT > 1 ? i + kHalf : 0];
+            half[i] = (upper ? high : low) + __shfl_xor(upper ? low : high, STEP);
+        }
+    } else {
+        half[0] = v[0] + __shfl_xor(v[0], STEP);
+    }
+    if constexpr (STEP == 1) return half[0];
+    else return sum_over_lanes<kHalf, STEP / 2>(half, lane);
+}
+
+// A workgroup has p.row_groups * 512 rows of B, a row to a thread.  Each reads all of A, contiguously, 512 columns of sixteen rows a wave at a time.
+template <bool BF>
+__global__ __launch_bounds__(64 * kOneWaves) void bcq_lora_one_kernel(LoraParams p)
+{
+    __shared__ float sums[kOneWaves][16];
+    __shared__ __attribute__((aligned(16))) float v[BCQ_MAX_RANK];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int M = p.a.desc.M, N = p.a.desc.N, width = p.a.desc.max_rank;
+    const int adapter = adapter_of(p.a, 0), rank = rank_of(p.a, adapter);
+    if (rank == 0 && !p.copy) return;
+    const int first = blockIdx.x * p.row_groups * 64 * kOneWaves + threadIdx.x;
+    const uint16_t *const b = p.a.B + (long long)max(adapter, 0) * M * width;
+    // the first row of B, its first sixteen columns, and its base are on their way while v is made
+    u32x4 head[2] = {};
+    uint16_t base = p.a.base[min(first, M - 1)];
+    if (rank) {
+        const uint16_t *const row = b + (long long)min(first, M - 1) * width;
+        head[0] = *reinterpret_cast<const u32x4 *>(row), head[1] = *reinterpret_cast<const u32x4 *>(row + (width > 8 ? 8 : 0));
+        const char *const a = reinterpret_cast<const char *>(p.a.A + (long long)adapter * width * N);
+        const float scale = p.a.scale ? p.a.scale[adapter] : 1.0f;
+        for (int row0 = 0; row0 < rank; row0 += 16) {
+            float acc[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[j] = 0.0f;
+            for (int col = 512 * wave; col < N; col += 512 * kOneWaves) {
+                const int mine = col + 8 * lane;
+                u32x4 x = {0, 0, 0, 0}, rows[16];
+                if (mine < N) x = *reinterpret_cast<const u32x4 *>(p.a.X + mine);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    rows[j] = u32x4{0, 0, 0, 0};
+                    if (mine < N) rows[j] = *reinterpret_cast<const u32x4 *>(a + 2u * (unsigned)(min(row0 + j, rank - 1) * N + mine));
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[j] = dot8<BF>(rows[j], x, acc[j]);
+            }
+            const float mine = sum_over_lanes<16>(acc, lane);
+            if ((lane & 3) == 0) sums[wave][lane >> 2] = mine;
+            __syncthreads();
+            if (threadIdx.x < 16) {
+                float all = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kOneWaves; ++w) all += sums[w][threadIdx.x];
+                v[row0 + threadIdx.x] = all * scale;
+            }
+            __syncthreads();
+        }
+    }
+    for (int group = 0; group < p.row_groups; ++group) {
+        const int m = first + group * 64 * kOneWaves;
+        if (m >= M) break;
+        if (group) base = p.a.base[m];
+        const uint16_t *const row = b + (long long)m * width;
+        float acc = 0.0f;
+        for (int j = 0; j < rank; j += 8) {
+            const u32x4 eight = group == 0 && j < 16 ? (j ? head[1] : head[0]) : *reinterpret_cast<const u32x4 *>(row + j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x2 pair = to_float2<BF>(eight[i]);
+                // (columns behind the rank hold anything)
+                acc = fmaf(j + 2 * i < rank ? pair.x : 0.0f, j + 2 * i < rank ? v[j + 2 * i] : 0.0f, acc);
+                acc = fmaf(j + 2 * i + 1 < rank ? pair.y : 0.0f, j + 2 * i + 1 < rank ? v[j + 2 * i + 1] : 0.0f, acc);
+            }
+        }
+        p.a.Y[m] = rank ? from_float<BF>(to_float<BF>(base) + acc) : base;
+    }
+}
+
 // ---- many tokens: v is turned into operands once, and waves that share nothing but the caches go by the rows of B ----
 
 template <bool BF>
@@ -556,6 +661,7 @@ namespace {
 
 struct LoraPlan {
     bool few, many;     // at most kFewTokens; many tokens of few adapters
+    bool one;           // one token of a small adapter
     int slots;          // most tiles there can be
     int row_tiles, row_blocks;  // shrink: rows of A of a workgroup in sixteens, and how many such blocks
     int slices, row_groups;
@@ -587,6 +693,15 @@ LoraPlan lora_plan(const bcq_adapters &d, int tokens)
     const int blocks = (d.M + 64 * kWaves - 1) / (64 * kWaves);
     const long long resident = 4 * compute_units(), groups = ((long long)blocks * likely + resident - 1) / resident;
     s.row_groups = (int)(groups < 1 ? 1 : groups > 16 ? 16 : groups);
+    // (a launch less, but A from the caches for every 512 rows of B: rank 16, 4096 to 4096: 5.9 us against 7.8 with two launches, 8192 to 10240 7.1
+    // against 8.6; rank 32: 8.8 against 8.5, 11.0 against 9.4)
+    s.one = tokens == 1 && (long long)d.max_rank * d.N <= kOneElements;
+    if (s.one) {
+        const int rows = 64 * kOneWaves, all = (d.M + rows - 1) / rows, parts = compute_units() < all ? compute_units() : all;
+        s.row_groups = (all + parts - 1) / parts;
+        s.part_bytes = s.order_bytes = s.tile_bytes = s.cursor_bytes = s.operand_bytes = s.unit_bytes = 0;
+        return s;
+    }
     const bool bf = d.dtype == BCQ_BF16;
     s.part_bytes = whole((size_t)s.slices * tokens * d.max_rank * sizeof(float));
     s.order_bytes = s.few ? 0 : whole((size_t)s.slots * (s.many ? kManyTokens : 16) * sizeof(int));
@@ -635,6 +750,11 @@ void launch_many(LoraParams p, const LoraPlan &s, hipStream_t stream)
 template <bool BF>
 void by_plan(const LoraParams &p, const LoraPlan &s, hipStream_t stream)
 {
+    if (s.one) {
+        const int rows = 64 * kOneWaves * s.row_groups;
+        bcq_lora_one_kernel<BF><<<(p.a.desc.M + rows - 1) / rows, 64 * kOneWaves, 0, stream>>>(p);
+        return;
+    }
     if (s.few) return launch<BF, true>(p, s, stream);
     bcq_lora_plan_kernel<<<1, 1024, 0, stream>>>(p, s.many ? kManyTokens : 16);
     s.many ? launch_many<BF>(p, s, stream) : launch<BF, false>(p, s, stream);

@@ -373,6 +373,21 @@ def test_lora_many_tokens(dtype, T, N, M, C, width):
         assert torch.equal(base, got)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("N,M,width", [(8192, 1300, 16), (520, 513, 40), (4104, 5000, 24), (16, 140000, 8), (1032, 511, 120), (8, 1, 256), (16384, 700, 8), (20000, 64, 16)])
+def test_lora_one_token(dtype, N, M, width):
+    """Adapters of every rank, numbers of none, into another tensor and in place."""
+    X, A, Bm, scale, rank, _, base = _lora_case(1, N, M, 6, width, dtype, seed=N, ranks=[width, 1, width - 3, 0, min(9, width), width - 7])
+    adapters = bcq.Adapters(A, Bm, scale, rank)
+    for a in (0, 1, 2, 3, 4, 5, -1, 6):
+        adapter = _ints([a])
+        ref, bound = lora_ref(X, A, Bm, scale, rank, adapter, base)
+        assert_close(adapters.add(X, adapter, base), ref, bound, f"adapter {a}")
+        own = base.clone()
+        adapters.add(X, adapter, own, out=own)
+        assert_close(own, ref, bound, f"adapter {a} in place")
+
+
 def test_lora_very_many_adapters():
     """More adapters than the sorting launch counts in LDS."""
     X, A, Bm, scale, rank, adapter, base = _lora_case(900, 64, 40, 5000, 8, "f16", bare=True)
