@@ -557,8 +557,9 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_pack_kernel(LoraParams p
 // load costs four times a contiguous one, and there would be four times as many.  Rows of the next group and base of the next two are on
 // their way during this one.
 // ST: steps that the operands have at most.
+constexpr int many_occupancy(int steps) { return steps == 8 ? 2 : steps == 1 ? 5 : 4; }  // workgroups of a compute unit
 template <bool BF, int ST>
-__global__ __launch_bounds__(64 * kWaves, ST == 8 ? 2 : 3) void bcq_lora_many_kernel(LoraParams p)
+__global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many_kernel(LoraParams p)
 {
     constexpr int kParts = BF ? 2 : 1, kOwn = (64 * 2 * ST + 64 * kWaves - 1) / (64 * kWaves);  // 16-byte pieces of a group's rows that a thread brings
     __shared__ u32x4 rows_lds[2][64 * (2 * ST + 1)];
@@ -736,10 +737,13 @@ void launch_many(LoraParams p, const LoraPlan &s, hipStream_t stream)
     launch_shrink<BF, kManyTokens / 16, false>(p, s, stream);
     p.operand_pieces = (int)(operand_bytes(BF, (p.a.desc.max_rank + 15) / 16) / 16);
     bcq_lora_pack_kernel<BF><<<dim3(s.slots, kManyTokens / 16), 64 * kWaves, 0, stream>>>(p);
-    const int blocks = (p.a.desc.M + 63) / 64;
-    p.row_groups = blocks >= 64 ? 8 : 1 + blocks / 16;
+    const int blocks = (p.a.desc.M + 63) / 64, steps = steps_up_to(p.a.desc.max_rank);
+    // All workgroups at once, as the registers allow.  (4 adapters, 2048 tokens of rank 64, 7168 to 28672: ROUNDS.)
+    const int columns = compute_units() * many_occupancy(steps) / s.slots;
+    p.row_groups = columns > 0 ? (blocks + columns - 1) / columns : blocks;
+    if (p.row_groups > 32) p.row_groups = 32;
     const dim3 grid((blocks + p.row_groups - 1) / p.row_groups, s.slots);
-    switch (steps_up_to(p.a.desc.max_rank)) {
+    switch (steps) {
         case 1: bcq_lora_many_kernel<BF, 1><<<grid, 64 * kWaves, 0, stream>>>(p); break;
         case 2: bcq_lora_many_kernel<BF, 2><<<grid, 64 * kWaves, 0, stream>>>(p); break;
         case 4: bcq_lora_many_kernel<BF, 4><<<grid, 64 * kWaves, 0, stream>>>(p); break;
