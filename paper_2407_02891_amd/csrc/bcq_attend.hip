@@ -7,13 +7,18 @@
 //  * The blocks of 32 keys of all requests form one line, which is cut into as many equal pieces as there are waves for a kv head
 //    (from the lengths on the device: the host does not see them).  A wave walks its piece, over the ends of requests, and leaves for each
 //    request sums, maximum and weight (slot wave + request, which no two share); a request that one wave has to itself is finished there.
-//    A second launch joins the others.
+//    A second launch joins the others.  Short requests take one launch instead, in which a workgroup has a request and kv head (one_launch below).
+//  * K and V come from memory in whole rows (a load in the operand's layout touches sixteen rows for 64 bytes of each) and pass through LDS (the wave's own, no
+//    barrier): K's pieces are read as the operand's, V through the transposing read, which gives four keys of one element.
 //  * S^T = K Q^T: a lane gets four keys' scores of one row, and the same lane group's weights are the operand of O^T = V^T P^T as they
-//    are, because the keys of a product may be numbered in any order.  V passes through LDS (the wave's own, no barrier), whose transposing read
-//    gives four keys of one element.
-//  * The next block's K and V are requested when this one's have been used, and its page numbers a block earlier.
+//    are, because the keys of a product may be numbered in any order.
+//  * The next block's K and V are requested when this one's have gone to LDS, and its page numbers a block earlier: 16 KB a wave are on their way.
 //  * Weights are taken relative to a running maximum that is renewed only when a score passes it by 2^8, so O is hardly ever rescaled.
 //    They enter the second product as the sum of two 16-bit numbers (22 or 16 bits): it costs a matrix instruction more, and those wait for memory.
+//
+// Measured: 64 requests of 200 to 8000 keys, 64 / 8 heads of 128 (1.05 GB): 168 us and 8 for the join, 6.2 TB/s; with the loads alone, the arithmetic taken out, it
+// took no less, so what is left to the 7.2 TB/s of a plain read is the start (lengths, pages, the first keys: three reads in a row) and the end.
+// A first kernel without matrix instructions took 2278 us, K in the operand's layout and kept in the caches 201, one workgroup more than fits 24 us more.
 #include "bcq_attend.h"
 
 namespace bcq {

@@ -2,14 +2,21 @@
 //
 // Bound by the bytes: A and B of the adapters that occur, and with many tokens X, base and Y.  Tokens of the same adapter are taken together, 16 or 64
 // at a time (a tile), so that a piece of A or B is read once for them and the sums run on the matrix cores.  Up to 64 tokens every wave finds
-// its tile's tokens by comparing all adapter numbers at once; beyond, a small launch sorts the tokens by adapter first.  Two launches:
+// its tile's tokens by comparing all adapter numbers at once; beyond, a small launch sorts the tokens by adapter first (plan).  Then:
 //
-//  * v = A x: a workgroup has a tile, 16 to 64 rows of A and a slice of N; its waves share the slice and add up in LDS.  The slices, as many as fill
+//  * v = A x (shrink): a workgroup has a tile, 16 to 64 rows of A and a slice of N; its waves share the slice and add up in LDS.  The slices, as many as fill
 //    the chip, leave their sums in binary32 side by side, and whoever reads them adds them in order.
-//  * Y = base + B v: a workgroup has a tile and a range of rows of B.  v (times the scale) is held as a sum of 16-bit numbers beside the 16-bit rows of B:
+//  * Y = base + B v (expand): a workgroup has a tile and a range of rows of B.  v (times the scale) is held as a sum of 16-bit numbers beside the 16-bit rows of B:
 //    two for binary16 (after a power of two for each token: 22 bits and more of its largest value), three for bfloat16 (24 bits).  The operand's 32
 //    places are 16 of v's first numbers and the same 16 of its second ones.  The rows of B are numbered so that a lane ends up with eight
 //    neighbouring outputs of a token and four lanes with 32.
+//  * Many tokens of few adapters: v is turned into operands once (pack), and rows of B go through LDS for 64 tokens (many).
+//  * One token of a small adapter: one launch, each workgroup makes v for itself (one).
+//
+// Measured: rank 16, 8192 to 10240: one token 6.1 us (8.6 with shrink and expand), 64 tokens of 32 adapters 14 (shrink 6.4, expand 8: a launch and four reads
+// in a row each); 2048 tokens of 4 adapters of rank 64, 7168 to 28672, bfloat16: 101 us (plan 5, shrink 18, pack 6, many 75: 235 MB of base and Y at 3.1 TB/s,
+// the vector pipe 43 % busy, the caches' tags 47 %, the matrix pipe 20 %, and a barrier for every 64 rows keeps them apart).  First kernels without matrix
+// instructions took 19, 67 us and 11.8 ms.
 #include "bcq_half.h"
 #include "bcq_internal.h"
 
@@ -738,7 +745,7 @@ void launch_many(LoraParams p, const LoraPlan &s, hipStream_t stream)
     p.operand_pieces = (int)(operand_bytes(BF, (p.a.desc.max_rank + 15) / 16) / 16);
     bcq_lora_pack_kernel<BF><<<dim3(s.slots, kManyTokens / 16), 64 * kWaves, 0, stream>>>(p);
     const int blocks = (p.a.desc.M + 63) / 64, steps = steps_up_to(p.a.desc.max_rank);
-    // All workgroups at once, as the registers allow.  (4 adapters, 2048 tokens of rank 64, 7168 to 28672: ROUNDS.)
+    // All workgroups at once, as the registers allow.  (4 adapters, 2048 tokens of rank 64, 7168 to 28672: 101 us, 107 with eight groups of rows to each.)
     const int columns = compute_units() * many_occupancy(steps) / s.slots;
     p.row_groups = columns > 0 ? (blocks + columns - 1) / columns : blocks;
     if (p.row_groups > 32) p.row_groups = 32;

@@ -6,6 +6,9 @@
 // a head, and a wave has U rows of heads of one token: their loads are under way at once, and they share the cosines and sines, which depend on the place
 // in the head alone.  A head's sum of squares goes over its lanes by lane exchanges; the other half of a pair in the first half of the rotated
 // elements comes through the wave's own LDS, as it was loaded.
+//
+// Measured: 4096 tokens of 168 heads of 128, half of each rotated (353 MB): 78 us, 4.5 TB/s read and written (a copy of 2 GB: 4.7); one token of 80 heads 3.2 us, which
+// is a launch and two reads in a row.  A first kernel with a head to a workgroup took 282 and 13 us.
 #include "bcq_half.h"
 #include "bcq_internal.h"
 
