@@ -27,8 +27,12 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kFewTokens = 64;     // that every wave sorts out by itself
 constexpr int kManyTokens = 64;    // a tile where adapters have many
-constexpr long long kOneElements = 128 * 1024;  // of an adapter's A that every workgroup may read for itself
+constexpr long long kOneElements = 240 * 1024;  // of an adapter's A that every workgroup may read for itself
 constexpr int kPlanGroups = 4096;  // adapters (and none) whose tokens are counted in LDS
+
+// Sixteen bytes of base and Y, whose rows begin anywhere.  (785 tokens, 25 adapters of rank 17, 15248 to 25668, where rows are not whole pieces: 63 us, element by
+// element 147.)
+typedef u32x4 u32x4_even __attribute__((aligned(2)));
 
 struct LoraParams {
     LoraArgs a;
@@ -42,7 +46,6 @@ struct LoraParams {
     int slices;
     int row_groups;    // expand: groups of 64 rows of B of a wave
     bool copy;         // Y is not base
-    bool wide;         // base and Y in 16-byte pieces
 };
 
 __device__ __forceinline__ int adapter_of(const LoraArgs &a, int t)
@@ -225,7 +228,7 @@ __device__ __forceinline__ void shrink_products(const LoraArgs &p, int adapter, 
 // 8 g .. + 7 of each 32 of token r16.
 __device__ __forceinline__ int row_of(int r16, int q) { return 32 * (q >> 1) + 8 * (r16 >> 2) + 4 * (q & 1) + (r16 & 3); }
 
-// Y = base + unit * acc for a lane's outputs of a token.  `base` holds them already where `vector` (whole groups, 16-byte pieces); without an adapter
+// Y = base + unit * acc for a lane's outputs of a token.  `base` holds them already where `vector` (whole groups); without an adapter
 // they are the base bit for bit.
 template <bool BF>
 __device__ __forceinline__ void store_rows(const LoraArgs &p, int token, int row0, int lane, bool vector, bool adapted, float unit, const u32x4 (&loaded)[2],
@@ -246,7 +249,7 @@ __device__ __forceinline__ void store_rows(const LoraArgs &p, int token, int row
                     pairs[i] = from_float2<BF>(fmaf(a[2 * (i & 1)], unit, x.x), fmaf(a[2 * (i & 1) + 1], unit, x.y));
                 }
             }
-            *reinterpret_cast<u32x4 *>(y + m) = pairs;
+            *reinterpret_cast<u32x4_even *>(y + m) = pairs;
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -383,10 +386,10 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
             b[q] = p.a.B + ((long long)max(tile.adapter, 0) * M + min(row0 + row_of(r16, q), M - 1)) * width;
             if (steps) head[q] = *reinterpret_cast<const u32x4 *>(b[q] + widest);
         }
-        if (p.wide && row0 + 64 <= M) {
+        if (row0 + 64 <= M) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                out[h] = *reinterpret_cast<const u32x4 *>(p.a.base + (long long)members[r16] * p.a.ld_base + row0 + 32 * h + 8 * g);
+                out[h] = *reinterpret_cast<const u32x4_even *>(p.a.base + (long long)members[r16] * p.a.ld_base + row0 + 32 * h + 8 * g);
         }
     };
     request(first_row(0));
@@ -402,7 +405,7 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_expand_kernel(LoraParams
     for (int group = 0; group < p.row_groups; ++group) {
         const int row0 = first_row(group);
         if (row0 >= M) break;
-        const bool vector = p.wide && row0 + 64 <= M;
+        const bool vector = row0 + 64 <= M;
         f32x4 acc[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) acc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -616,9 +619,9 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
             if (from_row[i] < 64) to[from_row[i] * (pieces + 1) + from_piece[i]] = own[i];
     };
     const auto request = [&](int row0, u32x4 (&to)[2]) {
-        if (!p.wide || row0 + 64 > M) return;
+        if (row0 + 64 > M) return;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) to[h] = *reinterpret_cast<const u32x4 *>(p.a.base + (long long)token * p.a.ld_base + row0 + 32 * h + 8 * g);
+        for (int h = 0; h < 2; ++h) to[h] = *reinterpret_cast<const u32x4_even *>(p.a.base + (long long)token * p.a.ld_base + row0 + 32 * h + 8 * g);
     };
     int groups = p.row_groups;  // those that exist
     while (groups > 0 && first_row(groups - 1) >= M) --groups;
@@ -655,7 +658,7 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
         }
         if (group + 1 < groups) put(rows_lds[(group + 1) & 1]);
         if (group + 2 < groups) fetch(first_row(group + 2));
-        if (r16 < count) store_rows<BF>(p.a, token, row0, lane, p.wide && row0 + 64 <= M, steps != 0, unit, base, acc);
+        if (r16 < count) store_rows<BF>(p.a, token, row0, lane, row0 + 64 <= M, steps != 0, unit, base, acc);
         base[0] = next_base[0], base[1] = next_base[1];
         next_base[0] = later_base[0], next_base[1] = later_base[1];
         // (LDS alone: the stores need not have arrived)
@@ -701,8 +704,8 @@ LoraPlan lora_plan(const bcq_adapters &d, int tokens)
     const int blocks = (d.M + 64 * kWaves - 1) / (64 * kWaves);
     const long long resident = 4 * compute_units(), groups = ((long long)blocks * likely + resident - 1) / resident;
     s.row_groups = (int)(groups < 1 ? 1 : groups > 16 ? 16 : groups);
-    // (a launch less, but A from the caches for every 512 rows of B: rank 16, 4096 to 4096: 5.9 us against 7.8 with two launches, 8192 to 10240 7.1
-    // against 8.6; rank 32: 8.8 against 8.5, 11.0 against 9.4)
+    // (A launch less, but A from the caches for every 512 rows of B.  One launch against two: rank 16, 4096 to 4096 5.0 and 7.8 us, 8192 to 10240 6.1 and 8.6,
+    // 14336 to 7168 7.6 and 9.3; rank 32, 8192 to 10240 9.8 and 9.4; rank 16, 28672 to 7168 12.9 and 10.0.)
     s.one = tokens == 1 && (long long)d.max_rank * d.N <= kOneElements;
     if (s.one) {
         const int rows = 64 * kOneWaves, all = (d.M + rows - 1) / rows, parts = compute_units() < all ? compute_units() : all;
@@ -799,7 +802,6 @@ hipError_t launch_lora(const LoraArgs &a, hipStream_t stream)
     p.slices = s.slices;
     p.row_groups = s.row_groups;
     p.copy = a.Y != a.base;
-    p.wide = a.ld_base % 8 == 0 && a.ldy % 8 == 0 && ((reinterpret_cast<uintptr_t>(a.base) | reinterpret_cast<uintptr_t>(a.Y)) & 15) == 0;
     if (a.desc.dtype == BCQ_BF16) by_plan<true>(p, s, stream);
     else by_plan<false>(p, s, stream);
     return hipGetLastError();
