@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
     const auto find_pages = [&](int r, int len, int first_key) {
         if (ANY) return;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) id[t] = page_of(p, r, min(first_key + 16 * t, max(len - 1, 0) & ~15));
+        for (int t = 0; t < 2; ++t) id[t] = page_of_all(p, r, min(first_key + 16 * t, max(len - 1, 0) & ~15));
     };
     const auto request = [&](int r, int len, int first_key) {
         const int last = max(len - 1, 0);
@@ -558,7 +558,7 @@ size_t attend_workspace_bytes(const bcq_cache &c, int tokens, int requests, int 
     const StreamPlan s = stream_plan(c, requests);
     const size_t one = which.stream ? s.part_bytes + s.slots * sizeof(f32x2) : 0;
     if (!which.chunk) return one;
-    const int parts = chunk_parts(tokens, q_heads / c.kv_heads, c.kv_heads, s.dim, (long long)max_pages * c.page_size);
+    const int parts = chunk_parts(tokens, requests, max_new, q_heads / c.kv_heads, c.kv_heads, s.dim, (long long)max_pages * c.page_size);
     const size_t other = chunk_bytes(parts, tokens, q_heads, s.dim);
     return one > other ? one : other;  // one after the other
 }
@@ -592,7 +592,7 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t stream)
     }
     if (which.chunk) {
         p.rows = which.stream ? kStreamRows : 0;
-        p.parts = chunk_parts(a.tokens, p.group, c.kv_heads, plan.dim, most_keys);
+        p.parts = chunk_parts(a.tokens, a.requests, a.max_new, p.group, c.kv_heads, plan.dim, most_keys);  // (no more than the workspace is for)
         p.stat = reinterpret_cast<f32x2 *>(static_cast<char *>(a.workspace) + chunk_part_bytes(p.parts, a.tokens, a.q_heads, plan.dim));
         launch_chunks(p, plan.dim, plan.any, passing, c.dtype == BCQ_BF16, stream);
     }

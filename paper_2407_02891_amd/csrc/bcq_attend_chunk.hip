@@ -98,7 +98,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
 #pragma unroll
             for (int i = 0; i < kTransfers; ++i) id[i] = page_of(p, r, min(key0 + kOwn * wave + i * kRows + in_rows, last));
         } else {
-            id[0] = page_of(p, r, min(key0 + kOwn * wave, last));
+            id[0] = page_of_all(p, r, min(key0 + kOwn * wave, last));
         }
     };
     // the 16-element unit of a row of V that unit 0 is exchanged with: four keys' pairs of units, which are read together, fill all banks
@@ -162,6 +162,10 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
         asm volatile("" ::: "memory");
         if (more) request(key0 + KB, next_k, next_v);  // (every wave is through with the other buffers)
         const bool work = has_rows && key0 < any_to && key0 + KB > any_from;
+        if (DT == 256) {  // Q stays where the matrix instructions can read it and nothing else needs the place
+#pragma unroll
+            for (int c = 0; c < C; ++c) asm volatile("" : "+a"(qr[c]));
+        }
         // the operand V^T: elements 32 d + r32 of keys 16 u + 4 h .. and 16 u + 8 + 4 h ..
         const auto column = [&](int u, int d, int lane) {
             const int key = 16 * u + 4 * (lane >> 5) + ((lane & 15) >> 2), e = 32 * d + (lane & 16) + 4 * (lane & 3);
@@ -232,7 +236,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
             // (a few pieces of K ahead of their use: the compiler would wait for each)
-            constexpr int kAhead = 4, kSteps = KT * C;
+            constexpr int kAhead = 6, kSteps = KT * C;
             u32x4 a[kAhead];
 #pragma unroll
             for (int n = 0; n < kAhead; ++n) a[n] = *reinterpret_cast<const u32x4 *>(k_at(kb, 32 * (n / C) + r32, 16 * (n % C) + 8 * h));
@@ -261,6 +265,10 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
             if (__ballot(high > most + kGrow)) {
                 const auto other = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, high), __builtin_bit_cast(unsigned, high), false, false);
                 const float m = fmaxf(most, fmaxf(__builtin_bit_cast(float, (unsigned)other[0]), __builtin_bit_cast(float, (unsigned)other[1])));
+                if (DT == 256) {  // (or it copies O from the accumulation registers for every block, not here)
+#pragma unroll
+                    for (int d = 0; d < DV; ++d) asm volatile("" : "+a"(o[d]));
+                }
                 const float shrink = most == -INFINITY ? 1.0f : exp2_fast(most - m);
                 most = m;
                 base = m == -INFINITY ? 0.0f : m;
@@ -405,13 +413,26 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_attend_chunk_join_few_kernel(
         u32x2{from_float2<BF>(y[0], y[1]), from_float2<BF>(y[2], y[3])};
 }
 
-// Pieces that the keys of a tile are cut into: enough workgroups for two on every compute unit, none with fewer than four blocks of the longest row of pages.
-int chunk_parts(int tokens, int group, int kv_heads, int dim, long long most_keys)
+// Pieces that the keys of a tile are cut into, none with fewer than four blocks of the longest row of pages.  The least of what the rounds of workgroups take (2 us a
+// block, whatever the head) and of writing and joining the pieces' sums (6 TB/s), if that saves a tenth.  More keys never make it fewer pieces.
+// (2 requests of 512 tokens over 4096 keys, 16 / 8 heads of 256, 128 tiles: one piece 198 us, two 120; 4 of 300 to 600, window 1000, 32 / 8 heads of 128, 480 tiles: one
+// 58, two 78; 700 over 3000, 176 tiles: two 68, three 72, five 64.)
+int chunk_parts(int tokens, int requests, int max_new, int group, int kv_heads, int dim, long long most_keys)
 {
-    const long long tiles = ((long long)tokens * group / kChunkRows + 1) * kv_heads;
-    const long long wanted = (long long)compute_units() * chunk_occupancy(dim) / tiles, most = most_keys / (4 * chunk_keys(dim));
-    const long long parts = wanted < most ? wanted : most;
-    return (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    const long long rows = (long long)tokens * group;
+    // tiles: all of them where the requests are alike, else half a tile more for each request
+    const long long tiles = kv_heads * (tokens == (long long)requests * max_new ? requests * (((long long)max_new * group + kChunkRows - 1) / kChunkRows)
+                                                                               : rows / kChunkRows + (requests + 1) / 2);
+    const long long at_once = (long long)compute_units() * chunk_occupancy(dim), blocks = most_keys / chunk_keys(dim), most = blocks / 4 < 64 ? blocks / 4 : 64;
+    const double all = 2.0 * blocks, join = rows * kv_heads * dim * 8 / 6e6;
+    const auto rounds = [&](long long parts) { return (double)((tiles * parts + at_once - 1) / at_once) / parts; };
+    int parts = 1;
+    double least = 0.9 * all * rounds(1);
+    for (int n = 2; n <= most && 4.0 + n * join < least; ++n) {
+        const double time = all * rounds(n) + 4.0 + n * join;
+        if (time < least) least = time, parts = n;
+    }
+    return parts;
 }
 
 template <int DT, bool BF>
