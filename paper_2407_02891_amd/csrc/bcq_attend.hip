@@ -16,7 +16,7 @@
 //  * Weights are taken relative to a running maximum that is renewed only when a score passes it by 2^8, so O is hardly ever rescaled.
 //    They enter the second product as the sum of two 16-bit numbers (22 or 16 bits): it costs a matrix instruction more, and those wait for memory.
 //
-// Measured: 64 requests of 200 to 8000 keys, 64 / 8 heads of 128 (1.05 GB): 168 us and 8 for the join, 6.2 TB/s; with the loads alone, the arithmetic taken out, it
+// Measured: 64 requests of 200 to 8000 keys, 64 / 8 heads of 128 (1.05 GB): 166 us and 8 for the join, 6.3 TB/s; with the loads alone, the arithmetic taken out, it
 // took no less, so what is left to the 7.2 TB/s of a plain read is the start (lengths, pages, the first keys: three reads in a row) and the end.
 // A first kernel without matrix instructions took 2278 us, K in the operand's layout and kept in the caches 201, one workgroup more than fits 24 us more.
 #include "bcq_attend.h"

@@ -13,10 +13,10 @@
 //  * Maxima are renewed only when a score passes them by 2^8; blocks that all of a wave's rows see have no masks, those that none sees are left out.
 //  * Few tiles and many keys: the keys of a tile are cut into `parts`, whose sums a second launch joins.
 //
-// Measured: 2048 tokens over 8192 keys, 56 heads of 128, bfloat16: 450 us, 935 TFLOP/s, three quarters of what a large library product reaches; the matrix
+// Measured: 2048 tokens over 8192 keys, 56 heads of 128, bfloat16: 442 us, 952 TFLOP/s, three quarters of what a large library product reaches; the matrix
 // pipe is busy 52 % of the time and the vector pipe 39 %, no bank conflicts, two waves per SIMD as the registers allow (216 of 256).  Sorting the
-// exponentials of 32 keys among the matrix instructions of the others by hand took 487 us, a higher priority for a wave in its matrix instructions 455.
-// A first kernel without matrix instructions took 62 ms.  Five tokens over 131077 keys (537 MB): 90 us and 6 for the join, 6.0 TB/s.
+// exponentials of 32 keys among the matrix instructions of the others by hand took 487 us against 455, a higher priority for a wave in its matrix instructions 456.
+// A first kernel without matrix instructions took 62 ms.  Five tokens over 131077 keys (537 MB): 86 us and 6 for the join, 6.2 TB/s.
 #include "bcq_attend.h"
 
 namespace bcq {
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_attend_chunk_join_few_kernel(
 
 // Pieces that the keys of a tile are cut into, none with fewer than four blocks of the longest row of pages.  The least of what the rounds of workgroups take (2 us a
 // block, whatever the head) and of writing and joining the pieces' sums (6 TB/s), if that saves a tenth.  More keys never make it fewer pieces.
-// (2 requests of 512 tokens over 4096 keys, 16 / 8 heads of 256, 128 tiles: one piece 198 us, two 120; 4 of 300 to 600, window 1000, 32 / 8 heads of 128, 480 tiles: one
+// (2 requests of 512 tokens over 4096 keys, 16 / 8 heads of 256, 128 tiles: one piece 198 us, two 119; 4 of 300 to 600, window 1000, 32 / 8 heads of 128, 480 tiles: one
 // 58, two 78; 700 over 3000, 176 tiles: two 68, three 72, five 64.)
 int chunk_parts(int tokens, int requests, int max_new, int group, int kv_heads, int dim, long long most_keys)
 {
