@@ -14,8 +14,9 @@
 //  * One token of a small adapter: one launch, each workgroup makes v for itself (one).
 //
 // Measured: rank 16, 8192 to 10240: one token 6.1 us (8.6 with shrink and expand), 64 tokens of 32 adapters 14 (shrink 6.4, expand 8: a launch and four reads
-// in a row each); 2048 tokens of 4 adapters of rank 64, 7168 to 28672, bfloat16: 101 us (plan 5, shrink 18, pack 6, many 75: 235 MB of base and Y at 3.1 TB/s,
-// the vector pipe 43 % busy, the caches' tags 47 %, the matrix pipe 20 %, and a barrier for every 64 rows keeps them apart).  First kernels without matrix
+// in a row each); 2048 tokens of 4 adapters of rank 64, 7168 to 28672, bfloat16: 97 us (plan 5, shrink 18, pack 6, many 72: 235 MB of base and Y at 3.3 TB/s;
+// its loads and stores of 16 rows each cost 64 clocks of the address unit, a third of the time, matrix and vector pipes and LDS a fifth each, and a barrier for
+// every 64 rows keeps them apart).  First kernels without matrix
 // instructions took 19, 67 us and 11.8 ms.
 #include "bcq_half.h"
 #include "bcq_internal.h"
@@ -588,21 +589,11 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
 #pragma unroll
         for (int s = 0; s < ST; ++s)
             if (s < steps) v[part][s] = operands[(part * steps + s) * 64 + lane];
-    u32x4 kept_last;  // of the last step: the columns that belong to the adapter
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int j = 16 * (steps - 1) + 8 * (g & 1) + 2 * i;
-        kept_last[i] = (j < rank ? 0xffffu : 0u) | (j + 1 < rank ? 0xffff0000u : 0u);
-    }
-    // pieces of a row, and which of a group's this thread brings
+    // pieces of a row, and where the piece number threadIdx.x + 256 i of a group goes
     const int pieces = width >> 3;
-    int from_row[kOwn], from_piece[kOwn];
+    int place[kOwn];
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-        const int n = threadIdx.x + i * 64 * kWaves;
-        from_row[i] = n / pieces;
-        from_piece[i] = n - from_row[i] * pieces;
-    }
+    for (int i = 0; i < kOwn; ++i) place[i] = threadIdx.x + i * 64 * kWaves + (threadIdx.x + i * 64 * kWaves) / pieces;
     const uint16_t *const b = p.a.B + (long long)max(adapter, 0) * M * width;
     u32x4 own[kOwn], base[2], next_base[2], later_base[2];  // base two groups ahead: a load takes longer than a group
     const auto first_row = [&](int group) { return (int)(group * gridDim.x + blockIdx.x) * 64; };
@@ -610,13 +601,19 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
         if (steps == 0) return;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i)
-            if (from_row[i] < 64) own[i] = *reinterpret_cast<const u32x4 *>(b + (long long)min(row0 + from_row[i], M - 1) * width + 8 * from_piece[i]);
+            if (place[i] < 64 * (pieces + 1)) own[i] = *reinterpret_cast<const u32x4 *>(b + min((long long)row0 * width + 8 * (threadIdx.x + i * 64 * kWaves), (long long)M * width - 8));
     };
     const auto put = [&](u32x4 *to) {
         if (steps == 0) return;
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i)
-            if (from_row[i] < 64) to[from_row[i] * (pieces + 1) + from_piece[i]] = own[i];
+        for (int i = 0; i < kOwn; ++i) {
+            if (rank < width) {  // columns behind the rank hold anything
+                const int first = 8 * (place[i] % (pieces + 1));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) own[i][e] &= (first + 2 * e < rank ? 0xffffu : 0u) | (first + 2 * e + 1 < rank ? 0xffff0000u : 0u);
+            }
+            if (place[i] < 64 * (pieces + 1)) to[place[i]] = own[i];
+        }
     };
     const auto request = [&](int row0, u32x4 (&to)[2]) {
         if (row0 + 64 > M) return;
@@ -626,6 +623,7 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
     int groups = p.row_groups;  // those that exist
     while (groups > 0 && first_row(groups - 1) >= M) --groups;
     if (groups == 0) return;
+    if (threadIdx.x < 128) rows_lds[threadIdx.x >> 6][(threadIdx.x & 63) * (pieces + 1) + pieces] = u32x4{0, 0, 0, 0};  // (a row may end in the first eight of a sixteen)
     fetch(first_row(0));
     request(first_row(0), base);
     if (groups > 1) request(first_row(1), next_base);
@@ -643,13 +641,9 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
 #pragma unroll
             for (int s = 0; s < ST; ++s) {
                 if (s >= steps) break;
-                const int piece = min(2 * s + (g & 1), pieces - 1);  // (a row may end in the first eight of a sixteen: the second are masked)
                 u32x4 rows[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    rows[q] = at[row_of(r16, q) * (pieces + 1) + piece];
-                    if (s == steps - 1) rows[q] &= kept_last;
-                }
+                for (int q = 0; q < 4; ++q) rows[q] = at[row_of(r16, q) * (pieces + 1) + 2 * s + (g & 1)];
 #pragma unroll
                 for (int part = 0; part < kParts; ++part)
 #pragma unroll
