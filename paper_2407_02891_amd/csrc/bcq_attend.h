@@ -85,7 +85,7 @@ static __device__ __attribute__((aligned(16))) const uint16_t g_zeros[8] = {};
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Joining the pieces of a row: piece i has its sums in part and its (maximum, weight) in stat at first + i * step.
+// Joining the pieces of a row: piece i has its sums in part and its (maximum, weight) in stat at at(i).
 struct Slots {
     long long first, step;
     __device__ __forceinline__ long long operator()(int i) const { return first + i * step; }
@@ -93,8 +93,8 @@ struct Slots {
 constexpr int kJoinAhead = 8;  // pieces requested together
 
 // y, weight: sums over the pieces from + share, from + share + STRIDE, .. < end, relative to the maximum over all pieces from .. end - 1.
-template <int DT, int STRIDE>
-__device__ __forceinline__ void join_pieces(const AttendParams &p, Slots at, int from, int end, int share, int lane, float (&y)[DT / 64], float &weight)
+template <int DT, int STRIDE, class At>
+__device__ __forceinline__ void join_pieces(const AttendParams &p, const At &at, int from, int end, int share, int lane, float (&y)[DT / 64], float &weight)
 {
     constexpr int E = DT / 64;  // elements of a lane
     float most = -INFINITY;

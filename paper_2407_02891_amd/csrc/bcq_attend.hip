@@ -6,7 +6,8 @@
 // instruction, so a key is read once for all of them.
 //  * The blocks of 32 keys of all requests form one line, which is cut into as many equal pieces as there are waves for a kv head
 //    (from the lengths on the device: the host does not see them).  A wave walks its piece, over the ends of requests, and leaves for each
-//    request sums, maximum and weight (slot wave + request, which no two share); a request that one wave has to itself is finished there.
+//    request sums, maximum and weight (slot wave + request, which no two share); a request that one wave has to itself is finished there, and
+//    what a workgroup's waves have of one request is one piece (one request of 32768 keys: 39.7 us, 34 with them).
 //    A second launch joins the others.  Short requests take one launch instead, in which a workgroup has a request and kv head (one_launch below).
 //  * K and V come from memory in whole rows (a load in the operand's layout touches sixteen rows for 64 bytes of each) and pass through LDS (the wave's own, no
 //    barrier): K's pieces are read as the operand's, V through the transposing read, which gives four keys of one element.
@@ -80,6 +81,7 @@ struct Segment {
     int r, start, n, todo, len;
     int key, blocks;   // first key (of a block), blocks
     bool whole;        // all of the request
+    int from, upto;    // the request's blocks in the line
 };
 
 }  // namespace
@@ -97,8 +99,7 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
     __shared__ __attribute__((aligned(16))) uint16_t lds[W][2 * kBlock * DT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, g = lane >> 4;
-    const int index = blockIdx.x * W + wave;
-    const int head = DIRECT ? blockIdx.x % p.kv_heads : index % p.kv_heads, worker = index / p.kv_heads;
+    const int head = blockIdx.x % p.kv_heads, first_worker = blockIdx.x / p.kv_heads * W, worker = first_worker + wave;
     int first_head = head * p.group;  // (of q)
     if (ANY) asm("" : "+v"(first_head));
     uint16_t *const ks = lds[wave], *const vs = ks + kBlock * DT;
@@ -112,20 +113,20 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
     // ---- this wave's piece of the line, or of the request ----
     Window w;
     Segment now;
-    int total = 0, first = 0, at, stop;
+    int total = 0, first = 0, workers = 0, at, stop;
     if (DIRECT) {
         const int r = blockIdx.x / p.kv_heads;
         const Request own = load_request(p, r);
         total = blocks_of(p, own);
         if (total == 0) return;
         at = total * wave / W, stop = total * (wave + 1) / W;
-        now = Segment{r, own.start, own.n, own.todo, own.len, (own.begin / kBlock + at) * kBlock, stop - at, false};
+        now = Segment{r, own.start, own.n, own.todo, own.len, (own.begin / kBlock + at) * kBlock, stop - at, false, 0, 0};
     } else {
         for (int c = 0; c < p.requests; c += 64) {
             w.load(p, c, total, lane);
             total = lane_of(w.upto, 63);
         }
-        const int workers = workers_of(p, total);
+        workers = workers_of(p, total);
         if (worker >= workers || total == 0) return;
         at = first_block(worker, workers, total);
         stop = first_block(worker + 1, workers, total);
@@ -144,6 +145,8 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
         e.key = (lane_of(w.q.begin, l) / kBlock + place - from) * kBlock;
         e.blocks = min(upto, stop) - place;
         e.whole = from == place && upto <= stop;
+        e.from = from;
+        e.upto = upto;
         return e;
     };
 
@@ -196,6 +199,9 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
 
     if (!DIRECT) now = segment_at(at);
     const bool any_block = !DIRECT || now.blocks > 0;
+    // All of the workgroup's pieces are of one request (each of its waves finds the same): their sums are joined here, and left as its first wave's.
+    const bool joint = DIRECT || (first_worker + W <= workers && first_block(first_worker, workers, total) >= now.from &&
+                                  first_block(first_worker + W, workers, total) <= now.upto);
     if (any_block) {
         find_pages(now.r, now.len, now.key);
         request(now.r, now.len, now.key);
@@ -346,7 +352,7 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
         }
         asm volatile("" ::: "memory");
         if (now.blocks) continue;
-        if (DIRECT) break;
+        if (joint) break;
         const float weight = sum_over_groups(sum), unit = 1.0f / weight;
         if (token < now.todo) {
             if (now.whole) {
@@ -360,7 +366,7 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
                         *reinterpret_cast<u32x2 *>(dst + 16 * d + 4 * g) = u32x2{from_float2<BF>(y[0], y[1]), from_float2<BF>(y[2], y[3])};
                     }
             } else {
-                const long long slot = ((long long)now.r * p.kv_heads + index) * kStreamRows + r16;  // (index: worker * kv_heads + head)
+                const long long slot = ((long long)(now.r + worker) * p.kv_heads + head) * kStreamRows + r16;
 #pragma unroll
                 for (int d = 0; d < DV; ++d) *reinterpret_cast<f32x4 *>(p.part + slot * DT + 16 * d + 4 * g) = o[d];
                 if (g == 0) p.stat[slot] = f32x2{most, weight};
@@ -370,12 +376,12 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
         now = next;
         begin_request(now);
     }
-    if (!DIRECT) return;
+    if (!joint) return;
 
     // ---- the waves' sums through LDS, each in its wave's own part; a row's are four banks from the next one's ----
     constexpr int kStep = DT + 4;
     static_assert(kStreamRows * kStep * sizeof(float) <= 2 * kBlock * DT * sizeof(uint16_t), "");
-    __shared__ f32x2 stat[DIRECT ? W : 1][kStreamRows];
+    __shared__ f32x2 stat[W][kStreamRows];
     const auto sums = [&](int w) { return reinterpret_cast<float *>(lds[w]); };
     const float part_weight = sum_over_groups(sum);
 #pragma unroll
@@ -385,17 +391,23 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
     const int rows = now.todo * p.group;
     for (int i = threadIdx.x; i < rows * (DT / 4); i += 64 * W) {
         const int row = i / (DT / 4), d = 4 * (i % (DT / 4)), t = row / p.group;
-        if (ANY && d >= p.head_dim) continue;
-        float high = -INFINITY, all = 0.0f;
+        if (ANY && DIRECT && d >= p.head_dim) continue;
+        float top = -INFINITY, all = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) high = fmaxf(high, stat[w][row].x);
-        if (high == -INFINITY) high = 0.0f;
+        for (int w = 0; w < W; ++w) top = fmaxf(top, stat[w][row].x);
+        const float high = top == -INFINITY ? 0.0f : top;
         f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             const float scale = exp2_fast(stat[w][row].x - high);
             all = fmaf(stat[w][row].y, scale, all);
             y += *reinterpret_cast<const f32x4 *>(sums(w) + row * kStep + d) * scale;
+        }
+        if (!DIRECT) {
+            const long long slot = ((long long)(now.r + first_worker) * p.kv_heads + head) * kStreamRows + row;
+            *reinterpret_cast<f32x4 *>(p.part + slot * DT + d) = y;
+            if (d == 0) p.stat[slot] = f32x2{top, all};
+            continue;
         }
         y *= 1.0f / all;
         visible_keys(p, now.n, now.len, t, from, to);
@@ -427,7 +439,16 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_attend_join_kernel(AttendPara
     const int workers = workers_of(p, total);
     const int w0 = worker_of(upto - own, workers, total), w1 = worker_of(upto - 1, workers, total);
     if (w0 == w1) return;  // finished by its one wave
-    const auto slots = [&](int row) { return Slots{((long long)r * p.kv_heads + head) * kStreamRows + row, (long long)p.kv_heads * kStreamRows}; };
+    // pieces: of single waves, of whole workgroups, of single waves
+    const int g0 = (w0 + kWaves - 1) / kWaves + (w0 % kWaves == 0 && first_block(w0, workers, total) < upto - own ? 1 : 0);
+    const int g1 = (w1 + 1) % kWaves == 0 && first_block(w1 + 1, workers, total) == upto ? (w1 + 1) / kWaves : w1 / kWaves;
+    const int groups = max(g1 - g0, 0), lead = groups ? kWaves * g0 - w0 : w1 - w0 + 1, pieces = lead + groups + (groups ? w1 + 1 - kWaves * g1 : 0);
+    const auto slots = [&](int row) {
+        return [=](int i) {
+            const int w = i < lead ? w0 + i : i < lead + groups ? kWaves * (g0 + i - lead) : kWaves * g1 + i - lead - groups;
+            return ((long long)(w + r) * p.kv_heads + head) * kStreamRows + row;
+        };
+    };
     const auto finish = [&](int row, const float (&y)[E], float weight) {
         int from, to;
         visible_keys(p, q.n, q.len, row / p.group, from, to);
@@ -437,15 +458,15 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_attend_join_kernel(AttendPara
             if (lane * E + e < p.head_dim) dst[lane * E + e] = from_float<BF>(to > from ? y[e] / weight : 0.0f);
     };
     float y[E], weight;
-    if (p.join_rows == kWaves && w1 - w0 < 2 * kJoinAhead) {
+    if (p.join_rows == kWaves && pieces <= 2 * kJoinAhead) {
         if (wave >= rows) return;
         const int row = first_row + wave;
-        join_pieces<DT, 1>(p, slots(row), w0, w1 + 1, 0, lane, y, weight);
+        join_pieces<DT, 1>(p, slots(row), 0, pieces, 0, lane, y, weight);
         finish(row, y, weight);
         return;
     }
     for (int row = first_row; row < first_row + rows; ++row) {
-        join_pieces<DT, kWaves>(p, slots(row), w0, w1 + 1, wave, lane, y, weight);
+        join_pieces<DT, kWaves>(p, slots(row), 0, pieces, wave, lane, y, weight);
 #pragma unroll
         for (int e = 0; e < E; ++e) shared[wave][lane * E + e] = y[e];
         if (lane == 0) shared[wave][DT] = weight;
@@ -491,8 +512,8 @@ StreamPlan stream_plan(const bcq_cache &c, int requests)
     s.dim = padded_dim(c.head_dim);
     s.any = c.head_dim != s.dim || c.page_size < 16;
     // As many waves as the chip holds: one workgroup more would start when the others end.
-    s.workers = compute_units() * kWaves * stream_occupancy(s.dim, s.any) / c.kv_heads;
-    if (s.workers < 1) s.workers = 1;
+    const int groups = compute_units() * stream_occupancy(s.dim, s.any) / c.kv_heads;
+    s.workers = kWaves * (groups > 1 ? groups : 1);
     s.slots = (size_t)(s.workers + requests) * c.kv_heads * kStreamRows;
     s.part_bytes = s.slots * s.dim * sizeof(float);
     return s;
@@ -514,7 +535,7 @@ void stream_and_join(const AttendParams &p, bool any, bool passing, hipStream_t 
         else stream_own<DT, BF, kWaves>(p, any, pairs, s);
         return;
     }
-    const int groups = (p.workers * p.kv_heads + kWaves - 1) / kWaves;
+    const int groups = (p.workers + kWaves - 1) / kWaves * p.kv_heads;
     if (any) bcq_attend_stream_kernel<DT, BF, true, false, 0><<<groups, 64 * kWaves, 0, s>>>(p);
     else if (passing) bcq_attend_stream_kernel<DT, BF, false, true, 0><<<groups, 64 * kWaves, 0, s>>>(p);
     else bcq_attend_stream_kernel<DT, BF, false, false, 0><<<groups, 64 * kWaves, 0, s>>>(p);
