@@ -7,7 +7,7 @@
 //  * The blocks of 32 keys of all requests form one line, which is cut into as many equal pieces as there are waves for a kv head
 //    (from the lengths on the device: the host does not see them).  A wave walks its piece, over the ends of requests, and leaves for each
 //    request sums, maximum and weight (slot wave + request, which no two share); a request that one wave has to itself is finished there, and
-//    what a workgroup's waves have of one request is one piece (one request of 32768 keys: 39.7 us, 34 with them).
+//    what a workgroup's waves have of one request is one piece (one request of 32768 keys: 30.5 us, 39.7 if every wave leaves its own).
 //    A second launch joins the others.  Short requests take one launch instead, in which a workgroup has a request and kv head (one_launch below).
 //  * K and V come from memory in whole rows (a load in the operand's layout touches sixteen rows for 64 bytes of each) and pass through LDS (the wave's own, no
 //    barrier): K's pieces are read as the operand's, V through the transposing read, which gives four keys of one element.
@@ -17,7 +17,7 @@
 //  * Weights are taken relative to a running maximum that is renewed only when a score passes it by 2^8, so O is hardly ever rescaled.
 //    They enter the second product as the sum of two 16-bit numbers (22 or 16 bits): it costs a matrix instruction more, and those wait for memory.
 //
-// Measured: 64 requests of 200 to 8000 keys, 64 / 8 heads of 128 (1.05 GB): 166 us and 8 for the join, 6.3 TB/s; with the loads alone, the arithmetic taken out, it
+// Measured: 64 requests of 200 to 8000 keys, 64 / 8 heads of 128 (1.05 GB): 165 us and 8 for the join, 6.3 TB/s; with the loads alone, the arithmetic taken out, it
 // took no less, so what is left to the 7.2 TB/s of a plain read is the start (lengths, pages, the first keys: three reads in a row) and the end.
 // A first kernel without matrix instructions took 2278 us, K in the operand's layout and kept in the caches 201, one workgroup more than fits 24 us more.
 #include "bcq_attend.h"
@@ -493,12 +493,12 @@ int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 12
 
 // One launch, in which a workgroup has a (request, kv head) to itself, or the line and its join?  The line balances and fills the chip with few
 // requests, but costs a launch more and its waves look at all requests first.  Measured with all requests of a length, heads of 128, 8 kv heads,
-// own against line: 16 requests of 1000 keys 15.9 and 23.0 us, 1 of 1000 11.9 and 11.8, 1 of 2000 18.2 and 12.8; with four waves 64 requests of
-// 200 keys 13.0 and 22.7, of 2000 99 and 99, of 4000 189 and 181.
+// own against line: 16 requests of 1000 keys 16.2 and 23.2 us, 1 of 1000 11.8 and 11.5, 4 of 2000 (without the rule) 20.4 and 17; with four waves 64 requests of
+// 200 keys 13.2 and 21.3, of 1000 51 and 53, of 2000 96 and 93.
 bool one_launch(long long pairs, int dim, long long most_keys)
 {
     if (pairs > 1 << 23) return false;  // (threads of a grid)
-    return most_keys <= (pairs < compute_units() ? 5 * kBlock * most_waves(dim) : 2048);
+    return most_keys <= (pairs < compute_units() ? 5 * kBlock * most_waves(dim) : 1536);
 }
 
 struct StreamPlan {

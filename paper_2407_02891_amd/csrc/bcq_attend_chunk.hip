@@ -13,7 +13,7 @@
 //  * Maxima are renewed only when a score passes them by 2^8; blocks that all of a wave's rows see have no masks, those that none sees are left out.
 //  * Few tiles and many keys: the keys of a tile are cut into `parts`, whose sums a second launch joins.
 //
-// Measured: 2048 tokens over 8192 keys, 56 heads of 128, bfloat16: 442 us, 952 TFLOP/s, three quarters of what a large library product reaches; the matrix
+// Measured: 2048 tokens over 8192 keys, 56 heads of 128, bfloat16: 440 us, 957 TFLOP/s, three quarters of what a large library product reaches; the matrix
 // pipe is busy 52 % of the time and the vector pipe 39 %, no bank conflicts, two waves per SIMD as the registers allow (216 of 256).  Sorting the
 // exponentials of 32 keys among the matrix instructions of the others by hand took 487 us against 455, a higher priority for a wave in its matrix instructions 456.
 // A first kernel without matrix instructions took 62 ms.  Five tokens over 131077 keys (537 MB): 86 us and 6 for the join, 6.2 TB/s.

@@ -14,7 +14,7 @@
 //  * One token of a small adapter: one launch, each workgroup makes v for itself (one).
 //
 // Measured: rank 16, 8192 to 10240: one token 6.1 us (8.6 with shrink and expand), 64 tokens of 32 adapters 14 (shrink 6.4, expand 8: a launch and four reads
-// in a row each); 2048 tokens of 4 adapters of rank 64, 7168 to 28672, bfloat16: 97 us (plan 5, shrink 18, pack 6, many 72: 235 MB of base and Y at 3.3 TB/s;
+// in a row each); 2048 tokens of 4 adapters of rank 64, 7168 to 28672, bfloat16: 98 us (plan 5, shrink 17, pack 5, many 70: 235 MB of base and Y at 3.4 TB/s;
 // its loads and stores of 16 rows each cost 64 clocks of the address unit, a third of the time, matrix and vector pipes and LDS a fifth each, and a barrier for
 // every 64 rows keeps them apart).  First kernels without matrix
 // instructions took 19, 67 us and 11.8 ms.
