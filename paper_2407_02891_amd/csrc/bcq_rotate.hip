@@ -7,7 +7,7 @@
 // in the head alone.  A head's sum of squares goes over its lanes by lane exchanges; the other half of a pair in the first half of the rotated
 // elements comes through the wave's own LDS, as it was loaded.
 //
-// Measured: 4096 tokens of 168 heads of 128, half of each rotated (353 MB): 78 us, 4.5 TB/s read and written (a copy of 2 GB: 4.7); one token of 80 heads 3.2 us, which
+// Measured: 4096 tokens of 168 heads of 128, half of each rotated (353 MB): 76 us, 4.6 TB/s read and written (a copy of 2 GB: 4.7); one token of 80 heads 3.2 us, which
 // is a launch and two reads in a row.  A first kernel with a head to a workgroup took 282 and 13 us.
 #include "bcq_half.h"
 #include "bcq_internal.h"
@@ -184,13 +184,15 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_rotate_kernel(RotateArgs p, i
             for (int e = 0; e < 8; e += 2) out[e / 2] = from_float2<BF>(y[e], y[e + 1]);
         }
         if (!in_head || head >= heads) continue;
+        // (whole lines, which no one reads before this kernel has ended: kept out of the caches' way, 4096 tokens of 80 heads take 38.7 us instead of 47.1, of 168 heads 76
+        // instead of 84, 512 of 80 9.2 instead of 10.1, few the same)
         if (is_q) {
-            *reinterpret_cast<u32x4 *>(p.q_out + (long long)t * p.ld_q + (long long)head * D + d) = out;
+            __builtin_nontemporal_store(out, reinterpret_cast<u32x4 *>(p.q_out + (long long)t * p.ld_q + (long long)head * D + d));
         } else if (slot >= 0 && slot < p.cache.num_pages * p.cache.page_size) {
             const int shift = __builtin_ctz(p.cache.page_size);
             const long long at = (long long)(slot >> shift) * p.cache.page_stride + (long long)(slot & (p.cache.page_size - 1)) * p.cache.slot_stride;
-            if (is_v) *reinterpret_cast<u32x4 *>(p.v + at + (long long)(head - qh - kvh) * p.cache.head_stride + d) = out;
-            else *reinterpret_cast<u32x4 *>(p.k + at + (long long)(head - qh) * p.cache.head_stride + d) = out;
+            if (is_v) __builtin_nontemporal_store(out, reinterpret_cast<u32x4 *>(p.v + at + (long long)(head - qh - kvh) * p.cache.head_stride + d));
+            else __builtin_nontemporal_store(out, reinterpret_cast<u32x4 *>(p.k + at + (long long)(head - qh) * p.cache.head_stride + d));
         }
     }
 }
