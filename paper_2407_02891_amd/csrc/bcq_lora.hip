@@ -229,33 +229,40 @@ __device__ __forceinline__ void shrink_products(const LoraArgs &p, int adapter, 
 // 8 g .. + 7 of each 32 of token r16.
 __device__ __forceinline__ int row_of(int r16, int q) { return 32 * (q >> 1) + 8 * (r16 >> 2) + 4 * (q & 1) + (r16 & 3); }
 
-// Y = base + unit * acc for a lane's outputs of a token.  `base` holds them already where `vector` (whole groups); without an adapter
-// they are the base bit for bit.
 template <bool BF>
-__device__ __forceinline__ void store_rows(const LoraArgs &p, int token, int row0, int lane, bool vector, bool adapted, float unit, const u32x4 (&loaded)[2],
-                                           const f32x4 (&acc)[4])
+__device__ __forceinline__ u32x4 add_pairs(u32x4 base, f32x4 low, f32x4 high, float unit)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 x = to_float2<BF>(base[i]);
+        const f32x4 a = i < 2 ? low : high;
+        base[i] = from_float2<BF>(fmaf(a[2 * (i & 1)], unit, x.x), fmaf(a[2 * (i & 1) + 1], unit, x.y));
+    }
+    return base;
+}
+
+// Y = base + unit * (low, high) for eight outputs of a token from m on, as far as there are so many; without an adapter they are the base bit for bit.
+template <bool BF>
+__device__ __forceinline__ void store_ends(const LoraArgs &p, int token, int m, bool adapted, float unit, f32x4 low, f32x4 high)
 {
     const uint16_t *const base = p.base + (long long)token * p.ld_base;
     uint16_t *const y = p.Y + (long long)token * p.ldy;
 #pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (m + i < p.desc.M) y[m + i] = adapted ? from_float<BF>(fmaf(i < 4 ? low[i & 3] : high[i & 3], unit, to_float<BF>(base[m + i]))) : base[m + i];
+}
+
+// All of a lane's outputs of a token, in the order that the products leave: 8 g .. + 7 of each 32.  `loaded` holds the base where all 64 exist (whole).
+template <bool BF>
+__device__ __forceinline__ void store_rows(const LoraArgs &p, int token, int row0, int lane, bool whole, bool adapted, float unit, const u32x4 (&loaded)[2],
+                                           const f32x4 (&acc)[4])
+{
+    uint16_t *const y = p.Y + (long long)token * p.ldy;
+#pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int m = row0 + 32 * h + 8 * (lane >> 4);
-        if (vector) {
-            u32x4 pairs = loaded[h];
-            if (adapted) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f32x2 x = to_float2<BF>(pairs[i]);
-                    const f32x4 a = acc[2 * h + (i >> 1)];
-                    pairs[i] = from_float2<BF>(fmaf(a[2 * (i & 1)], unit, x.x), fmaf(a[2 * (i & 1) + 1], unit, x.y));
-                }
-            }
-            *reinterpret_cast<u32x4_even *>(y + m) = pairs;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (m + i < p.desc.M) y[m + i] = adapted ? from_float<BF>(fmaf(acc[2 * h + (i >> 2)][i & 3], unit, to_float<BF>(base[m + i]))) : base[m + i];
-        }
+        if (whole) *reinterpret_cast<u32x4_even *>(y + m) = adapted ? add_pairs<BF>(loaded[h], acc[2 * h], acc[2 * h + 1], unit) : loaded[h];
+        else store_ends<BF>(p, token, m, adapted, unit, acc[2 * h], acc[2 * h + 1]);
     }
 }
 
@@ -568,7 +575,7 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_pack_kernel(LoraParams p
 // load costs four times a contiguous one, and there would be four times as many.  Rows of the next group and base of the next two are on
 // their way during this one.
 // ST: steps that the operands have at most.
-constexpr int many_occupancy(int steps) { return steps == 8 ? 2 : steps == 1 ? 5 : 4; }  // workgroups of a compute unit
+constexpr int many_occupancy(int steps) { return steps == 8 ? 2 : steps == 1 ? 6 : 4; }  // workgroups of a compute unit: what the registers allow
 template <bool BF, int ST>
 __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many_kernel(LoraParams p)
 {
@@ -580,7 +587,26 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
     const int adapter = p.tiles[2 + 2 * slot], count = p.tiles[3 + 2 * slot] - 16 * wave;
     const int rank = rank_of(p.a, adapter), steps = (rank + 15) / 16;
     if (steps == 0 && !p.copy) return;
-    const int token = p.order[slot * kManyTokens + (r16 < count ? 16 * wave + r16 : 0)];
+    // Low ranks: base and Y in whole lines.  A load or store takes all 64 outputs of eight tokens, the first and then the second eight; lanes r16 and r16 ^ 8 exchange what
+    // is the other's.  (In the order that the products leave, 32 outputs of sixteen tokens, an instruction costs twice the time of the address unit: 4096 tokens of rank 16,
+    // 4096 to 4096, 47 us against 41.  High ranks gain nothing, 57.3 and 57.5 us with 2048 tokens of rank 64, 8192 to 10240, and lack the registers.)
+    // 32 outputs after the other, because sixteen registers less are two workgroups more.
+    constexpr bool kLines = ST <= 2;
+    const bool upper = r16 & 8;
+    const auto place_of = [&](int i) { return kLines ? (r16 & 7) + 8 * i : r16; };         // of the lane's i-th piece: token of the wave
+    const auto column_of = [&](int i) { return 8 * g + 32 * (kLines ? upper : i); };        // and output of a group
+    int tokens[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) tokens[i] = p.order[slot * kManyTokens + (place_of(i) < count ? 16 * wave + place_of(i) : 0)];
+    const auto exchange = [&](u32x4 (&x)[2]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t give = upper ? x[0][e] : x[1][e];
+            const uint32_t got = __builtin_amdgcn_mov_dpp(give, 0x128, 0xf, 0xf, true);  // row_ror:8
+            x[0][e] = upper ? got : x[0][e];
+            x[1][e] = upper ? x[1][e] : got;
+        }
+    };
     const float unit = BF ? 1.0f : p.units[slot * kManyTokens + 16 * wave + r16];
     u32x4 v[kParts][ST];
     const u32x4 *const operands = p.operands + (size_t)(slot * (kManyTokens / 16) + wave) * p.operand_pieces;
@@ -618,7 +644,7 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
     const auto request = [&](int row0, u32x4 (&to)[2]) {
         if (row0 + 64 > M) return;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) to[h] = *reinterpret_cast<const u32x4_even *>(p.a.base + (long long)token * p.a.ld_base + row0 + 32 * h + 8 * g);
+        for (int i = 0; i < 2; ++i) to[i] = *reinterpret_cast<const u32x4_even *>(p.a.base + (long long)tokens[kLines ? i : 0] * p.a.ld_base + row0 + column_of(i));
     };
     int groups = p.row_groups;  // those that exist
     while (groups > 0 && first_row(groups - 1) >= M) --groups;
@@ -633,26 +659,62 @@ __global__ __launch_bounds__(64 * kWaves, many_occupancy(ST)) void bcq_lora_many
     for (int group = 0; group < groups; ++group) {
         const int row0 = first_row(group);
         if (group + 2 < groups) request(first_row(group + 2), later_base);
-        f32x4 acc[4];
+        const bool whole = row0 + 64 <= M;
+        const u32x4 *const at = rows_lds[group & 1];
+        const auto next_rows = [&] {
+            if (group + 1 < groups) put(rows_lds[(group + 1) & 1]);
+            if (group + 2 < groups) fetch(first_row(group + 2));
+        };
+        if constexpr (kLines) {
+            if (whole && steps) exchange(base);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) acc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (count > 0) {
-            const u32x4 *const at = rows_lds[group & 1];
+            for (int h = 0; h < 2; ++h) {
+                f32x4 acc[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+                if (count > 0) {
 #pragma unroll
-            for (int s = 0; s < ST; ++s) {
-                if (s >= steps) break;
-                u32x4 rows[4];
+                    for (int s = 0; s < ST; ++s) {
+                        if (s >= steps) break;
+                        u32x4 rows[2];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) rows[q] = at[row_of(r16, q) * (pieces + 1) + 2 * s + (g & 1)];
+                        for (int q = 0; q < 2; ++q) rows[q] = at[row_of(r16, 2 * h + q) * (pieces + 1) + 2 * s + (g & 1)];
 #pragma unroll
-                for (int part = 0; part < kParts; ++part)
+                        for (int part = 0; part < kParts; ++part)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[q] = mfma16<BF>(rows[q], v[part][s], acc[q]);
+                            for (int q = 0; q < 2; ++q) acc[q] = mfma16<BF>(rows[q], v[part][s], acc[q]);
+                    }
+                }
+                if (whole && steps) base[h] = add_pairs<BF>(base[h], acc[0], acc[1], unit);
+                else if (!whole && r16 < count) store_ends<BF>(p.a, (upper ? tokens[1] : tokens[0]), row0 + 32 * h + 8 * g, steps != 0, unit, acc[0], acc[1]);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            next_rows();
+            if (whole) {
+                if (steps) exchange(base);
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (place_of(i) < count)
+                        __builtin_nontemporal_store(base[i], reinterpret_cast<u32x4_even *>(p.a.Y + (long long)tokens[i] * p.a.ldy + row0 + column_of(i)));
+            }
+        } else {
+            f32x4 acc[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (count > 0) {
+#pragma unroll
+                for (int s = 0; s < ST; ++s) {
+                    if (s >= steps) break;
+                    u32x4 rows[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) rows[q] = at[row_of(r16, q) * (pieces + 1) + 2 * s + (g & 1)];
+#pragma unroll
+                    for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) acc[q] = mfma16<BF>(rows[q], v[part][s], acc[q]);
+                }
+            }
+            next_rows();
+            if (r16 < count) store_rows<BF>(p.a, tokens[0], row0, lane, whole, steps != 0, unit, base, acc);
         }
-        if (group + 1 < groups) put(rows_lds[(group + 1) & 1]);
-        if (group + 2 < groups) fetch(first_row(group + 2));
-        if (r16 < count) store_rows<BF>(p.a, token, row0, lane, row0 + 64 <= M, steps != 0, unit, base, acc);
         base[0] = next_base[0], base[1] = next_base[1];
         next_base[0] = later_base[0], next_base[1] = later_base[1];
         // (LDS alone: the stores need not have arrived)
