@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
         if (ANY) asm volatile("" : "+v"(dim));  // (compared here, not held as masks through the loop)
         const int first = min(key0 + kOwn * wave, last & -kOwn);         // keys behind the last are the last's copies, and masked
         const long long base = ANY ? 0 : __builtin_amdgcn_readfirstlane(id[0]) * p.page_stride + (long long)((first & ((1 << p.page_shift) - 1)) * p.slot_stride);
-        const int most = (last - first) * p.slot_stride;
+        const int most = min(last - first, kOwn - 1) * p.slot_stride;   // (inside the page: the keys that are left would pass 32 bits)
 #pragma unroll
         for (int i = 0; i < kTransfers; ++i) {
             const int in_lds = kOwn * wave + i * kRows + in_rows;
