@@ -304,7 +304,7 @@ typedef struct bcq_cache {
  *   positions DEVICE [tokens]; bounded to 0 .. max_position - 1
  *   cos_sin   DEVICE [max_position][rot_dim] binary32: rot_dim / 2 cosines, then as many sines; NULL iff rot_dim = 0
  *   q_weight, k_weight DEVICE [head_dim] of the cache's type, or NULL (no norm of these heads)
- *   q_out     DEVICE, row stride ld_q >= q_heads * head_dim; may be qkv itself with ld_q = ld_qkv
+ *   q_out     DEVICE, row stride ld_q >= q_heads * head_dim; may be qkv itself, with ld_q = ld_qkv if tokens > 1
  *   slots     DEVICE [tokens]: the token's slot; a value outside the cache (-1) means its k and v are not stored.  Tokens
  *             of one call have different slots.
  * Pointers 16-byte aligned (cos_sin 4), ld_qkv and ld_q multiples of 8, rot_dim even and at most head_dim, eps >= 0.
@@ -346,7 +346,8 @@ bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v
  *   rank    DEVICE [count] int32, bounded to 0 .. max_rank, or NULL (max_rank for all)
  *   scale   DEVICE [count] binary32, or NULL (1 for all)
  *   adapter DEVICE [tokens] int32
- *   X       DEVICE [tokens] rows of N, stride ldx;  base, Y DEVICE [tokens] rows of M, strides ld_base, ldy; Y may be base
+ *   X       DEVICE [tokens] rows of N, stride ldx;  base, Y DEVICE [tokens] rows of M, strides ld_base, ldy; Y may be base,
+ *           with ldy = ld_base if tokens > 1
  *   workspace DEVICE, bcq_lora_workspace_bytes(desc, tokens) bytes, 16-byte aligned; scratch, no init
  * N and max_rank multiples of 8, max_rank at most BCQ_MAX_RANK; A, B, X 16-byte aligned, ldx a multiple of 8; base and Y
  * aligned to 2 bytes, any M and strides (multiples of 8 elements and 16 bytes are faster).  tokens = 0 launches nothing.

@@ -67,7 +67,7 @@ bcq_status bcq_rotate(const bcq_cache *cache, int32_t tokens, int32_t q_heads, c
     if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(q_weight, 16) ||
         !aligned(k_weight, 16) || !aligned(cos_sin, 4) || !aligned(positions, 4) || !aligned(slots, 4))
         return BCQ_ERR_INVALID_ARG;
-    if (q_out == qkv && ld_q != ld_qkv) return BCQ_ERR_INVALID_ARG;
+    if (q_out == qkv && tokens > 1 && ld_q != ld_qkv) return BCQ_ERR_INVALID_ARG;  // (a lone row has no next one)
     RotateArgs a{half(qkv), half(q_weight), half(k_weight), positions, slots, cos_sin, half(q_out), half(k_cache), half(v_cache),
                  ld_qkv, ld_q, tokens, q_heads, rot_dim, max_position, eps, interleaved != 0, *cache};
     return launch_rotate(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
@@ -132,7 +132,7 @@ bcq_status bcq_lora(const bcq_adapters *desc, const void *A, const void *B, cons
     if (!aligned(A, 16) || !aligned(B, 16) || !aligned(X, 16) || !aligned(base, 2) || !aligned(Y, 2) || !aligned(rank, 4) || !aligned(scale, 4) ||
         !aligned(adapter, 4))
         return BCQ_ERR_INVALID_ARG;
-    if (Y == base && ldy != ld_base) return BCQ_ERR_INVALID_ARG;
+    if (Y == base && tokens > 1 && ldy != ld_base) return BCQ_ERR_INVALID_ARG;
     if (lora_workspace_bytes(*desc, tokens) > 0 && (!workspace || !aligned(workspace, 16))) return BCQ_ERR_WORKSPACE;
     LoraArgs a{half(A), half(B), half(X), half(base), rank, adapter, scale, half(Y), ldx, ld_base, ldy, tokens, workspace, *desc};
     return launch_lora(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;

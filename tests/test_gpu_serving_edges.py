@@ -6,8 +6,8 @@ import pytest
 import torch
 
 import paper_2407_02891_amd as bcq
-from tests.serving_util import assert_close, attend_ref
-from tests.test_gpu_serving import DT, _gen, _ints
+from tests.serving_util import assert_close, attend_ref, rotate_ref
+from tests.test_gpu_serving import DT, _gen, _ints, _rotate_case
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +35,32 @@ def test_attend_keys_times_slot_stride_beyond_32_bits(dtype, new, D, kv):
     got = bcq.PagedCache(k, v).attend(q, _ints([0, new]), _ints([kv]), table, new)
     ref, bound, _ = attend_ref(q, k, v, _ints([0, new]), _ints([kv]), table, 4, D ** -0.5, True, 0)
     assert_close(got, ref, bound)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("q_heads,kv_heads,D,gap", [(64, 8, 128, 0), (3, 1, 80, 8), (5, 5, 256, 0)])
+def test_rotate_one_token_in_place(q_heads, kv_heads, D, gap, interleaved, dtype):
+    qkv, k, v, slots, positions, table, (wq, wk) = _rotate_case(1, q_heads, kv_heads, D, D, interleaved, 3, dtype, gap=gap)
+    before = qkv.clone()
+    q = bcq.PagedCache(k, v).rotate(qkv, positions, table, slots, wq, wk, interleaved=interleaved, out=qkv[:, : q_heads * D])
+    assert q.data_ptr() == qkv.data_ptr()
+    ref, bound = rotate_ref(before, q_heads, kv_heads, D, positions, table, wq, wk, 1e-6, interleaved)
+    assert_close(q.view(1, q_heads, D), ref[:, :q_heads], bound[:, :q_heads])
+    assert torch.equal(qkv[:, q_heads * D:], before[:, q_heads * D:])
+    at = int(slots[0])
+    assert_close(k[at // 16, :, at % 16][None], ref[:, q_heads:q_heads + kv_heads], bound[:, q_heads:q_heads + kv_heads])
+    assert torch.equal(v[at // 16, :, at % 16], before.view(-1, D)[q_heads + kv_heads:])
+
+
+def test_lora_one_row_in_place_whatever_its_strides():
+    """Through the C entry points' binding: a lone row may be named with two strides."""
+    from paper_2407_02891_amd import binding as B
+    A, Bm = (torch.randn(s, device="cuda", generator=_gen(1)).half() * 0.1 for s in ((2, 8, 64), (2, 40, 8)))
+    X, base = torch.randn((1, 64), device="cuda", generator=_gen(2)).half(), torch.randn((1, 40), device="cuda", generator=_gen(3)).half()
+    ids = _ints([1])
+    want = bcq.Adapters(A, Bm).add(X, ids, base)
+    desc = B.AdaptersDesc(B.BCQ_F16, 2, 8, 40, 64)
+    scratch = torch.empty(bcq.lora_workspace_bytes(desc, 1) + 16, dtype=torch.uint8, device="cuda")
+    bcq.lora(desc, A, Bm, None, None, 1, ids, X, 64, base, 40, base, 96, scratch)
+    assert torch.equal(base, want)
