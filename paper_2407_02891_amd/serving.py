@@ -41,6 +41,7 @@ class PagedCache:
     def __init__(self, k, v):
         where = "PagedCache"
         _need(k.dim() == 4 and k.dtype in _DTYPES, where, "k: [pages][kv_heads][page_size][head_dim] of float16 or bfloat16")
+        _need(k.is_cuda, where, f"k: on a GPU, not on {k.device}")
         strides = [[n if size > 1 else t.shape[3] for n, size in zip(t.stride(), t.shape)] for t in (k, v)]  # (of a lone page or slot: nothing)
         _need(v.shape == k.shape and v.dtype == k.dtype and strides[0] == strides[1] and v.device == k.device, where,
               "v: shape, strides, type and device of k")
@@ -78,6 +79,7 @@ class Adapters:
     def __init__(self, A, B_, scale=None, rank=None):
         where = "Adapters"
         _need(A.dim() == 3 and A.dtype in _DTYPES and A.is_contiguous(), where, "A: contiguous [count][max_rank][N] of float16 or bfloat16")
+        _need(A.is_cuda, where, f"A: on a GPU, not on {A.device}")
         count, width, N = A.shape
         _need(B_.dim() == 3 and B_.shape[0] == count and B_.shape[2] == width and B_.dtype == A.dtype and B_.is_contiguous() and B_.device == A.device,
               where, "B: contiguous [count][M][max_rank] of A's type")
