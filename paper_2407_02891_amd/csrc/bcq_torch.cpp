@@ -128,6 +128,13 @@ T *address(PyObject *o)
     return reinterpret_cast<T *>(integer(o));
 }
 
+// What rows are divided by (the entry points check the rest of the cache).
+int64_t head_dim(const bcq_cache &c, const char *where)
+{
+    if (c.head_dim < 1) refuse(where, "cache: heads without elements");
+    return c.head_dim;
+}
+
 // rotate(desc, k, v, qkv, positions, cos_sin, slots, q_weight, k_weight, eps, interleaved, out, stream)
 at::Tensor rotate(PyObject *const *a)
 {
@@ -135,7 +142,7 @@ at::Tensor rotate(PyObject *const *a)
     const bcq_cache *const c = address<const bcq_cache>(a[0]);
     const at::Tensor &k = tensor(a[1], where, "k"), &v = tensor(a[2], where, "v"), &qkv = tensor(a[3], where, "qkv");
     const Place place{k.scalar_type(), k.device(), where};
-    const int64_t D = c->head_dim;
+    const int64_t D = head_dim(*c, where);
     if (qkv.dim() != 2 || qkv.size(1) % D || qkv.size(1) / D <= 2 * (int64_t)c->kv_heads)
         refuse(where, "qkv: [tokens][heads * head_dim], at least one q head before the k and v heads");
     const int64_t T = qkv.size(0), q_heads = qkv.size(1) / D - 2 * c->kv_heads;
@@ -166,7 +173,7 @@ at::Tensor attend(PyObject *const *a)
     const bcq_cache *const c = address<const bcq_cache>(a[0]);
     const at::Tensor &k = tensor(a[1], where, "k"), &v = tensor(a[2], where, "v"), &q = tensor(a[3], where, "q"), &pages = tensor(a[6], where, "pages");
     const Place place{k.scalar_type(), k.device(), where};
-    const int64_t D = c->head_dim;
+    const int64_t D = head_dim(*c, where);
     if (q.dim() != 2 || q.size(1) % D) refuse(where, "q: [tokens][q_heads * head_dim]");
     if (pages.dim() != 2 || pages.scalar_type() != at::kInt || pages.device() != place.device || !pages.is_contiguous())
         refuse(where, "pages: contiguous int32 [requests][max_pages]");

@@ -1,4 +1,7 @@
 """What the objects over the serving operators refuse before they reach the library (no GPU needed)."""
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -21,3 +24,23 @@ def test_tensors_that_are_not_on_a_gpu(device):
     A, Bm = (torch.zeros(s, dtype=torch.bfloat16, device=device) for s in ((1, 8, 64), (1, 40, 8)))
     _refused(lambda: bcq.Adapters(A, Bm))
     _refused(lambda: bcq.Adapters(A, Bm, torch.ones(1, device=device), torch.ones(1, dtype=torch.int32, device=device)))
+
+
+@pytest.mark.parametrize("call", ["rotate(at, k, k, x, ids, None, ids, None, None, 1e-6, False, None, 0)",
+                                  "attend(at, k, k, x, ids, ids, ids[:, None], 1, 1.0, True, 0, None, 0)"])
+def test_heads_without_elements(call):
+    """Refused, where rows were divided by them (in a process of its own, which that ended)."""
+    code = f"""
+import ctypes, torch
+import paper_2407_02891_amd as bcq
+from paper_2407_02891_amd import binding as B, serving
+desc = B.Cache(B.BCQ_F16, 1, 0, 16, 2, 16, 16, 8)
+at, k = ctypes.addressof(desc), torch.zeros((2, 1, 16, 0), dtype=torch.float16)
+x, ids = torch.zeros((1, 0), dtype=torch.float16), torch.zeros(1, dtype=torch.int32)
+try:
+    serving._load().{call}
+except bcq.BcqError as e:
+    print("refused", e.status)
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
+    assert (done.returncode, done.stdout.strip()) == (0, f"refused {B.BCQ_ERR_INVALID_ARG}"), done
