@@ -4,6 +4,7 @@
 // computes: the entry points of include/bcq.h do, through the library that bind() is given.  Errors are raised as the package's BcqError.
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
 #include <dlfcn.h>
 
 #include <string>
@@ -142,6 +143,7 @@ at::Tensor rotate(PyObject *const *a)
     const bcq_cache *const c = address<const bcq_cache>(a[0]);
     const at::Tensor &k = tensor(a[1], where, "k"), &v = tensor(a[2], where, "v"), &qkv = tensor(a[3], where, "qkv");
     const Place place{k.scalar_type(), k.device(), where};
+    const c10::DeviceGuard there(place.device);  // (launches go to the current device)
     const int64_t D = head_dim(*c, where);
     if (qkv.dim() != 2 || qkv.size(1) % D || qkv.size(1) / D <= 2 * (int64_t)c->kv_heads)
         refuse(where, "qkv: [tokens][heads * head_dim], at least one q head before the k and v heads");
@@ -173,6 +175,7 @@ at::Tensor attend(PyObject *const *a)
     const bcq_cache *const c = address<const bcq_cache>(a[0]);
     const at::Tensor &k = tensor(a[1], where, "k"), &v = tensor(a[2], where, "v"), &q = tensor(a[3], where, "q"), &pages = tensor(a[6], where, "pages");
     const Place place{k.scalar_type(), k.device(), where};
+    const c10::DeviceGuard there(place.device);  // (launches go to the current device)
     const int64_t D = head_dim(*c, where);
     if (q.dim() != 2 || q.size(1) % D) refuse(where, "q: [tokens][q_heads * head_dim]");
     if (pages.dim() != 2 || pages.scalar_type() != at::kInt || pages.device() != place.device || !pages.is_contiguous())
@@ -200,6 +203,7 @@ at::Tensor add(PyObject *const *a)
     const bcq_adapters *const d = address<const bcq_adapters>(a[0]);
     const at::Tensor &A = tensor(a[1], where, "A"), &B = tensor(a[2], where, "B"), &X = tensor(a[5], where, "X"), &base = tensor(a[7], where, "base");
     const Place place{A.scalar_type(), A.device(), where};
+    const c10::DeviceGuard there(place.device);
     if (X.dim() != 2 || X.size(0) > INT32_MAX) refuse(where, "X: [tokens][N]");
     const int64_t T = X.size(0), ldx = place.rows(X, "X", T, d->N), ld_base = place.rows(base, "base", T, d->M);
     const int32_t *const adapter = place.ints(a[6], "adapter", T);

@@ -7,7 +7,7 @@ import torch
 
 import paper_2407_02891_amd as bcq
 from tests.serving_util import assert_close, attend_ref, rotate_ref
-from tests.test_gpu_serving import DT, _gen, _ints, _rotate_case
+from tests.test_gpu_serving import DT, Batch, _gen, _ints, _lora_case, _rotate_case
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,19 @@ def test_lora_one_row_in_place_whatever_its_strides():
     scratch = torch.empty(bcq.lora_workspace_bytes(desc, 1) + 16, dtype=torch.uint8, device="cuda")
     bcq.lora(desc, A, Bm, None, None, 1, ids, X, 64, base, 40, base, 96, scratch)
     assert torch.equal(base, want)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two GPUs")
+def test_objects_of_a_device_that_is_not_the_current_one():
+    """The same calls with everything on the second device, while the first is the current one."""
+    first = Batch([1, 40], [300, 70], 4, 2, 64, 16, "f16")
+    want = first.run()
+    there = "cuda:1"
+    cache = bcq.PagedCache(first.k.to(there), first.v.to(there))
+    got = cache.attend(first.q.to(there), first.q_start.to(there), first.kv_len.to(there), first.pages.to(there), 40)
+    assert torch.cuda.current_device() == 0 and got.device == torch.device(there)
+    assert torch.equal(got.cpu(), want.cpu())
+    X, A, Bm, scale, rank, adapter, base = _lora_case(200, 256, 200, 3, 16, "f16")
+    want = bcq.Adapters(A, Bm, scale).add(X, adapter, base)
+    got = bcq.Adapters(A.to(there), Bm.to(there), scale.to(there)).add(X.to(there), adapter.to(there), base.to(there))
+    assert torch.equal(got.cpu(), want.cpu())
