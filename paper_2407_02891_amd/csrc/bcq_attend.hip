@@ -14,8 +14,8 @@
 //  * S^T = K Q^T: a lane gets four keys' scores of one row, and the same lane group's weights are the operand of O^T = V^T P^T as they
 //    are, because the keys of a product may be numbered in any order.
 //  * The next block's K and V are requested when this one's have gone to LDS, and its page numbers a block earlier: 16 KB a wave are on their way.
-//  * Weights are taken relative to a running maximum that is renewed only when a score passes it by 2^8, so O is hardly ever rescaled.
-//    They enter the second product as the sum of two 16-bit numbers (22 or 16 bits): it costs a matrix instruction more, and those wait for memory.
+//  * Weights are taken relative to a running maximum (Weights in bcq_attend.h).  They enter the second product as the sum of two 16-bit numbers: it costs a matrix
+//    instruction more, and those wait for memory.  bfloat16: 16 bits.  binary16: 22 bits of a weight down to 2^-17 of the largest, fewer below, 11 at 2^-28.
 //
 // Measured: 64 requests of 200 to 8000 keys, 64 / 8 heads of 128 (1.05 GB): 165 us and 8 for the join, 6.3 TB/s; with the loads alone, the arithmetic taken out, it
 // took no less, so what is left to the 7.2 TB/s of a plain read is the start (lengths, pages, the first keys: three reads in a row) and the end.
@@ -28,8 +28,9 @@ namespace {
 
 constexpr int kBlock = 32;  // keys of a step
 constexpr int kWaves = 4;
-constexpr float kGrow = 8.0f;
 constexpr int kStreamRows = 16;
+template <bool BF>
+using StreamWeights = Weights<BF, 1>;  // (renewing costs nothing where memory is waited for)
 constexpr int kMostRows = 128;  // of a tile of either kernel
 constexpr long long kPassingBytes = 128ll << 20;  // half of what the last level holds
 
@@ -289,11 +290,11 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
         float high = x[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) high = fmaxf(high, x[e]);
-        if (__ballot(high > most + kGrow)) {
+        if (__ballot(high > most + StreamWeights<BF>::grow)) {
             const float m = fmaxf(most, max_over_groups(high));
             const float shrink = most == -INFINITY ? 1.0f : exp2_fast(most - m);
             most = m;
-            base = m == -INFINITY ? 0.0f : m;
+            base = m == -INFINITY ? 0.0f : m - StreamWeights<BF>::lift;
             sum *= shrink;
 #pragma unroll
             for (int d = 0; d < DV; ++d) o[d] *= shrink;

@@ -9,8 +9,9 @@
 //    both kinds of reads find all banks.
 //  * S^T = K Q^T with Q in registers: a lane has one row's scores, 32 for a block of 64 keys, so a row's maximum and sum need one exchange between
 //    two lanes; its weights, rounded to 16 bits, are the operand of O^T = V^T P^T as they are, for the keys of a product may be numbered in any order.
-//    V's side of it comes from the transposing read.  The rounding of the weights adds to a result what its own rounding does (1.4 times in the mean square).
-//  * Maxima are renewed only when a score passes them by 2^8; blocks that all of a wave's rows see have no masks, those that none sees are left out.
+//    V's side of it comes from the transposing read.  The rounding of the weights adds to a result what its own rounding does (1.4 times in the mean square).  Weights are taken relative to a running maximum (Weights in
+//    bcq_attend.h).
+//  * Blocks that all of a wave's rows see have no masks, those that none sees are left out.
 //  * Few tiles and many keys: the keys of a tile are cut into `parts`, whose sums a second launch joins.
 //
 // Measured: 2048 tokens over 8192 keys, 56 heads of 128, bfloat16: 440 us, 957 TFLOP/s, three quarters of what a large library product reaches; the matrix
@@ -24,8 +25,10 @@ namespace bcq {
 namespace {
 
 constexpr int kWaves = 4, kChunkRows = 32 * kWaves;
-constexpr float kGrow = 8.0f;
 constexpr int kFewParts = 8;
+// (Renewed at half of that, heads of 128 take 1 % more and heads of 256 10; at a quarter 2 and 20.)
+template <bool BF>
+using ChunkWeights = Weights<BF, 8>;
 constexpr int chunk_keys(int dim) { return dim == 256 ? 32 : 64; }  // a block
 constexpr int chunk_occupancy(int dim) { return dim == 256 ? 1 : 2; }
 
@@ -262,7 +265,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
 #pragma unroll
             for (int e = 1; e < 16 * KT; ++e) high = fmaxf(high, x[e]);
             high *= p.scale;
-            if (__ballot(high > most + kGrow)) {
+            if (__ballot(high > most + ChunkWeights<BF>::grow)) {
                 const auto other = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, high), __builtin_bit_cast(unsigned, high), false, false);
                 const float m = fmaxf(most, fmaxf(__builtin_bit_cast(float, (unsigned)other[0]), __builtin_bit_cast(float, (unsigned)other[1])));
                 if (DT == 256) {  // (or it copies O from the accumulation registers for every block, not here)
@@ -271,7 +274,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
                 }
                 const float shrink = most == -INFINITY ? 1.0f : exp2_fast(most - m);
                 most = m;
-                base = m == -INFINITY ? 0.0f : m;
+                base = m == -INFINITY ? 0.0f : m - ChunkWeights<BF>::lift;
                 sum *= shrink;
 #pragma unroll
                 for (int d = 0; d < DV; ++d) o[d] *= shrink;

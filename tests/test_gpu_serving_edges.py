@@ -80,3 +80,26 @@ def test_objects_of_a_device_that_is_not_the_current_one():
     want = bcq.Adapters(A, Bm, scale).add(X, adapter, base)
     got = bcq.Adapters(A.to(there), Bm.to(there), scale.to(there)).add(X.to(there), adapter.to(there), base.to(there))
     assert torch.equal(got.cpu(), want.cpu())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 20, 140])
+@pytest.mark.parametrize("kv,nats", [(1000, 13.0), (1000, 14.0), (131073, 16.0), (131073, 18.0)])
+def test_attend_small_weights_beside_a_key_of_no_value(kv, nats, new, dtype):
+    """The first key has nearly all the weight and a value of zero, so the small weights are the result."""
+    D, page = 64, 16
+    if kv > 1000 and new > 20:
+        new, kv = 140, 16385
+    dt = DT[dtype]
+    pages = -(-kv // page)
+    k = torch.zeros((pages, 1, page, D), dtype=dt, device="cuda")
+    v = (1 + 0.1 * torch.randn((pages, 1, page, D), device="cuda", generator=_gen(kv))).to(dt)
+    k[0, 0, 0] = nats / 8
+    v[0, 0, 0] = 0
+    q = torch.ones((new, D), dtype=dt, device="cuda")
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    # (with a table far longer than the keys too: the keys are cut otherwise)
+    for wide in (table, torch.cat([table, table.new_zeros((1, 3 * 131072 // page))], 1)):
+        got = bcq.PagedCache(k, v).attend(q, _ints([0, new]), _ints([kv]), wide.contiguous(), new)
+        ref, bound, _ = attend_ref(q, k, v, _ints([0, new]), _ints([kv]), table, 1, D ** -0.5, True, 0)
+        assert_close(got, ref, bound)
