@@ -95,6 +95,9 @@ struct Weights {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// 2^x, x <= 0, that sums are multiplied by: never zero, which would make a NaN of a sum that is infinite.
+__device__ __forceinline__ float shrink_by(float x) { return fmaxf(exp2_fast(x), 0x1p-149f); }
+
 // Joining the pieces of a row: piece i has its sums in part and its (maximum, weight) in stat at at(i).
 struct Slots {
     long long first, step;
@@ -118,7 +121,7 @@ __device__ __forceinline__ void join_pieces(const AttendParams &p, const At &at,
     for (int c = from + share; c < end; c += 64 * STRIDE) {  // sixty-four pieces, a lane has the statistics of one
         const int mine = c + lane * STRIDE, n = min((end - 1 - c) / STRIDE + 1, 64);
         const f32x2 stat = p.stat[at(min(mine, end - 1))];
-        const float scale = exp2_fast(stat.x - base);
+        const float scale = shrink_by(stat.x - base);
         if (mine < end) weight = fmaf(stat.y, scale, weight);
         for (int i = 0; i < n; i += kJoinAhead) {
             float part[kJoinAhead][E];

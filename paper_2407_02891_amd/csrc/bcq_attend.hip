@@ -239,18 +239,17 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
         // K and V to LDS, scores
         const int key0 = now.key;
         const bool masked = key0 + kBlock > all_to || key0 < all_from;
-        // Infinities or NaN among values that not every row sees: zero times them must not reach the rows that do not.  They are replaced by
-        // zeros, and what they make of the rows that do see them, an infinity or a NaN, is found by products of ones.
-        bool odd = false;
-        if (masked) {
+        // Infinities or NaN among the values: zero times them must not reach the rows that do not see them, nor must the second number of a weight, which may be zero or
+        // negative, or a weight too small for its type, make a NaN of an infinity.  They are replaced by zeros, and what they make of the rows that do see them, an infinity or a
+        // NaN, is found by products of ones.
+        float zero = 0.0f;
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+            for (int c = 0; c < C; ++c)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) odd |= not_finite<BF>(vr[t][c][i]);
-            odd = __ballot(odd) != 0;
-        }
+                for (int i = 0; i < 4; ++i) zero = times_zero<BF>(vr[t][c][i], zero);
+        const bool odd = __ballot(zero != 0.0f) != 0;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -292,7 +291,7 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
         for (int e = 1; e < 8; ++e) high = fmaxf(high, x[e]);
         if (__ballot(high > most + StreamWeights<BF>::grow)) {
             const float m = fmaxf(most, max_over_groups(high));
-            const float shrink = most == -INFINITY ? 1.0f : exp2_fast(most - m);
+            const float shrink = most == -INFINITY ? 1.0f : shrink_by(most - m);
             most = m;
             base = m == -INFINITY ? 0.0f : m - StreamWeights<BF>::lift;
             sum *= shrink;
@@ -400,7 +399,7 @@ __global__ __launch_bounds__(64 * (OWN ? OWN : kWaves), OWN ? most_waves(DT) / 4
         f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            const float scale = exp2_fast(stat[w][row].x - high);
+            const float scale = shrink_by(stat[w][row].x - high);
             all = fmaf(stat[w][row].y, scale, all);
             y += *reinterpret_cast<const f32x4 *>(sums(w) + row * kStep + d) * scale;
         }

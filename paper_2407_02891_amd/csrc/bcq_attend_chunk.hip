@@ -61,6 +61,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
     constexpr int kTransfers = KB / (kRows * kWaves);           // of a wave for a block of K, and for one of V
     // Two buffers each, as objects of their own: the compiler holds reads of one back for the transfers to it alone.
     __shared__ __attribute__((aligned(1024))) uint16_t k0[KB * DT], k1[KB * DT], v0[KB * DT], v1[KB * DT];
+    __shared__ int votes[kWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r32 = lane & 31, h = lane >> 5;
 
@@ -149,11 +150,8 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
         }
     }
     f32x16 o[DV];
-#pragma unroll
-    for (int d = 0; d < DV; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-    float most = -INFINITY, base = 0.0f, sum = 0.0f;
+    float most, base, sum;
+    bool careful = false;  // all blocks of V are looked at for infinities and NaN, not only those with masks
 
     const auto step = [&](int b, const uint16_t *kb, uint16_t *vb, uint16_t *next_k, uint16_t *next_v) {
         const int key0 = b * KB;
@@ -175,18 +173,19 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
             const u32x2 v0 = lds_column(v_at(vb, key, e)), v1 = lds_column(v_at(vb, key + 8, e));
             return u32x4{v0.x, v0.y, v1.x, v1.y};
         };
-        if (key0 + KB > tile_to || key0 < tile_from) {
+        if (careful || key0 + KB > tile_to || key0 < tile_from) {
             // Not all rows of the tile see all of these keys.  Infinities or NaN among the values: zero times them must not reach the rows that do not
             // see them.  They are replaced by zeros, and what they make of the rows that do, an infinity or a NaN, is found by products of ones.  (Every wave looks at the whole block, so all of them meet at the barriers or none.)
             int it = lane;
             asm volatile("" : "+v"(it));  // what follows from it is not worth registers over the loop
-            bool odd = false;
+            float zero = 0.0f;
 #pragma unroll 1
             for (int i = it; i < KB * DT / 8; i += 64) {
                 const u32x4 x = *reinterpret_cast<const u32x4 *>(vb + 8 * i);
-                odd |= not_finite<BF>(x[0]) || not_finite<BF>(x[1]) || not_finite<BF>(x[2]) || not_finite<BF>(x[3]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) zero = times_zero<BF>(x[e], zero);
             }
-            if (__ballot(odd)) {
+            if (__ballot(zero != 0.0f)) {
                 if (work) {
                     const unsigned span = max(to - from, 0);
 #pragma unroll
@@ -272,7 +271,7 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
 #pragma unroll
                     for (int d = 0; d < DV; ++d) asm volatile("" : "+a"(o[d]));
                 }
-                const float shrink = most == -INFINITY ? 1.0f : exp2_fast(most - m);
+                const float shrink = most == -INFINITY ? 1.0f : shrink_by(most - m);
                 most = m;
                 base = m == -INFINITY ? 0.0f : m - ChunkWeights<BF>::lift;
                 sum *= shrink;
@@ -300,13 +299,41 @@ __global__ __launch_bounds__(64 * kWaves, chunk_occupancy(DT)) void bcq_attend_c
             }
         }
     };
-    if (b0 < b1) {
-        find_pages(b0 * KB);
-        request(b0 * KB, k0, v0);
-    }
-    for (int b = b0; b < b1; b += 2) {
-        step(b, k0, v0, k1, v1);
-        if (b + 1 < b1) step(b + 1, k1, v1, k0, v0);
+    // Once, and again with care if a result is not finite: an infinity that all rows see would be a NaN of the rows whose weight for it is too small for its type.
+    for (;;) {
+#pragma unroll
+        for (int d = 0; d < DV; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+        most = -INFINITY;
+        base = sum = 0.0f;
+        int first = b0;
+        asm volatile("" : "+s"(first));  // (or what the first request computes would be kept for the second time)
+        if (first < b1) {
+            find_pages(first * KB);
+            request(first * KB, k0, v0);
+        }
+        for (int b = first; b < b1; b += 2) {
+            step(b, k0, v0, k1, v1);
+            if (b + 1 < b1) step(b + 1, k1, v1, k0, v0);
+        }
+        if (careful) break;
+        float zero = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DV; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) zero = fmaf(o[d][i], 0.0f, zero);
+        const unsigned long long odd = __ballot(real && zero != 0.0f);  // (a NaN)
+        if (lane == 0) votes[wave] = odd != 0;
+        asm volatile("" ::: "memory");
+        all_arrived();
+        __builtin_amdgcn_s_barrier();  // (and every wave is through with the buffers)
+        asm volatile("" ::: "memory");
+        int any = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) any |= votes[w];
+        careful = __builtin_amdgcn_readfirstlane(any) != 0;
+        if (!careful) break;
     }
 
     // ---- results: lane (h, r32) has of row r32 the elements 32 d + 8 u + 4 h + i in number 4 u + i of o[d] ----
@@ -402,7 +429,7 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_attend_chunk_join_few_kernel(
 #pragma unroll
     for (int k = 0; k < kFewParts; ++k)
         if (k < p.parts) {
-            const float scale = exp2_fast(stat[k].x - base);
+            const float scale = shrink_by(stat[k].x - base);
             weight = fmaf(stat[k].y, scale, weight);
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = fmaf(part[k][e], scale, y[e]);

@@ -43,12 +43,12 @@ __device__ __forceinline__ f32x2 to_float2(uint32_t pair)
     else return f32x2{half_bits_to_float(pair & 0xffffu), half_bits_to_float(pair >> 16)};
 }
 
-// One of the two elements is an infinity or a NaN.
+// sum + 0 * the pair's elements: NaN once one of them was an infinity or a NaN.
 template <bool BF>
-__device__ __forceinline__ bool not_finite(uint32_t pair)
+__device__ __forceinline__ float times_zero(uint32_t pair, float sum)
 {
-    constexpr uint32_t kExponent = BF ? 0x7f80u : 0x7c00u;
-    return (pair & kExponent) == kExponent || (pair >> 16 & kExponent) == kExponent;
+    if constexpr (BF) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b16x2, pair), b16x2{0, 0}, sum, false);
+    else return __builtin_amdgcn_fdot2(__builtin_bit_cast(h16x2, pair), h16x2{0, 0}, sum, false);
 }
 
 template <bool BF>

@@ -103,3 +103,19 @@ def test_attend_small_weights_beside_a_key_of_no_value(kv, nats, new, dtype):
         got = bcq.PagedCache(k, v).attend(q, _ints([0, new]), _ints([kv]), wide.contiguous(), new)
         ref, bound, _ = attend_ref(q, k, v, _ints([0, new]), _ints([kv]), table, 1, D ** -0.5, True, 0)
         assert_close(got, ref, bound)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("q_heads,kv_heads,D,page", [(4, 2, 64, 16), (4, 2, 128, 16), (2, 2, 256, 32), (4, 2, 80, 8)])
+@pytest.mark.parametrize("gain", [1.0, 8.0, 40.0])
+def test_attend_infinities_that_are_seen(gain, q_heads, kv_heads, D, page, dtype):
+    """An infinity among the values is one of every row that sees it, however little weight its key has and wherever it lies; a NaN, and infinities of both signs, are NaN."""
+    for long_table in (False, True):
+        b = Batch([1, 3, 70, 150, 1], [700, 500, 300, 650, 2100], q_heads, kv_heads, D, page, dtype, seed=D, gain=gain)
+        if long_table:
+            b.pages = torch.cat([b.pages, b.pages.new_zeros((5, 20000 // page))], 1).contiguous()
+        for r, j, value in ((0, 3, math.inf), (0, 400, -math.inf), (1, 130, math.inf), (1, 498, -math.inf), (2, 64, -math.inf), (2, 260, math.nan), (3, 40, math.inf),
+                            (3, 600, math.inf), (4, 1000, -math.inf)):
+            b.v[int(b.pages[r, j // page]), 0, j % page, (r + j % 2)::3] = value
+        b.check(what=f"long table {long_table}")
+        b.check(window=100, what=f"window, long table {long_table}")
