@@ -594,7 +594,8 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t stream)
     p.ld_q = a.ld_q, p.ld_out = a.ld_out, p.page_stride = c.page_stride, p.head_stride = c.head_stride, p.slot_stride = (int)c.slot_stride;
     p.tokens = a.tokens, p.requests = a.requests, p.kv_heads = c.kv_heads, p.group = a.q_heads / c.kv_heads;
     p.head_dim = c.head_dim, p.page_shift = __builtin_ctz(c.page_size), p.num_pages = c.num_pages, p.max_pages = a.max_pages;
-    p.max_new = a.max_new, p.window = a.window, p.causal = a.causal;
+    p.max_new = a.max_new, p.causal = a.causal;
+    p.window = a.window > 1 << 30 ? 0 : a.window;  // (no request has so many keys, and positions less a window stay in range)
     // What the rows of a tile can see at most, as far as the host knows.
     long long most_keys = (long long)a.max_pages * c.page_size;
     const int tile_tokens = kMostRows / p.group + 2 < a.max_new ? kMostRows / p.group + 2 : a.max_new;

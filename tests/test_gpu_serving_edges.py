@@ -119,3 +119,12 @@ def test_attend_infinities_that_are_seen(gain, q_heads, kv_heads, D, page, dtype
             b.v[int(b.pages[r, j // page]), 0, j % page, (r + j % 2)::3] = value
         b.check(what=f"long table {long_table}")
         b.check(window=100, what=f"window, long table {long_table}")
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 5, 2 ** 30 + 1, 2 ** 30])
+def test_attend_windows_longer_than_anything(window):
+    """No window at all, also where there are more new tokens than keys."""
+    for new, kv in (([1, 3, 16], [400, 2, 9]), ([200, 1, 70], [100, 50, 300])):
+        b = Batch(new, kv, 2, 2, 64, 16, "f16")
+        b.check(window=window)
+        assert torch.equal(b.run(window=window), b.run())
