@@ -3,7 +3,9 @@ marshalling only.  Tensors are torch CUDA(ROCm) tensors used as device memory;
 the stream is torch's current stream unless one is given.  There is no CPU
 fallback: if the library is missing, loading raises."""
 import ctypes
+import importlib.util
 import os
+import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libbcq.so")
@@ -53,6 +55,18 @@ class BcqError(RuntimeError):
 _lib = None
 
 
+def _share_torch_runtime():
+    """torch brings a HIP runtime of its own, and a process with two of them cannot pass streams from one to the other.  The first that is loaded
+    serves both, so where torch is installed but not imported yet, its runtime is loaded before the library (without torch: ROCm's)."""
+    if "torch" in sys.modules:
+        return
+    spec = importlib.util.find_spec("torch")
+    if spec is not None and spec.origin:
+        runtime = os.path.join(os.path.dirname(spec.origin), "lib", "libamdhip64.so")
+        if os.path.exists(runtime):
+            ctypes.CDLL(runtime)
+
+
 def lib():
     """Load libbcq.so (built in-tree by build.py).  Raises if it is not there."""
     global _lib
@@ -60,6 +74,7 @@ def lib():
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: run `python __graft_entry__.py build` "
                                "(there is no fallback path)")
+        _share_torch_runtime()
         L = ctypes.CDLL(LIB_PATH)
         vp, i32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
         dp = ctypes.POINTER(Desc)

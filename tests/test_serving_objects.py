@@ -44,3 +44,28 @@ except bcq.BcqError as e:
 """
     done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
     assert (done.returncode, done.stdout.strip()) == (0, f"refused {B.BCQ_ERR_INVALID_ARG}"), done
+
+
+def test_the_package_needs_no_torch():
+    """Importing it and calling the C ABI through it leaves torch alone, as it did before there were objects over tensors."""
+    code = """
+import sys
+import paper_2407_02891_amd as bcq
+assert bcq.packed_bytes(bcq.Desc(64, 128, 2, 128)) > 0 and "PagedCache" in dir(bcq)
+assert "torch" not in sys.modules
+assert bcq.PagedCache.__name__ == "PagedCache" and bcq.Adapters.__name__ == "Adapters" and "torch" in sys.modules
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
+    assert done.returncode == 0, done.stderr
+
+
+@pytest.mark.parametrize("order", ["bcq.lib(); import torch", "import torch; bcq.lib()"])
+def test_one_hip_runtime_whatever_is_loaded_first(order):
+    """Streams of torch's mean nothing to a second HIP runtime."""
+    code = f"""
+import paper_2407_02891_amd as bcq
+{order}
+print(len({{l.split()[-1] for l in open("/proc/self/maps") if "libamdhip64" in l}}))
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
+    assert (done.returncode, done.stdout.strip()) == (0, "1"), done
