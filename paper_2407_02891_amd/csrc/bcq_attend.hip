@@ -577,9 +577,10 @@ size_t attend_workspace_bytes(const bcq_cache &c, int tokens, int requests, int 
 {
     const Split which = split(tokens, requests, q_heads / c.kv_heads, max_new);
     const StreamPlan s = stream_plan(c, requests);
-    const size_t one = which.stream ? s.part_bytes + s.slots * sizeof(f32x2) : 0;
+    const long long most_keys = (long long)max_pages * c.page_size;  // (a window makes them fewer, and one launch no less likely)
+    const size_t one = which.stream && !one_launch((long long)requests * c.kv_heads, s.dim, most_keys) ? s.part_bytes + s.slots * sizeof(f32x2) : 0;
     if (!which.chunk) return one;
-    const int parts = chunk_parts(tokens, requests, max_new, q_heads / c.kv_heads, c.kv_heads, s.dim, (long long)max_pages * c.page_size);
+    const int parts = chunk_parts(tokens, requests, max_new, q_heads / c.kv_heads, c.kv_heads, s.dim, most_keys);
     const size_t other = chunk_bytes(parts, tokens, q_heads, s.dim);
     return one > other ? one : other;  // one after the other
 }

@@ -128,3 +128,11 @@ def test_attend_windows_longer_than_anything(window):
         b = Batch(new, kv, 2, 2, 64, 16, "f16")
         b.check(window=window)
         assert torch.equal(b.run(window=window), b.run())
+
+
+def test_attend_in_one_launch_takes_no_workspace():
+    b = Batch([1, 2, 1], [600, 33, 1], 8, 2, 128, 16, "f16")
+    out = torch.empty_like(b.q)
+    assert bcq.attend_workspace_bytes(b.cache.desc, 4, 3, 8, b.pages.shape[1], 2) == 0
+    bcq.attend(b.cache.desc, b.k, b.v, 4, 3, 8, b.q, b.q.stride(0), b.q_start, b.kv_len, b.pages, b.pages.shape[1], 2, 128 ** -0.5, True, 0, out, out.stride(0), None)
+    assert torch.equal(out, b.run())
