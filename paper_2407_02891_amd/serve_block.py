@@ -43,7 +43,13 @@ class Requests:
         self.adapter = adapter  # of each request, any number outside the adapters': none
         self.device = device
 
+    def _room(self, new):
+        for r, n in enumerate(new):
+            if self.length[r] + n > self.width * self.page_size:
+                raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"Requests (request {r}: {self.length[r]} tokens and {n} more do not fit its {self.width} pages)")
+
     def take(self, new):
+        self._room(new)
         positions, slots, owner = [], [], []
         for r, n in enumerate(new):
             at = range(self.length[r], self.length[r] + n)
@@ -57,6 +63,7 @@ class Requests:
 
     def advance(self, batch):
         """The next single token of every request (pages of a request are neighbours here, so slots advance by one)."""
+        self._room([1] * len(self.length))
         for name in ("positions", "slots", "kv_len"):
             batch[name].add_(1)
         self.length = [n + 1 for n in self.length]
