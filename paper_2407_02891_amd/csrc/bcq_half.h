@@ -36,6 +36,14 @@ __device__ __forceinline__ uint32_t from_float2(float a, float b)
     else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), h16x2));
 }
 
+// The same, rounded toward zero.
+template <bool BF>
+__device__ __forceinline__ uint32_t toward_zero2(float a, float b)
+{
+    if constexpr (BF) return __builtin_bit_cast(uint32_t, a) >> 16 | (__builtin_bit_cast(uint32_t, b) & 0xffff0000u);
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+}
+
 template <bool BF>
 __device__ __forceinline__ f32x2 to_float2(uint32_t pair)
 {

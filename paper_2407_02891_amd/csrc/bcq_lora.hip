@@ -7,7 +7,7 @@
 //  * v = A x (shrink): a workgroup has a tile, 16 to 64 rows of A and a slice of N; its waves share the slice and add up in LDS.  The slices, as many as fill
 //    the chip, leave their sums in binary32 side by side, and whoever reads them adds them in order.
 //  * Y = base + B v (expand): a workgroup has a tile and a range of rows of B.  v (times the scale) is held as a sum of 16-bit numbers beside the 16-bit rows of B:
-//    two for binary16 (after a power of two for each token: 22 bits and more of its largest value), three for bfloat16 (24 bits).  The operand's 32
+//    two for binary16 (after a power of two for each token: 21 bits and more of its largest value), three for bfloat16 (23 bits).  The operand's 32
 //    places are 16 of v's first numbers and the same 16 of its second ones.  The rows of B are numbered so that a lane ends up with eight
 //    neighbouring outputs of a token and four lanes with 32.
 //  * Many tokens of few adapters: v is turned into operands once (pack), and rows of B go through LDS for 64 tokens (many).
@@ -269,16 +269,26 @@ __device__ __forceinline__ void store_rows(const LoraArgs &p, int token, int row
 // binary16: v's largest value is brought to 2^13 .. 2^14; its bits -> the power of two to divide by.
 __device__ __forceinline__ int power_of(uint32_t largest) { return min(max((int)(largest >> 23) - 127, -100), 100) - 13; }
 
-// Two values of v as sums of 16-bit numbers; nothing is left of an infinity or a NaN.
+// Two values of v as sums of 16-bit numbers, all of a value's sign and none of them zero unless it is: an infinity among B's weights is then one of the result, as it
+// is without the split, where a zero or a second number of the other sign would make a NaN of it.  (What that adds, 2^-24 beside 2^13 or 2^-126, is behind the last
+// bit.)  Nothing is left of an infinity or a NaN.  binary16: first and second; bfloat16: third too, half of what is left, which is used twice.
 template <bool BF>
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t &first, uint32_t &second, uint32_t &third)
 {
-    first = from_float2<BF>(a, b);
+    const uint32_t tiny = (a != 0.0f ? (BF ? 0x0080u : 1u) : 0u) | (b != 0.0f ? (BF ? 0x00800000u : 0x10000u) : 0u);
+    const uint32_t sign = (__builtin_bit_cast(uint32_t, a) >> 16 & 0x8000u) | (__builtin_bit_cast(uint32_t, b) & 0x80000000u);
+    const auto no_zero = [&](uint32_t pair) {
+        if (!(pair & 0x7fffu)) pair |= (tiny | sign) & 0xffffu;
+        if (!(pair & 0x7fff0000u)) pair |= (tiny | sign) & 0xffff0000u;
+        return pair;
+    };
+    first = toward_zero2<BF>(a, b);
     f32x2 kept = to_float2<BF>(first);
     a = fabsf(kept.x) < INFINITY ? a - kept.x : 0.0f, b = fabsf(kept.y) < INFINITY ? b - kept.y : 0.0f;
-    second = from_float2<BF>(a, b);
+    second = BF ? toward_zero2<BF>(a, b) : from_float2<BF>(a, b);
     kept = to_float2<BF>(second);
-    third = BF ? from_float2<BF>(a - kept.x, b - kept.y) : 0u;
+    third = BF ? no_zero(from_float2<BF>(0.5f * (a - kept.x), 0.5f * (b - kept.y))) : 0u;
+    first = no_zero(first), second = no_zero(second);
 }
 
 // NT: tokens of a tile in sixteens.  RT: rows of A of a workgroup in sixteens.
@@ -316,7 +326,7 @@ __global__ __launch_bounds__(64 * kWaves) void bcq_lora_shrink_kernel(LoraParams
     }
 }
 
-// v of sixteen tokens as matrix operands: [part][step of 16][lane] 16 bytes; part 1 (bfloat16 only) the third numbers.
+// v of sixteen tokens as matrix operands: [part][step of 16][lane] 16 bytes; part 1 (bfloat16 only) the third numbers, twice their halves.
 constexpr size_t operand_bytes(bool bf, int steps) { return (size_t)(bf ? 2 : 1) * steps * 1024; }
 
 // Adds up the slices of v of sixteen tokens and turns it into operands.  binary16: largest[] (zeros before) becomes each token's largest value's bits, of
@@ -364,7 +374,7 @@ __device__ __forceinline__ void make_operands(const LoraParams &p, int adapter, 
         }
         u32x4 *const at = operands + (eight >> 1) * 64 + token + 16 * (eight & 1);
         at[0] = first, at[32] = second;
-        if (BF) at[64 * steps] = rest, at[64 * steps + 32] = u32x4{0, 0, 0, 0};
+        if (BF) at[64 * steps] = rest, at[64 * steps + 32] = rest;
     }
 }
 

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2407_02891_amd as bcq
-from tests.serving_util import assert_close, attend_ref, rotate_ref
+from tests.serving_util import assert_close, attend_ref, lora_ref, rotate_ref
 from tests.test_gpu_serving import DT, Batch, _gen, _ints, _lora_case, _rotate_case
 
 pytestmark = pytest.mark.gpu
@@ -136,3 +136,17 @@ def test_attend_in_one_launch_takes_no_workspace():
     assert bcq.attend_workspace_bytes(b.cache.desc, 4, 3, 8, b.pages.shape[1], 2) == 0
     bcq.attend(b.cache.desc, b.k, b.v, 4, 3, 8, b.q, b.q.stride(0), b.q_start, b.kv_len, b.pages, b.pages.shape[1], 2, 128 ** -0.5, True, 0, out, out.stride(0), None)
     assert torch.equal(out, b.run())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,N,M,C,width", [(1, 64, 200, 2, 16), (1, 16384, 100, 2, 64), (5, 264, 130, 2, 24), (64, 512, 100, 3, 8), (300, 136, 333, 3, 40), (1100, 264, 200, 2, 64),
+                                           (4200, 72, 130, 2, 16)])
+def test_lora_infinities_among_the_weights(T, N, M, C, width, dtype):
+    """An infinity in an adapter's B is one of the outputs it belongs to, for tokens of that adapter; a NaN, and infinities of both signs there, are NaN."""
+    X, A, Bm, scale, rank, adapter, base = _lora_case(T, N, M, C, width, dtype, seed=T, ranks=[width, width - 3])
+    for m, j, value in ((3, 0, math.inf), (7, 4, -math.inf), (64, 2, math.inf), (64, 3, math.inf), (90, 1, math.nan), (M - 1, 4, math.inf)):
+        Bm[0, m, j] = value
+    adapter[0] = 0
+    ref, bound = lora_ref(X, A, Bm, scale, rank, adapter, base)
+    assert bool(ref.isinf().any()) and bool(ref.isnan().any())
+    assert_close(bcq.Adapters(A, Bm, scale, rank).add(X, adapter, base), ref, bound)
