@@ -492,13 +492,16 @@ namespace {
 int padded_dim(int head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
 
 // One launch, in which a workgroup has a (request, kv head) to itself, or the line and its join?  The line balances and fills the chip with few
-// requests, but costs a launch more and its waves look at all requests first.  Measured with all requests of a length, heads of 128, 8 kv heads,
-// own against line: 16 requests of 1000 keys 16.2 and 23.2 us, 1 of 1000 11.8 and 11.5, 4 of 2000 (without the rule) 20.4 and 17; with four waves 64 requests of
-// 200 keys 13.2 and 21.3, of 1000 51 and 53, of 2000 96 and 93.
+// requests, but costs a launch more and its waves look at all requests first.  With fewer pairs than compute units a wave may have five blocks in a row, four (heads of 64:
+// three) where there are so few pairs that the line's many waves have hardly one.  Measured, own against line (replayed graphs, all requests of a length, 8 kv heads of 8 query
+// heads): heads of 128, 1 request of 500 keys 8.2 and 10.9 us, 1000 11.6 and 11.1 (eager calls 10.5 and 10.6), 1200 13.0 and 10.9; 4 of 1200 14.2 and 15.5, 16 of 1000
+// 15.5 and 23.3; heads of 64, 1 of 1500 9.6 and 9.7, 2000 11.1 and 9.7, 4 of 2500 13.8 and 14.2; heads of 256, 1 of 300 13.8 and 16.3, 600 19.4 and 17.7, 4 of 600 20.5 and
+// 26.0.  With four waves, heads of 128, 64 requests of 200 keys 13.3 and 21.6, of 1000 50.8 and 52.4; heads of 64, 64 of 1500 39.0 and 41.7.
 bool one_launch(long long pairs, int dim, long long most_keys)
 {
     if (pairs > 1 << 23) return false;  // (threads of a grid)
-    return most_keys <= (pairs < compute_units() ? 5 * kBlock * most_waves(dim) : 1536);
+    const int cus = compute_units(), in_a_row = pairs >= cus / 16 ? 5 : dim == 64 ? 3 : 4;
+    return most_keys <= (pairs < cus ? in_a_row * kBlock * most_waves(dim) : 1536);
 }
 
 struct StreamPlan {
