@@ -269,7 +269,8 @@ bcq_status bcq_gemm_skinny(const bcq_desc *desc, const void *packed,
  * low-rank adapters of many requests (bcq_lora), norms of q and k per head with the position rotation and the append to a
  * paged cache in one pass (bcq_rotate), attention over that cache (bcq_attend).  Elements are binary16 or bfloat16
  * (bcq_dtype; 16-bit patterns behind void *), sums, statistics and norms are binary32, each result is rounded once, to
- * nearest even.  Index arrays are DEVICE int32; the host does not see their values, so what they hold is bounded in the
+ * nearest even; what an operator rounds to 16 bits on the way is said with it.  Outputs overlap no input but where it is
+ * said.  Index arrays are DEVICE int32; the host does not see their values, so what they hold is bounded in the
  * kernels: no value of theirs makes a kernel read or write outside the buffers described here.
  */
 typedef enum { BCQ_F16 = 0, BCQ_BF16 = 1 } bcq_dtype;
@@ -322,13 +323,19 @@ bcq_status bcq_rotate(const bcq_cache *cache, int32_t tokens, int32_t q_heads, c
  * sees the keys j < kv_len[r] with j <= p (causal) and j > p - window (window > 0, causal only):
  *     out = sum_j softmax_j(scale * q . k_j) v_j
  * Query head h uses the cache's head h / (q_heads / kv_heads).  A token that sees no key gets zeros; keys that a token does
- * not see have no part in its result whatever they hold (infinities and NaN too).
+ * not see have no part in its result whatever they hold (infinities and NaN too), and an infinity among the values that it
+ * sees is one of its result.  Rows of out that belong to no request are left alone.
+ * The weights (exponentials of binary32) are summed in binary32; they meet the values as the sum of two 16-bit numbers where a
+ * request has at most 16 rows (new tokens times q_heads / kv_heads), as one 16-bit number in chunks of more, which adds about
+ * as much to a result as its own rounding does.  binary16: weights below 2^-21 (chunks) or 2^-28 of a row's largest have fewer
+ * bits than the type, and none below 2^-32 or 2^-39.
  *   q, out    DEVICE [tokens] rows of q_heads * head_dim, strides ld_q, ld_out (multiples of 8), 16-byte aligned
  *   q_start   DEVICE [requests + 1], kv_len DEVICE [requests]
  *   pages     DEVICE [requests] rows of max_pages page numbers, row stride max_pages; kv_len[r] <= max_pages * page_size
  *   max_new   no request has more new tokens than this (those behind it are not computed)
  *   scale     > 0
- *   workspace DEVICE, bcq_attend_workspace_bytes(...) bytes, 16-byte aligned; scratch, no init, used by one call at a time
+ *   workspace DEVICE, bcq_attend_workspace_bytes(...) bytes, 16-byte aligned (NULL if that is 0); scratch, no init, used by one
+ *             call at a time
  * tokens = 0 or requests = 0 launches nothing.
  */
 size_t bcq_attend_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_pages,
@@ -348,7 +355,8 @@ bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v
  *   adapter DEVICE [tokens] int32
  *   X       DEVICE [tokens] rows of N, stride ldx;  base, Y DEVICE [tokens] rows of M, strides ld_base, ldy; Y may be base,
  *           with ldy = ld_base if tokens > 1
- *   workspace DEVICE, bcq_lora_workspace_bytes(desc, tokens) bytes, 16-byte aligned; scratch, no init
+ *   workspace DEVICE, bcq_lora_workspace_bytes(desc, tokens) bytes, 16-byte aligned (NULL if that is 0); scratch, no init
+ * A X is a binary32 sum and meets B in at least 21 bits of a token's largest element of it.
  * N and max_rank multiples of 8, max_rank at most BCQ_MAX_RANK; A, B, X 16-byte aligned, ldx a multiple of 8; base and Y
  * aligned to 2 bytes, any M and strides (multiples of 8 elements and 16 bytes are faster).  tokens = 0 launches nothing.
  */

@@ -9,13 +9,14 @@
 //    both kinds of reads find all banks.
 //  * S^T = K Q^T with Q in registers: a lane has one row's scores, 32 for a block of 64 keys, so a row's maximum and sum need one exchange between
 //    two lanes; its weights, rounded to 16 bits, are the operand of O^T = V^T P^T as they are, for the keys of a product may be numbered in any order.
-//    V's side of it comes from the transposing read.  The rounding of the weights adds to a result what its own rounding does (1.4 times in the mean square).  Weights are taken relative to a running maximum (Weights in
-//    bcq_attend.h).
+//    V's side of it comes from the transposing read.  The rounding of the weights adds to a result what its own rounding does (1.3 times in the mean square); held as
+//    two numbers they cost 8 to 30 % from two waves' rows on (5 tokens over 131077 keys, 8 query heads a kv head: 116 us against 97).  Weights are taken
+//    relative to a running maximum (Weights in bcq_attend.h).
 //  * Blocks that all of a wave's rows see have no masks, those that none sees are left out.
 //  * Few tiles and many keys: the keys of a tile are cut into `parts`, whose sums a second launch joins.
 //
-// Measured: 2048 tokens over 8192 keys, 56 heads of 128, bfloat16: 440 us, 957 TFLOP/s, three quarters of what a large library product reaches; the matrix
-// pipe is busy 52 % of the time and the vector pipe 39 %, no bank conflicts, two waves per SIMD as the registers allow (216 of 256).  Sorting the
+// Measured: 2048 tokens over 8192 keys, 56 heads of 128, bfloat16: 434 us, 970 TFLOP/s, three quarters of what a large library product reaches; the matrix
+// pipe is busy 53 % of the time and the vector pipe 39 %, no bank conflicts, two waves per SIMD as the registers allow (226 of 256).  Sorting the
 // exponentials of 32 keys among the matrix instructions of the others by hand took 487 us against 455, a higher priority for a wave in its matrix instructions 456.
 // A first kernel without matrix instructions took 62 ms.  Five tokens over 131077 keys (537 MB): 86 us and 6 for the join, 6.2 TB/s.
 #include "bcq_attend.h"
