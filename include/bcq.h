@@ -372,6 +372,56 @@ bcq_status bcq_lora(const bcq_adapters *desc, const void *A, const void *B, cons
                     void *Y, int64_t ldy, void *workspace, void *stream);
 
 /*
+ * From the lengths of requests to what a step's operators read: the row starts, lengths, positions and slots of its new tokens, and the table of
+ * pages, for which free pages are taken and pages that are not needed any more given back.  Request r has cached[r] tokens in the cache (fewer than
+ * before where drafts were rejected, none where it is over) and brings fresh[r] new ones.  Its row of the table holds held[r] pages, the first fixed[r]
+ * of which (a prompt that others have too) are not its own and are neither taken nor given back.
+ *     want     = max(ceil((cached + fresh) / page_size), fixed)
+ *     q_start  = sums of fresh, no more than `tokens`; kv_len = cached + fresh
+ *     rows of a request: position cached + i, slot pages[r][position / page_size] * page_size + position % page_size, owner r
+ *     rows behind the last request's: position 0, slot -1, owner -1
+ * First the pages from `want` on go onto the stack free_pages (free_count of them lie there), request by request; then the missing ones are taken from
+ * its top, request by request, as long as it has all that a request needs.  A request behind the first that it has not gets none either.
+ *   lack      0; or the pages that a request needed and did not get; or -1 where its row of the table is too short or the rows up to and with its
+ *             own are more than `tokens`.  Unless it is 0 the request keeps what it held, its kv_len is 0 and its rows have slot -1, so that
+ *             bcq_rotate stores nothing and bcq_attend gives zeros.
+ *   held_out, free_count_out  the counts after the step; may be held and free_count
+ *   pages     DEVICE [requests] rows of max_pages, in place (entries behind held_out are left as they are); free_pages DEVICE [num_pages], in place
+ *   cached, fresh, held, fixed (or NULL: 0), kv_len, lack, held_out DEVICE [requests]; q_start DEVICE [requests + 1]
+ *   positions, slots, owner DEVICE [tokens]: the rows of the batch, which may be more than there are
+ * Negative numbers count as 0, held as no more than max_pages, fixed as no more than held.  page_size a power of two, at most 65536.
+ */
+typedef struct bcq_page_table {
+    int32_t page_size, num_pages;
+    int32_t requests, max_pages;
+} bcq_page_table;
+
+bcq_status bcq_plan(const bcq_page_table *table, int32_t *pages, const int32_t *held, const int32_t *fixed, int32_t *free_pages,
+                    const int32_t *free_count, const int32_t *cached, const int32_t *fresh, int32_t tokens, int32_t *q_start, int32_t *kv_len,
+                    int32_t *lack, int32_t *held_out, int32_t *free_count_out, int32_t *positions, int32_t *slots, int32_t *owner, void *stream);
+
+/*
+ * The next tokens from logits.  Row by row, m the largest logit, in the order of descending logits and, among equal ones, ascending index:
+ *     w_i = exp((x_i - m) / temperature)
+ *     the first top_k (all if top_k <= 0); S their weight
+ *     of these the ones before which less than top_p S stands, always the first (all if top_p >= 1)
+ *     of these the ones with w_i >= min_p (all if min_p <= 0; 1 if it is more)
+ *     M the weight of what is left; the token is the first up to and with which more than uniform * M stands, its probability w / M
+ * Where the temperature is not above 0, or top_k is 1, the token is the first of the largest logits, with probability 1.  A logit that is NaN or -infinity
+ * has no part; where +infinity occurs nothing else has; a row without any part gets token -1 and probability 0.  Weights and sums are binary64.
+ *   logits      DEVICE [rows] of vocab elements of `dtype` (a bcq_dtype), row stride ld >= vocab; aligned to 2 bytes (rows that begin at 16 are faster)
+ *   temperature, uniform DEVICE [rows] binary32 (uniform is bounded to 0 .. 1 - 2^-24); top_k DEVICE [rows] int32, top_p, min_p DEVICE [rows] binary32,
+ *               or NULL (all)
+ *   token       DEVICE [rows] int32; probability DEVICE [rows] binary32, or NULL
+ *   workspace   DEVICE, bcq_sample_workspace_bytes(rows, vocab) bytes, 16-byte aligned (NULL if that is 0); scratch, no init, used by one call at a time
+ * rows = 0 launches nothing.
+ */
+#define BCQ_MAX_VOCAB (1 << 22)
+size_t bcq_sample_workspace_bytes(int32_t rows, int32_t vocab);
+bcq_status bcq_sample(int32_t dtype, int32_t rows, int32_t vocab, const void *logits, int64_t ld, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *probability, void *workspace, void *stream);
+
+/*
  * Streaming-read probe: reads `bytes` (a multiple of 16) of DEVICE memory with
  * the same 128-bit coalesced loads and launch shape the GEMV uses and writes a
  * 4-byte checksum per workgroup to `sink` (DEVICE, at least

@@ -19,11 +19,13 @@ EXPORTS = ["bcq_packed_bytes", "bcq_workspace_bytes", "bcq_workspace_init", "bcq
            "bcq_pack_rows", "bcq_from_linear", "bcq_quant_workspace_bytes", "bcq_quant_hessian", "bcq_quant_factor_workspace_bytes", "bcq_quant_factor", "bcq_quant_search",
            "bcq_quant_gptq", "bcq_from_linear_rows", "bcq_unpack", "bcq_gemv", "bcq_gemv_noalloc", "bcq_gemm_skinny", "bcq_read_probe_sink_bytes",
            "bcq_read_probe", "bcq_set_option", "bcq_status_string",
-           "bcq_rotate", "bcq_attend_workspace_bytes", "bcq_attend", "bcq_lora_workspace_bytes", "bcq_lora"]
+           "bcq_rotate", "bcq_attend_workspace_bytes", "bcq_attend", "bcq_lora_workspace_bytes", "bcq_lora",
+           "bcq_plan", "bcq_sample_workspace_bytes", "bcq_sample"]
 
 BCQ_F16, BCQ_BF16 = range(2)
 BCQ_MAX_HEAD_DIM = 256
 BCQ_MAX_RANK = 256
+BCQ_MAX_VOCAB = 1 << 22
 
 
 class Desc(ctypes.Structure):
@@ -44,6 +46,11 @@ class AdaptersDesc(ctypes.Structure):
     """struct bcq_adapters"""
     _fields_ = [("dtype", ctypes.c_int32), ("count", ctypes.c_int32), ("max_rank", ctypes.c_int32),
                 ("M", ctypes.c_int32), ("N", ctypes.c_int32)]
+
+
+class PageTableDesc(ctypes.Structure):
+    """struct bcq_page_table"""
+    _fields_ = [("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("requests", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
 
 
 class BcqError(RuntimeError):
@@ -111,6 +118,9 @@ def lib():
         L.bcq_attend.restype = i32
         L.bcq_attend.argtypes = [cp, vp, vp, i32, i32, i32, vp, i64, vp, vp, vp, i32, i32, f32, i32, i32, vp, i64, vp, vp]
         L.bcq_lora_workspace_bytes.restype, L.bcq_lora_workspace_bytes.argtypes = sz, [ap, i32]
+        L.bcq_plan.restype, L.bcq_plan.argtypes = i32, [ctypes.POINTER(PageTableDesc)] + [vp] * 7 + [i32] + [vp] * 9
+        L.bcq_sample_workspace_bytes.restype, L.bcq_sample_workspace_bytes.argtypes = sz, [i32, i32]
+        L.bcq_sample.restype, L.bcq_sample.argtypes = i32, [i32, i32, i32, vp, i64] + [vp] * 9
         L.bcq_lora.restype, L.bcq_lora.argtypes = i32, [ap, vp, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp]
         L.bcq_status_string.restype, L.bcq_status_string.argtypes = ctypes.c_char_p, [i32]
         _lib = L
@@ -281,6 +291,22 @@ def lora_workspace_bytes(desc, tokens):
 def lora(desc, A, B, rank, scale, tokens, adapter, X, ldx, base, ld_base, Y, ldy, workspace, stream=None):
     _check(lib().bcq_lora(ctypes.byref(desc), _ptr(A), _ptr(B), _ptr(rank), _ptr(scale), tokens, _ptr(adapter), _ptr(X), ldx,
                           _ptr(base), ld_base, _ptr(Y), ldy, _ptr(workspace), _stream(stream)), "bcq_lora")
+
+
+def plan(table, pages, held, fixed, free_pages, free_count, cached, fresh, tokens, q_start, kv_len, lack, held_out, free_count_out, positions, slots, owner,
+         stream=None):
+    _check(lib().bcq_plan(ctypes.byref(table), _ptr(pages), _ptr(held), _ptr(fixed), _ptr(free_pages), _ptr(free_count), _ptr(cached), _ptr(fresh), tokens,
+                          _ptr(q_start), _ptr(kv_len), _ptr(lack), _ptr(held_out), _ptr(free_count_out), _ptr(positions), _ptr(slots), _ptr(owner),
+                          _stream(stream)), "bcq_plan")
+
+
+def sample_workspace_bytes(rows, vocab):
+    return int(lib().bcq_sample_workspace_bytes(rows, vocab))
+
+
+def sample(dtype, rows, vocab, logits, ld, temperature, top_k, top_p, min_p, uniform, token, probability, workspace, stream=None):
+    _check(lib().bcq_sample(dtype, rows, vocab, _ptr(logits), ld, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(uniform), _ptr(token),
+                            _ptr(probability), _ptr(workspace), _stream(stream)), "bcq_sample")
 
 
 def set_option(name, value):

@@ -111,7 +111,7 @@ def build(verbose=False, extra_flags=()):
         raise subprocess.CalledProcessError(proc.returncode, cmd)
     res = kernel_resources(proc.stderr)
     hot = {k: v for k, v in res.items() if "bcq_gemv" in k or "bcq_skinny" in k or "bcq_few" in k or "bcq_wide" in k
-           or "bcq_attend" in k or "bcq_rotate" in k or "bcq_lora" in k}
+           or "bcq_attend" in k or "bcq_rotate" in k or "bcq_lora" in k or "bcq_plan" in k or "bcq_sample" in k}
     if not hot:
         raise RuntimeError("no resource remarks for the compute kernels: cannot check for spills")
     bad = {k: v for k, v in hot.items()

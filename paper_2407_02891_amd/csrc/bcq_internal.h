@@ -111,6 +111,30 @@ struct LoraArgs {
 size_t lora_workspace_bytes(const bcq_adapters &d, int tokens);
 hipError_t launch_lora(const LoraArgs &a, hipStream_t stream);
 
+struct PlanArgs {
+    int *pages;
+    const int *held, *fixed;
+    int *free_pages;
+    const int *free_count, *cached, *fresh;
+    int *q_start, *kv_len, *lack, *held_out, *free_count_out, *positions, *slots, *owner;
+    int page_size, page_shift, num_pages, max_pages, requests, tokens;
+};
+hipError_t launch_plan(const PlanArgs &a, hipStream_t stream);
+
+struct SampleArgs {
+    const uint16_t *logits;
+    long long ld;
+    const float *temperature, *top_p, *min_p, *uniform;
+    const int *top_k;
+    int *token;
+    float *probability;
+    int rows, vocab;
+    bool bf16;
+    void *workspace;
+};
+size_t sample_workspace_bytes(int rows, int vocab);
+hipError_t launch_sample(const SampleArgs &a, hipStream_t stream);
+
 constexpr int kProbeBlocks = 512;  // the GEMV's grid: two workgroups per CU
 
 constexpr int kTraceSlots = 16;  // words per wave in the tracing build's timeline buffer

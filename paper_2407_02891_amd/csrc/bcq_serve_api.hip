@@ -138,4 +138,53 @@ bcq_status bcq_lora(const bcq_adapters *desc, const void *A, const void *B, cons
     return launch_lora(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
 }
 
+bcq_status bcq_plan(const bcq_page_table *table, int32_t *pages, const int32_t *held, const int32_t *fixed, int32_t *free_pages, const int32_t *free_count,
+                    const int32_t *cached, const int32_t *fresh, int32_t tokens, int32_t *q_start, int32_t *kv_len, int32_t *lack, int32_t *held_out,
+                    int32_t *free_count_out, int32_t *positions, int32_t *slots, int32_t *owner, void *stream)
+{
+    if (!table || table->page_size < 1 || table->num_pages < 1 || table->requests < 0 || table->max_pages < 1 || tokens < 0) return BCQ_ERR_INVALID_ARG;
+    if (table->page_size > 65536 || (table->page_size & (table->page_size - 1)) || tokens > kMaxTokens || table->requests > kMaxTokens) return BCQ_ERR_UNSUPPORTED;
+    if ((int64_t)table->num_pages * table->page_size > 0x7fffffffLL || (int64_t)table->max_pages * table->page_size > (1 << 30) ||
+        (int64_t)table->requests * table->max_pages > 0x7fffffffLL)
+        return BCQ_ERR_UNSUPPORTED;  // slots, keys of a request, and pages of all requests are int
+    if (!free_pages || !free_count || !q_start || !free_count_out) return BCQ_ERR_INVALID_ARG;
+    if (table->requests > 0 && (!pages || !held || !cached || !fresh || !kv_len || !lack || !held_out)) return BCQ_ERR_INVALID_ARG;
+    if (tokens > 0 && (!positions || !slots || !owner)) return BCQ_ERR_INVALID_ARG;
+    for (const int32_t *p : {(const int32_t *)pages, held, fixed, (const int32_t *)free_pages, free_count, cached, fresh, (const int32_t *)q_start,
+                             (const int32_t *)kv_len, (const int32_t *)lack, (const int32_t *)held_out, (const int32_t *)free_count_out,
+                             (const int32_t *)positions, (const int32_t *)slots, (const int32_t *)owner})
+        if (!aligned(p, 4)) return BCQ_ERR_INVALID_ARG;
+    PlanArgs a{pages, held, fixed, free_pages, free_count, cached, fresh, q_start, kv_len, lack, held_out, free_count_out, positions, slots, owner,
+               table->page_size, __builtin_ctz(table->page_size), table->num_pages, table->max_pages, table->requests, tokens};
+    return launch_plan(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
+}
+
+static bcq_status sample_shape(int32_t rows, int32_t vocab)
+{
+    if (rows < 0 || vocab < 1) return BCQ_ERR_INVALID_ARG;
+    return rows > kMaxTokens || vocab > BCQ_MAX_VOCAB ? BCQ_ERR_UNSUPPORTED : BCQ_OK;
+}
+
+size_t bcq_sample_workspace_bytes(int32_t rows, int32_t vocab)
+{
+    return sample_shape(rows, vocab) != BCQ_OK || rows == 0 ? 0 : sample_workspace_bytes(rows, vocab);
+}
+
+bcq_status bcq_sample(int32_t dtype, int32_t rows, int32_t vocab, const void *logits, int64_t ld, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *probability, void *workspace, void *stream)
+{
+    if (dtype != BCQ_F16 && dtype != BCQ_BF16) return BCQ_ERR_INVALID_ARG;
+    const bcq_status why = sample_shape(rows, vocab);
+    if (why != BCQ_OK) return why;
+    if (ld < vocab) return BCQ_ERR_INVALID_ARG;
+    if (rows == 0) return BCQ_OK;
+    if (!logits || !temperature || !uniform || !token) return BCQ_ERR_INVALID_ARG;
+    if (!aligned(logits, 2) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(uniform, 4) ||
+        !aligned(token, 4) || !aligned(probability, 4))
+        return BCQ_ERR_INVALID_ARG;
+    if (sample_workspace_bytes(rows, vocab) > 0 && (!workspace || !aligned(workspace, 16))) return BCQ_ERR_WORKSPACE;
+    SampleArgs a{half(logits), ld, temperature, top_p, min_p, uniform, top_k, token, probability, rows, vocab, dtype == BCQ_BF16, workspace};
+    return launch_sample(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
+}
+
 }  // extern "C"

@@ -20,6 +20,9 @@ struct {
     decltype(&bcq_attend_workspace_bytes) attend_workspace_bytes;
     decltype(&bcq_lora) lora;
     decltype(&bcq_lora_workspace_bytes) lora_workspace_bytes;
+    decltype(&bcq_plan) plan;
+    decltype(&bcq_sample) sample;
+    decltype(&bcq_sample_workspace_bytes) sample_workspace_bytes;
 } g_bcq;
 
 // A refusal or a failed call, on its way to Python.
@@ -55,6 +58,15 @@ struct Place {
         if (t.scalar_type() != at::kInt || t.dim() != 1 || t.size(0) != n || t.device() != device || !t.is_contiguous())
             refuse(where, std::string(name) + ": contiguous int32 of " + std::to_string(n) + " on " + device.str());
         return static_cast<const int32_t *>(t.data_ptr());
+    }
+    template <class T>
+    T *vector(PyObject *o, const char *name, int64_t n, at::ScalarType of) const  // null for None
+    {
+        if (o == Py_None) return nullptr;
+        const at::Tensor &t = tensor(o, where, name);
+        if (t.scalar_type() != of || t.dim() != 1 || t.size(0) != n || t.device() != device || !t.is_contiguous())
+            refuse(where, std::string(name) + ": contiguous " + c10::toString(of) + " [" + std::to_string(n) + "] on " + device.str());
+        return static_cast<T *>(t.data_ptr());
     }
     const void *weight(PyObject *o, const char *name, int64_t n) const
     {
@@ -100,7 +112,10 @@ void succeeded(bcq_status status, const char *where)
 }
 
 // One of the functions below, with its argument count checked and what it throws turned into Python's errors.
-template <int COUNT, at::Tensor (*CALL)(PyObject *const *)>
+PyObject *wrapped(const at::Tensor &t) { return THPVariable_Wrap(t); }
+PyObject *wrapped(PyObject *o) { return o; }
+
+template <int COUNT, auto CALL>
 PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (n != COUNT) {
@@ -108,7 +123,7 @@ PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n)
         return nullptr;
     }
     try {
-        return THPVariable_Wrap(CALL(args));
+        return wrapped(CALL(args));
     } catch (const Refused &r) {
         if (!PyErr_Occurred()) {
             PyObject *what = Py_BuildValue("(is)", r.status, r.where.c_str());
@@ -218,6 +233,109 @@ at::Tensor add(PyObject *const *a)
     return out;
 }
 
+// step(desc, pages, held, fixed, free_pages, free_count, cached, fresh, tokens, trial, out, names, stream): a dict of the tensors that `names` names, in the order
+// of the entry point's arguments; those of `out`, or new ones.
+PyObject *step(PyObject *const *a)
+{
+    const char *const where = "PageTable.step";
+    const bcq_page_table *const d = address<const bcq_page_table>(a[0]);
+    const at::Tensor &pages = tensor(a[1], where, "pages");
+    const Place place{at::kInt, pages.device(), where};
+    const c10::DeviceGuard there(place.device);
+    const int64_t R = d->requests, T = int32(a[8], where, "tokens");
+    if (T < 0) refuse(where, "tokens: negative");
+    int32_t *const held = place.vector<int32_t>(a[2], "held", R, at::kInt), *const fixed = place.vector<int32_t>(a[3], "fixed", R, at::kInt);
+    int32_t *const free_pages = place.vector<int32_t>(a[4], "free", d->num_pages, at::kInt), *const free_count = place.vector<int32_t>(a[5], "free_count", 1, at::kInt);
+    const int32_t *const cached = place.ints(a[6], "cached", R), *const fresh = place.ints(a[7], "fresh", R);
+    const bool trial = truth(a[9]);
+    // q_start, kv_len, lack, held, free_count, positions, slots, owner
+    constexpr int kOut = 8;
+    const int64_t sizes[kOut] = {R + 1, R, R, R, 1, T, T, T};
+    PyObject *const names = a[11];
+    if (!PyTuple_Check(names) || PyTuple_GET_SIZE(names) != kOut) refuse(where, "names: of eight tensors");
+    int32_t *to[kOut];
+    PyObject *out = a[10];
+    const auto mine = [&](int i) { return !trial && (i == 3 || i == 4); };  // the table's own counts
+    if (out != Py_None) {
+        if (!PyDict_Check(out)) refuse(where, "out: a dict as an earlier step returned it");
+        for (int i = 0; i < kOut; ++i) {
+            PyObject *const t = PyDict_GetItem(out, PyTuple_GET_ITEM(names, i));
+            const char *const name = PyUnicode_AsUTF8(PyTuple_GET_ITEM(names, i));
+            if (!t || t == Py_None) refuse(where, std::string("out: without ") + (name ? name : "a tensor"));
+            to[i] = place.vector<int32_t>(t, name ? name : "out", sizes[i], at::kInt);
+        }
+        if (mine(3) ? to[3] != held || to[4] != free_count : to[3] == held || to[4] == free_count)
+            refuse(where, mine(3) ? "out: held and free_count of a trial" : "out: the table's own held and free_count, which a trial leaves");
+        Py_INCREF(out);
+    } else {
+        int64_t total = 0;
+        for (int i = 0; i < kOut; ++i) total += mine(i) ? 0 : (sizes[i] + 3) & ~int64_t(3);  // (each at 16 bytes)
+        const at::Tensor all = at::empty({total}, at::TensorOptions().dtype(at::kInt).device(place.device));
+        out = PyDict_New();
+        if (!out) throw Refused{-1, ""};
+        int64_t from = 0;
+        for (int i = 0; i < kOut; ++i) {
+            PyObject *t;
+            if (mine(i)) {
+                t = a[i == 3 ? 2 : 5];
+                Py_INCREF(t);
+                to[i] = i == 3 ? held : free_count;
+            } else {
+                const at::Tensor part = all.narrow(0, from, sizes[i]);
+                from += (sizes[i] + 3) & ~int64_t(3);
+                to[i] = static_cast<int32_t *>(part.data_ptr());
+                t = THPVariable_Wrap(part);
+            }
+            if (t) PyDict_SetItem(out, PyTuple_GET_ITEM(names, i), t);
+            Py_XDECREF(t);
+        }
+    }
+    const bcq_status status = g_bcq.plan(d, static_cast<int32_t *>(pages.data_ptr()), held, fixed, free_pages, free_count, cached, fresh, (int32_t)T, to[0], to[1],
+                                         to[2], to[3], to[4], to[5], to[6], to[7], address<void>(a[12]));
+    if (status != BCQ_OK) {
+        Py_DECREF(out);
+        throw Refused{status, where};
+    }
+    return out;
+}
+
+// draw(temperature, top_k, top_p, min_p, logits, uniform, out, stream): (tokens, probabilities)
+PyObject *draw(PyObject *const *a)
+{
+    const char *const where = "Sampler.draw";
+    const at::Tensor &temperature = tensor(a[0], where, "temperature"), &logits = tensor(a[4], where, "logits");
+    if (logits.scalar_type() != at::kHalf && logits.scalar_type() != at::kBFloat16) refuse(where, "logits: float16 or bfloat16");
+    const Place place{logits.scalar_type(), temperature.device(), where};
+    const c10::DeviceGuard there(place.device);
+    const int64_t R = temperature.size(0);
+    if (logits.dim() != 2 || logits.size(1) > INT32_MAX || logits.size(1) < 1) refuse(where, "logits: [rows][vocabulary]");
+    const int64_t V = logits.size(1), ld = place.rows(logits, "logits", R, V);
+    const float *const top_p = place.vector<float>(a[2], "top_p", R, at::kFloat), *const min_p = place.vector<float>(a[3], "min_p", R, at::kFloat);
+    const int32_t *const top_k = place.vector<int32_t>(a[1], "top_k", R, at::kInt);
+    const float *const uniform = place.vector<float>(tensor(a[5], where, "uniform").defined() ? a[5] : Py_None, "uniform", R, at::kFloat);
+    at::Tensor token, probability;
+    if (a[6] == Py_None) {
+        token = at::empty({R}, at::TensorOptions().dtype(at::kInt).device(place.device));
+        probability = at::empty({R}, at::TensorOptions().dtype(at::kFloat).device(place.device));
+    } else {
+        if (!PyTuple_Check(a[6]) || PyTuple_GET_SIZE(a[6]) != 2) refuse(where, "out: (tokens, probabilities)");
+        place.ints(PyTuple_GET_ITEM(a[6], 0), "out[0]", R);
+        token = tensor(PyTuple_GET_ITEM(a[6], 0), where, "out[0]"), probability = tensor(PyTuple_GET_ITEM(a[6], 1), where, "out[1]");
+        place.vector<float>(PyTuple_GET_ITEM(a[6], 1), "out[1]", R, at::kFloat);
+    }
+    const size_t bytes = g_bcq.sample_workspace_bytes((int32_t)R, (int32_t)V);
+    const at::Tensor workspace = bytes ? place.scratch(bytes) : at::Tensor();
+    succeeded(g_bcq.sample(place.type == at::kBFloat16 ? BCQ_BF16 : BCQ_F16, (int32_t)R, (int32_t)V, logits.data_ptr(), ld,
+                           place.vector<float>(a[0], "temperature", R, at::kFloat), top_k, top_p, min_p, uniform, static_cast<int32_t *>(token.data_ptr()),
+                           static_cast<float *>(probability.data_ptr()), bytes ? workspace.data_ptr() : nullptr, address<void>(a[7])),
+              where);
+    PyObject *const t = THPVariable_Wrap(token), *const p = THPVariable_Wrap(probability);
+    PyObject *const both = t && p ? PyTuple_Pack(2, t, p) : nullptr;
+    Py_XDECREF(t);
+    Py_XDECREF(p);
+    return both;
+}
+
 // bind(handle of libbcq, BcqError)
 PyObject *bind(PyObject *, PyObject *args)
 {
@@ -231,14 +349,15 @@ PyObject *bind(PyObject *, PyObject *args)
         return to != nullptr;
     };
     if (!find(g_bcq.rotate, "bcq_rotate") || !find(g_bcq.attend, "bcq_attend") || !find(g_bcq.attend_workspace_bytes, "bcq_attend_workspace_bytes") ||
-        !find(g_bcq.lora, "bcq_lora") || !find(g_bcq.lora_workspace_bytes, "bcq_lora_workspace_bytes"))
+        !find(g_bcq.lora, "bcq_lora") || !find(g_bcq.lora_workspace_bytes, "bcq_lora_workspace_bytes") ||
+        !find(g_bcq.plan, "bcq_plan") || !find(g_bcq.sample, "bcq_sample") || !find(g_bcq.sample_workspace_bytes, "bcq_sample_workspace_bytes"))
         return nullptr;
     Py_INCREF(error);
     Py_XSETREF(g_error, error);
     Py_RETURN_NONE;
 }
 
-template <int COUNT, at::Tensor (*CALL)(PyObject *const *)>
+template <int COUNT, auto CALL>
 PyCFunction fast()
 {
     return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(&guarded<COUNT, CALL>));
@@ -248,6 +367,8 @@ PyMethodDef g_methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                            {"rotate", fast<13, rotate>(), METH_FASTCALL, nullptr},
                            {"attend", fast<13, attend>(), METH_FASTCALL, nullptr},
                            {"add", fast<10, add>(), METH_FASTCALL, nullptr},
+                           {"step", fast<13, step>(), METH_FASTCALL, nullptr},
+                           {"draw", fast<8, draw>(), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_serving", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

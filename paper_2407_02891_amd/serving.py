@@ -1,5 +1,5 @@
-"""Objects over the serving operators of include/bcq.h: a paged key/value cache that is appended to and attended, and the adapters of
-many requests beside a shared projection.  They hold tensors and descriptors and call the C entry points on torch's current stream (no
+"""Objects over the serving operators of include/bcq.h: a paged key/value cache that is appended to and attended, the adapters of
+many requests beside a shared projection, the table of a cache's pages from one step to the next, and the drawing of tokens from logits.  They hold tensors and descriptors and call the C entry points on torch's current stream (no
 arithmetic here).  Scratch memory comes from torch's allocator for each call, so calls on different streams share none of it; tensors
 that another stream wrote or will free follow torch's usual rules (wait_stream, record_stream).
 
@@ -97,3 +97,56 @@ class Adapters:
         """bcq_lora: base + scale * B (A X) by the adapter of each row (int32 [tokens]; any number outside 0 .. count - 1: none).  `out` may
         be base."""
         return self._native.add(self._desc, self.A, self.B, self._rank, self._scale, X, adapter, base, out, B.raw_stream(self._index))
+
+
+class PageTable:
+    """Which pages of a pool each request has: pages int32 [requests][max_pages] (the first held[r] of row r are the request's), the stack of free ones
+    (int32 [pages of the pool], the first free_count[0] of them), held int32 [requests], free_count int32 [1]."""
+
+    STEP = ("q_start", "kv_len", "lack", "held", "free_count", "positions", "slots", "owner")
+
+    def __init__(self, pages, held, free, free_count, page_size):
+        where = "PageTable"
+        _need(pages.dim() == 2 and pages.dtype == torch.int32 and pages.is_contiguous(), where, "pages: contiguous int32 [requests][max_pages]")
+        _need(pages.is_cuda, where, f"pages: on a GPU, not on {pages.device}")
+        for name, t, n in (("held", held, pages.shape[0]), ("free", free, None), ("free_count", free_count, 1)):
+            _need(t.dim() == 1 and t.dtype == torch.int32 and t.is_contiguous() and t.device == pages.device and (n is None or t.shape[0] == n), where,
+                  f"{name}: contiguous int32 [{'pages of the pool' if n is None else n}] on {pages.device}")
+        self.pages, self.held, self.free, self.free_count, self.page_size, self.device = pages, held, free, free_count, int(page_size), pages.device
+        self.desc = B.PageTableDesc(self.page_size, free.shape[0], *pages.shape)
+        self._desc, self._index, self._native = ctypes.addressof(self.desc), pages.get_device(), _load()
+
+    @classmethod
+    def empty(cls, requests, max_pages, num_pages, page_size, device="cuda"):
+        """All pages of the pool free, none held; page 0 is taken first."""
+        return cls(torch.zeros((requests, max_pages), dtype=torch.int32, device=device), torch.zeros(requests, dtype=torch.int32, device=device),
+                   torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device), torch.full((1,), num_pages, dtype=torch.int32, device=device), page_size)
+
+    def step(self, cached, fresh, tokens, fixed=None, out=None, trial=False):
+        """bcq_plan: cached[r] tokens of request r are in the cache, fresh[r] more come with a batch of `tokens` rows (int32 [requests]); the first fixed[r] pages of a
+        row are not its own.  Returns a dict of q_start, kv_len, lack, held, free_count, positions, slots, owner (`out`: one that an earlier step returned, whose
+        tensors are written again).  held and free_count are the table's own and move with the step.  With `trial` they stay, and those that the step would leave are
+        tensors of their own: what a step would take and who would lack pages, before it is made (entries of `pages` behind held, and of `free` behind free_count,
+        are scratch)."""
+        return self._native.step(self._desc, self.pages, self.held, fixed, self.free, self.free_count, cached, fresh, tokens, trial, out, self.STEP,
+                                 B.raw_stream(self._index))
+
+
+class Sampler:
+    """Settings of the rows of a batch: temperature float32 [rows] (not above 0: the largest logit), top_k int32 (0: all), top_p (1: all) and min_p (0: all)
+    float32 [rows], or None."""
+
+    def __init__(self, temperature, top_k=None, top_p=None, min_p=None):
+        where = "Sampler"
+        _need(temperature.dim() == 1 and temperature.dtype == torch.float32 and temperature.is_contiguous(), where, "temperature: contiguous float32 [rows]")
+        _need(temperature.is_cuda, where, f"temperature: on a GPU, not on {temperature.device}")
+        for name, t, dtype in (("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+            _need(t is None or (t.shape == temperature.shape and t.dtype == dtype and t.is_contiguous() and t.device == temperature.device), where,
+                  f"{name}: contiguous {dtype} [rows] on {temperature.device}")
+        self.temperature, self.top_k, self.top_p, self.min_p = temperature, top_k, top_p, min_p
+        self._index, self._native = temperature.get_device(), _load()
+
+    def draw(self, logits, uniform, out=None):
+        """bcq_sample: logits [rows][vocabulary] float16 or bfloat16, uniform float32 [rows] in 0 .. 1.  Returns (tokens int32 [rows], -1 where a row has nothing to
+        draw from; their probabilities among what the filters keep, float32 [rows]), `out`."""
+        return self._native.draw(self.temperature, self.top_k, self.top_p, self.min_p, logits, uniform, out, B.raw_stream(self._index))

@@ -1,0 +1,89 @@
+"""Argument checks of the table of pages and of the draw: all before any launch, so none of this needs a GPU."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2407_02891_amd as bcq
+from paper_2407_02891_amd import binding as B
+
+OK = 0x1000
+
+
+def plan(t=(), **kw):
+    d = dict(page_size=16, num_pages=1000, requests=8, max_pages=40)
+    d.update(t)
+    a = dict(pages=OK, held=OK, fixed=OK, free=OK, free_count=OK, cached=OK, fresh=OK, tokens=8, q_start=OK, kv_len=OK, lack=OK, held_out=OK, count_out=OK,
+             positions=OK, slots=OK, owner=OK)
+    a.update(kw)
+    return bcq.lib().bcq_plan(ctypes.byref(B.PageTableDesc(*d.values())), *a.values(), None)
+
+
+def sample(**kw):
+    a = dict(dtype=0, rows=4, vocab=100, logits=OK, ld=100, temperature=OK, top_k=OK, top_p=OK, min_p=OK, uniform=OK, token=OK, probability=OK, workspace=OK)
+    a.update(kw)
+    return bcq.lib().bcq_sample(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw", [dict(tokens=-1)] + [{n: v} for n in ("pages", "held", "free", "free_count", "cached", "fresh", "q_start", "kv_len", "lack", "held_out",
+                                                                  "count_out", "positions", "slots", "owner") for v in (None, OK + 2)] + [dict(fixed=OK + 1)])
+def test_plan_refuses(kw):
+    assert plan(**kw) == B.BCQ_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("t", [dict(page_size=0), dict(page_size=-4), dict(num_pages=0), dict(requests=-1), dict(max_pages=0)])
+def test_plan_refuses_tables(t):
+    assert plan(t) == B.BCQ_ERR_INVALID_ARG
+    assert bcq.lib().bcq_plan(None, *[OK] * 7, 8, *[OK] * 8, None) == B.BCQ_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("t,kw", [(dict(page_size=24), {}), (dict(page_size=1 << 17), {}), (dict(num_pages=1 << 28), {}), (dict(max_pages=1 << 27), {}),
+                                  (dict(requests=(1 << 20) + 1), {}), (dict(requests=1 << 20, max_pages=1 << 12), {}), ({}, dict(tokens=(1 << 20) + 1))])
+def test_plan_limits(t, kw):
+    assert plan(t, **kw) == B.BCQ_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=2), dict(dtype=-1), dict(rows=-1), dict(vocab=0), dict(vocab=-5), dict(ld=99), dict(logits=None), dict(temperature=None),
+                                dict(uniform=None), dict(token=None), dict(logits=OK + 1), dict(temperature=OK + 2), dict(top_k=OK + 1), dict(top_p=OK + 2),
+                                dict(min_p=OK + 3), dict(uniform=OK + 2), dict(token=OK + 2), dict(probability=OK + 2)])
+def test_sample_refuses(kw):
+    assert sample(**kw) == B.BCQ_ERR_INVALID_ARG
+
+
+def test_sample_limits():
+    assert sample(rows=(1 << 20) + 1) == B.BCQ_ERR_UNSUPPORTED
+    assert sample(vocab=B.BCQ_MAX_VOCAB + 1, ld=1 << 40) == B.BCQ_ERR_UNSUPPORTED
+    assert sample(rows=0, logits=None, token=None) == B.BCQ_OK   # nothing to do
+    assert sample(vocab=200000, ld=200000, workspace=None) == B.BCQ_ERR_WORKSPACE
+    assert sample(vocab=200000, ld=200000, workspace=OK + 8) == B.BCQ_ERR_WORKSPACE
+
+
+def test_sample_workspace():
+    assert bcq.sample_workspace_bytes(-1, 100) == bcq.sample_workspace_bytes(4, 0) == bcq.sample_workspace_bytes(0, 100) == 0
+    assert bcq.sample_workspace_bytes(4, B.BCQ_MAX_VOCAB + 1) == 0
+    for rows in (1, 2, 100, 1000, 1 << 20):  # bounded, however many rows there are
+        for vocab in (1, 50, 4097, 32000, 65528, 65529, 262144, B.BCQ_MAX_VOCAB):
+            assert 0 <= bcq.sample_workspace_bytes(rows, vocab) < 200 << 20
+    assert bcq.sample_workspace_bytes(1, 262144) > 0
+
+
+def _refused(call):
+    with pytest.raises(bcq.BcqError) as e:
+        call()
+    assert e.value.status == B.BCQ_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("device", ["cpu", "meta"])
+def test_tensors_that_are_not_on_a_gpu(device):
+    pages, held = torch.zeros((2, 4), dtype=torch.int32, device=device), torch.zeros(2, dtype=torch.int32, device=device)
+    _refused(lambda: bcq.PageTable(pages, held, held, held[:1], 16))
+    _refused(lambda: bcq.PageTable.empty(2, 4, 8, 16, device=device))
+    _refused(lambda: bcq.Sampler(torch.ones(2, device=device)))
+
+
+def test_objects_refuse():
+    i = torch.zeros(2, dtype=torch.int32)
+    _refused(lambda: bcq.PageTable(i, i, i, i[:1], 16))
+    _refused(lambda: bcq.PageTable(torch.zeros((4, 2), dtype=torch.int32).t(), i, i, i[:1], 16))
+    _refused(lambda: bcq.Sampler(torch.ones(2, dtype=torch.float64)))
+    _refused(lambda: bcq.Sampler(torch.ones((2, 1))))
