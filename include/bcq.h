@@ -346,6 +346,22 @@ bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v
                       void *out, int64_t ld_out, void *workspace, void *stream);
 
 /*
+ * bcq_attend where groups of requests share their first keys (a long prompt in front of many): group c is the requests group_start[c] ..
+ * group_start[c+1] - 1, whose keys j < shared_len[c] are taken from the row of pages of the first of them and read once for all; the others are each request's own.
+ * The results are those of bcq_attend where the requests' own rows of pages hold the same keys there (what they hold for j < shared_len[c] is not looked at), with the
+ * weights rounded as in its chunks.  Positions, masks, rows that see nothing and rows of nobody as for bcq_attend.
+ *   group_start DEVICE [groups + 1], rising; requests outside of all groups share nothing.  shared_len DEVICE [groups], any number of keys (no whole pages
+ *               needed), bounded to 0 .. max_shared: keys behind that are taken as each request's own
+ *   workspace   DEVICE, bcq_attend_shared_workspace_bytes(...) bytes, 16-byte aligned; scratch, no init, used by one call at a time
+ * The other arguments as for bcq_attend.  tokens = 0 or requests = 0 launches nothing.
+ */
+size_t bcq_attend_shared_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t groups, int32_t q_heads, int32_t max_pages);
+bcq_status bcq_attend_shared(const bcq_cache *cache, const void *k_cache, const void *v_cache, int32_t tokens, int32_t requests, int32_t groups,
+                             int32_t q_heads, const void *q, int64_t ld_q, const int32_t *q_start, const int32_t *kv_len, const int32_t *pages,
+                             int32_t max_pages, int32_t max_new, const int32_t *group_start, const int32_t *shared_len, int32_t max_shared, float scale,
+                             int32_t causal, int32_t window, void *out, int64_t ld_out, void *workspace, void *stream);
+
+/*
  * Low-rank adapters of many requests beside a shared projection of N inputs and M outputs:
  *     Y[t] = base[t] + scale[a] * B[a] (A[a] X[t]),   a = adapter[t];   Y[t] = base[t] where a is outside 0 .. count - 1
  *   A       DEVICE [count][max_rank][N], B DEVICE [count][M][max_rank]; only the first rank[a] rows of A[a] and columns of

@@ -20,7 +20,7 @@ EXPORTS = ["bcq_packed_bytes", "bcq_workspace_bytes", "bcq_workspace_init", "bcq
            "bcq_quant_gptq", "bcq_from_linear_rows", "bcq_unpack", "bcq_gemv", "bcq_gemv_noalloc", "bcq_gemm_skinny", "bcq_read_probe_sink_bytes",
            "bcq_read_probe", "bcq_set_option", "bcq_status_string",
            "bcq_rotate", "bcq_attend_workspace_bytes", "bcq_attend", "bcq_lora_workspace_bytes", "bcq_lora",
-           "bcq_plan", "bcq_sample_workspace_bytes", "bcq_sample"]
+           "bcq_attend_shared_workspace_bytes", "bcq_attend_shared", "bcq_plan", "bcq_sample_workspace_bytes", "bcq_sample"]
 
 BCQ_F16, BCQ_BF16 = range(2)
 BCQ_MAX_HEAD_DIM = 256
@@ -118,6 +118,9 @@ def lib():
         L.bcq_attend.restype = i32
         L.bcq_attend.argtypes = [cp, vp, vp, i32, i32, i32, vp, i64, vp, vp, vp, i32, i32, f32, i32, i32, vp, i64, vp, vp]
         L.bcq_lora_workspace_bytes.restype, L.bcq_lora_workspace_bytes.argtypes = sz, [ap, i32]
+        L.bcq_attend_shared_workspace_bytes.restype, L.bcq_attend_shared_workspace_bytes.argtypes = sz, [cp] + [i32] * 5
+        L.bcq_attend_shared.restype = i32
+        L.bcq_attend_shared.argtypes = [cp, vp, vp, i32, i32, i32, i32, vp, i64, vp, vp, vp, i32, i32, vp, vp, i32, f32, i32, i32, vp, i64, vp, vp]
         L.bcq_plan.restype, L.bcq_plan.argtypes = i32, [ctypes.POINTER(PageTableDesc)] + [vp] * 7 + [i32] + [vp] * 9
         L.bcq_sample_workspace_bytes.restype, L.bcq_sample_workspace_bytes.argtypes = sz, [i32, i32]
         L.bcq_sample.restype, L.bcq_sample.argtypes = i32, [i32, i32, i32, vp, i64] + [vp] * 9
@@ -282,6 +285,17 @@ def attend(cache, k_cache, v_cache, tokens, requests, q_heads, q, ld_q, q_start,
     _check(lib().bcq_attend(ctypes.byref(cache), _ptr(k_cache), _ptr(v_cache), tokens, requests, q_heads, _ptr(q), ld_q,
                             _ptr(q_start), _ptr(kv_len), _ptr(pages), max_pages, max_new, scale, 1 if causal else 0, window,
                             _ptr(out), ld_out, _ptr(workspace), _stream(stream)), "bcq_attend")
+
+
+def attend_shared_workspace_bytes(cache, tokens, requests, groups, q_heads, max_pages):
+    return int(lib().bcq_attend_shared_workspace_bytes(ctypes.byref(cache), tokens, requests, groups, q_heads, max_pages))
+
+
+def attend_shared(cache, k_cache, v_cache, tokens, requests, groups, q_heads, q, ld_q, q_start, kv_len, pages, max_pages, max_new, group_start, shared_len,
+                  max_shared, scale, causal, window, out, ld_out, workspace, stream=None):
+    _check(lib().bcq_attend_shared(ctypes.byref(cache), _ptr(k_cache), _ptr(v_cache), tokens, requests, groups, q_heads, _ptr(q), ld_q, _ptr(q_start),
+                                   _ptr(kv_len), _ptr(pages), max_pages, max_new, _ptr(group_start), _ptr(shared_len), max_shared, scale, 1 if causal else 0,
+                                   window, _ptr(out), ld_out, _ptr(workspace), _stream(stream)), "bcq_attend_shared")
 
 
 def lora_workspace_bytes(desc, tokens):

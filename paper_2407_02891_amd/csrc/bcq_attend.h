@@ -80,6 +80,20 @@ __device__ __forceinline__ int page_of_all(const AttendParams &p, int r, int key
     return min(max(*(scalar_int)at, 0), p.num_pages - 1);
 }
 
+__device__ __forceinline__ int prefix_sum(int v, int lane)
+{
+#pragma unroll
+    for (int step = 1; step < 64; step <<= 1) {
+        const int below = __shfl_up(v, step);
+        if (lane >= step) v += below;
+    }
+    return v;
+}
+
+// A line of `total` blocks that workers share: worker w has the blocks from first_block(w) on, worker_of(b) has block b.
+__device__ __forceinline__ int first_block(int worker, int workers, int total) { return (int)((long long)worker * total / workers); }
+__device__ __forceinline__ int worker_of(int block, int workers, int total) { return (int)((((long long)block + 1) * workers - 1) / total); }
+
 // What elements behind head_dim are loaded from.
 static __device__ __attribute__((aligned(16))) const uint16_t g_zeros[8] = {};
 

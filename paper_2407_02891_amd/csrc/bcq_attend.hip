@@ -47,16 +47,6 @@ __device__ __forceinline__ int blocks_of(const AttendParams &p, const Request &q
     return max(1, (q.end + kBlock - 1) / kBlock - q.begin / kBlock);
 }
 
-__device__ __forceinline__ int prefix_sum(int v, int lane)
-{
-#pragma unroll
-    for (int step = 1; step < 64; step <<= 1) {
-        const int below = __shfl_up(v, step);
-        if (lane >= step) v += below;
-    }
-    return v;
-}
-
 // Sixty-four requests, one a lane, with the blocks up to and with each of them.
 struct Window {
     Request q;
@@ -74,8 +64,6 @@ __device__ __forceinline__ int lane_of(int v, int lane) { return __builtin_amdgc
 
 // Waves that share the line: no more than it has blocks.
 __device__ __forceinline__ int workers_of(const AttendParams &p, int total) { return min(p.workers, max(total, 1)); }
-__device__ __forceinline__ int first_block(int worker, int workers, int total) { return (int)((long long)worker * total / workers); }
-__device__ __forceinline__ int worker_of(int block, int workers, int total) { return (int)((((long long)block + 1) * workers - 1) / total); }
 
 // A wave's share of one request.
 struct Segment {

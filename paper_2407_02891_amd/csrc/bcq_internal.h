@@ -98,6 +98,14 @@ struct AttendArgs {
 size_t attend_workspace_bytes(const bcq_cache &c, int tokens, int requests, int q_heads, int max_new, int max_pages);
 hipError_t launch_attend(const AttendArgs &a, hipStream_t stream);
 
+struct AttendSharedArgs {
+    AttendArgs of;
+    const int *group_start, *shared_len;
+    int groups, max_shared;
+};
+size_t attend_shared_workspace_bytes(const bcq_cache &c, int tokens, int requests, int groups, int q_heads);
+hipError_t launch_attend_shared(const AttendSharedArgs &a, hipStream_t stream);
+
 struct LoraArgs {
     const uint16_t *A, *B, *X, *base;
     const int *rank, *adapter;

@@ -84,6 +84,22 @@ static bcq_status attend_shape(const bcq_cache *cache, int32_t tokens, int32_t r
     return BCQ_OK;
 }
 
+// What both attentions check beside the shape.
+static bcq_status attend_arguments(const bcq_cache *cache, const void *k_cache, const void *v_cache, int32_t tokens, int32_t requests, int32_t q_heads,
+                                   const void *q, int64_t ld_q, const int32_t *q_start, const int32_t *kv_len, const int32_t *pages, int32_t max_new, float scale,
+                                   int32_t causal, int32_t window, const void *out, int64_t ld_out)
+{
+    const int64_t cols = (int64_t)q_heads * cache->head_dim;
+    if (!row_stride_ok(ld_q, cols) || !row_stride_ok(ld_out, cols) || max_new < 1) return BCQ_ERR_INVALID_ARG;
+    if (!(scale > 0.0f) || isinf(scale) || (causal != 0 && causal != 1) || window < 0 || (window > 0 && !causal)) return BCQ_ERR_INVALID_ARG;
+    if (tokens == 0 || requests == 0) return BCQ_OK;
+    if (!k_cache || !v_cache || !q || !q_start || !kv_len || !pages || !out) return BCQ_ERR_INVALID_ARG;
+    if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(q_start, 4) || !aligned(kv_len, 4) ||
+        !aligned(pages, 4))
+        return BCQ_ERR_INVALID_ARG;
+    return BCQ_OK;
+}
+
 size_t bcq_attend_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t q_heads, int32_t max_pages,
                                   int32_t max_new)
 {
@@ -98,18 +114,49 @@ bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v
 {
     const bcq_status why = attend_shape(cache, tokens, requests, q_heads, max_pages, max_new);
     if (why != BCQ_OK) return why;
-    const int64_t cols = (int64_t)q_heads * cache->head_dim;
-    if (!row_stride_ok(ld_q, cols) || !row_stride_ok(ld_out, cols) ) return BCQ_ERR_INVALID_ARG;
-    if (!(scale > 0.0f) || isinf(scale) || (causal != 0 && causal != 1) || window < 0 || (window > 0 && !causal)) return BCQ_ERR_INVALID_ARG;
+    const bcq_status args = attend_arguments(cache, k_cache, v_cache, tokens, requests, q_heads, q, ld_q, q_start, kv_len, pages, max_new, scale, causal, window,
+                                             out, ld_out);
+    if (args != BCQ_OK) return args;
     if (tokens == 0 || requests == 0) return BCQ_OK;
-    if (!k_cache || !v_cache || !q || !q_start || !kv_len || !pages || !out) return BCQ_ERR_INVALID_ARG;
-    if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(q_start, 4) || !aligned(kv_len, 4) ||
-        !aligned(pages, 4))
-        return BCQ_ERR_INVALID_ARG;
     if (attend_workspace_bytes(*cache, tokens, requests, q_heads, max_new, max_pages) > 0 && (!workspace || !aligned(workspace, 16))) return BCQ_ERR_WORKSPACE;
     AttendArgs a{half(k_cache), half(v_cache), half(q), q_start, kv_len, pages, half(out), ld_q, ld_out, tokens, requests, q_heads, max_pages,
                  max_new, window, scale, causal != 0, workspace, *cache};
     return launch_attend(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
+}
+
+static bcq_status attend_shared_shape(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t groups, int32_t q_heads, int32_t max_pages)
+{
+    const bcq_status why = attend_shape(cache, tokens, requests, q_heads, max_pages, 1);
+    if (why != BCQ_OK) return why;
+    if (groups < 0) return BCQ_ERR_INVALID_ARG;
+    if (groups > kMaxTokens) return BCQ_ERR_UNSUPPORTED;
+    const int64_t tiles = 2 * (int64_t)tokens * (q_heads / cache->kv_heads) / 128 + groups + requests + 1;
+    return tiles * (max_pages * (int64_t)cache->page_size / 32 + 1) > 0x7fffffffLL ? BCQ_ERR_UNSUPPORTED : BCQ_OK;  // blocks of keys of all tiles are int
+}
+
+size_t bcq_attend_shared_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t groups, int32_t q_heads, int32_t max_pages)
+{
+    if (attend_shared_shape(cache, tokens, requests, groups, q_heads, max_pages) != BCQ_OK || tokens == 0 || requests == 0) return 0;
+    return attend_shared_workspace_bytes(*cache, tokens, requests, groups, q_heads);
+}
+
+bcq_status bcq_attend_shared(const bcq_cache *cache, const void *k_cache, const void *v_cache, int32_t tokens, int32_t requests, int32_t groups,
+                             int32_t q_heads, const void *q, int64_t ld_q, const int32_t *q_start, const int32_t *kv_len, const int32_t *pages,
+                             int32_t max_pages, int32_t max_new, const int32_t *group_start, const int32_t *shared_len, int32_t max_shared, float scale,
+                             int32_t causal, int32_t window, void *out, int64_t ld_out, void *workspace, void *stream)
+{
+    bcq_status why = attend_shared_shape(cache, tokens, requests, groups, q_heads, max_pages);
+    if (why != BCQ_OK) return why;
+    why = attend_arguments(cache, k_cache, v_cache, tokens, requests, q_heads, q, ld_q, q_start, kv_len, pages, max_new, scale, causal, window, out, ld_out);
+    if (why != BCQ_OK) return why;
+    if (max_shared < 0) return BCQ_ERR_INVALID_ARG;
+    if (tokens == 0 || requests == 0) return BCQ_OK;
+    if (groups > 0 && (!group_start || !shared_len || !aligned(group_start, 4) || !aligned(shared_len, 4))) return BCQ_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16)) return BCQ_ERR_WORKSPACE;
+    AttendSharedArgs a{{half(k_cache), half(v_cache), half(q), q_start, kv_len, pages, half(out), ld_q, ld_out, tokens, requests, q_heads, max_pages,
+                        max_new, window, scale, causal != 0, workspace, *cache},
+                       group_start, shared_len, groups, max_shared};
+    return launch_attend_shared(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
 }
 
 size_t bcq_lora_workspace_bytes(const bcq_adapters *desc, int32_t tokens)

@@ -20,6 +20,8 @@ struct {
     decltype(&bcq_attend_workspace_bytes) attend_workspace_bytes;
     decltype(&bcq_lora) lora;
     decltype(&bcq_lora_workspace_bytes) lora_workspace_bytes;
+    decltype(&bcq_attend_shared) attend_shared;
+    decltype(&bcq_attend_shared_workspace_bytes) attend_shared_workspace_bytes;
     decltype(&bcq_plan) plan;
     decltype(&bcq_sample) sample;
     decltype(&bcq_sample_workspace_bytes) sample_workspace_bytes;
@@ -183,30 +185,70 @@ at::Tensor rotate(PyObject *const *a)
     return out;
 }
 
+// What both attentions are given: desc, k, v, q, q_start, kv_len, pages, max_new first.
+struct Attended {
+    const bcq_cache *cache;
+    Place place;
+    const at::Tensor &k, &v, &q, &pages;
+    int64_t T, R, max_pages, q_heads, ld;
+    const int32_t *q_start, *kv_len;
+    int32_t max_new;
+
+    Attended(PyObject *const *a, const char *where)
+        : cache(address<const bcq_cache>(a[0])), place{tensor(a[1], where, "k").scalar_type(), tensor(a[1], where, "k").device(), where}, k(tensor(a[1], where, "k")),
+          v(tensor(a[2], where, "v")), q(tensor(a[3], where, "q")), pages(tensor(a[6], where, "pages"))
+    {
+        const int64_t D = head_dim(*cache, where);
+        if (q.dim() != 2 || q.size(1) % D) refuse(where, "q: [tokens][q_heads * head_dim]");
+        if (pages.dim() != 2 || pages.scalar_type() != at::kInt || pages.device() != place.device || !pages.is_contiguous())
+            refuse(where, "pages: contiguous int32 [requests][max_pages]");
+        T = q.size(0), R = pages.size(0), max_pages = pages.size(1), q_heads = q.size(1) / D;
+        if (T > INT32_MAX || R > INT32_MAX - 1 || max_pages > INT32_MAX || q_heads > INT32_MAX) refuse(where, "q or pages: too large");
+        ld = place.rows(q, "q", T, q.size(1));
+        q_start = place.ints(a[4], "q_start", R + 1), kv_len = place.ints(a[5], "kv_len", R);
+        max_new = int32(a[7], where, "max_new");
+    }
+    at::Tensor result(PyObject *out) const { return out == Py_None ? place.fresh(T, q.size(1)) : tensor(out, place.where, "out"); }
+};
+
 // attend(desc, k, v, q, q_start, kv_len, pages, max_new, scale, causal, window, out, stream)
 at::Tensor attend(PyObject *const *a)
 {
     const char *const where = "PagedCache.attend";
-    const bcq_cache *const c = address<const bcq_cache>(a[0]);
-    const at::Tensor &k = tensor(a[1], where, "k"), &v = tensor(a[2], where, "v"), &q = tensor(a[3], where, "q"), &pages = tensor(a[6], where, "pages");
-    const Place place{k.scalar_type(), k.device(), where};
-    const c10::DeviceGuard there(place.device);  // (launches go to the current device)
-    const int64_t D = head_dim(*c, where);
-    if (q.dim() != 2 || q.size(1) % D) refuse(where, "q: [tokens][q_heads * head_dim]");
-    if (pages.dim() != 2 || pages.scalar_type() != at::kInt || pages.device() != place.device || !pages.is_contiguous())
-        refuse(where, "pages: contiguous int32 [requests][max_pages]");
-    const int64_t T = q.size(0), R = pages.size(0), max_pages = pages.size(1), q_heads = q.size(1) / D;
-    if (T > INT32_MAX || R > INT32_MAX - 1 || max_pages > INT32_MAX || q_heads > INT32_MAX) refuse(where, "q or pages: too large");
-    const int64_t ld = place.rows(q, "q", T, q.size(1));
-    const int32_t *const q_start = place.ints(a[4], "q_start", R + 1), *const kv_len = place.ints(a[5], "kv_len", R);
-    const int32_t max_new = int32(a[7], where, "max_new"), window = int32(a[10], where, "window");
-    const at::Tensor out = a[11] == Py_None ? place.fresh(T, q.size(1)) : tensor(a[11], where, "out");
-    const int64_t ld_out = place.rows(out, "out", T, q.size(1));
-    const size_t bytes = g_bcq.attend_workspace_bytes(c, (int32_t)T, (int32_t)R, (int32_t)q_heads, (int32_t)max_pages, max_new);
-    const at::Tensor workspace = bytes ? place.scratch(bytes) : at::Tensor();
-    succeeded(g_bcq.attend(c, k.data_ptr(), v.data_ptr(), (int32_t)T, (int32_t)R, (int32_t)q_heads, q.data_ptr(), ld, q_start, kv_len,
-                           static_cast<const int32_t *>(pages.data_ptr()), (int32_t)max_pages, max_new, (float)number(a[8]), truth(a[9]), window,
+    const Attended x(a, where);
+    const c10::DeviceGuard there(x.place.device);  // (launches go to the current device)
+    const int32_t window = int32(a[10], where, "window");
+    const at::Tensor out = x.result(a[11]);
+    const int64_t ld_out = x.place.rows(out, "out", x.T, x.q.size(1));
+    const size_t bytes = g_bcq.attend_workspace_bytes(x.cache, (int32_t)x.T, (int32_t)x.R, (int32_t)x.q_heads, (int32_t)x.max_pages, x.max_new);
+    const at::Tensor workspace = bytes ? x.place.scratch(bytes) : at::Tensor();
+    succeeded(g_bcq.attend(x.cache, x.k.data_ptr(), x.v.data_ptr(), (int32_t)x.T, (int32_t)x.R, (int32_t)x.q_heads, x.q.data_ptr(), x.ld, x.q_start, x.kv_len,
+                           static_cast<const int32_t *>(x.pages.data_ptr()), (int32_t)x.max_pages, x.max_new, (float)number(a[8]), truth(a[9]), window,
                            out.data_ptr(), ld_out, bytes ? workspace.data_ptr() : nullptr, address<void>(a[12])),
+              where);
+    return out;
+}
+
+// attend_shared(desc, k, v, q, q_start, kv_len, pages, max_new, group_start, shared_len, max_shared, scale, causal, window, out, stream)
+at::Tensor attend_shared(PyObject *const *a)
+{
+    const char *const where = "PagedCache.attend_shared";
+    const Attended x(a, where);
+    const c10::DeviceGuard there(x.place.device);
+    const at::Tensor &lengths = tensor(a[9], where, "shared_len");
+    if (lengths.dim() != 1 || lengths.size(0) > INT32_MAX - 1) refuse(where, "shared_len: int32 [groups]");
+    const int64_t groups = lengths.size(0);
+    const int32_t *const shared_len = x.place.ints(a[9], "shared_len", groups), *const group_start = x.place.ints(a[8], "group_start", groups + 1);
+    const int32_t max_shared = int32(a[10], where, "max_shared"), window = int32(a[13], where, "window");
+    const at::Tensor out = x.result(a[14]);
+    const int64_t ld_out = x.place.rows(out, "out", x.T, x.q.size(1));
+    const size_t bytes =
+        g_bcq.attend_shared_workspace_bytes(x.cache, (int32_t)x.T, (int32_t)x.R, (int32_t)groups, (int32_t)x.q_heads, (int32_t)x.max_pages);
+    const at::Tensor workspace = bytes ? x.place.scratch(bytes) : at::Tensor();
+    succeeded(g_bcq.attend_shared(x.cache, x.k.data_ptr(), x.v.data_ptr(), (int32_t)x.T, (int32_t)x.R, (int32_t)groups, (int32_t)x.q_heads, x.q.data_ptr(), x.ld,
+                                  x.q_start, x.kv_len, static_cast<const int32_t *>(x.pages.data_ptr()), (int32_t)x.max_pages, x.max_new, group_start, shared_len,
+                                  max_shared, (float)number(a[11]), truth(a[12]), window, out.data_ptr(), ld_out, bytes ? workspace.data_ptr() : nullptr,
+                                  address<void>(a[15])),
               where);
     return out;
 }
@@ -350,6 +392,7 @@ PyObject *bind(PyObject *, PyObject *args)
     };
     if (!find(g_bcq.rotate, "bcq_rotate") || !find(g_bcq.attend, "bcq_attend") || !find(g_bcq.attend_workspace_bytes, "bcq_attend_workspace_bytes") ||
         !find(g_bcq.lora, "bcq_lora") || !find(g_bcq.lora_workspace_bytes, "bcq_lora_workspace_bytes") ||
+        !find(g_bcq.attend_shared, "bcq_attend_shared") || !find(g_bcq.attend_shared_workspace_bytes, "bcq_attend_shared_workspace_bytes") ||
         !find(g_bcq.plan, "bcq_plan") || !find(g_bcq.sample, "bcq_sample") || !find(g_bcq.sample_workspace_bytes, "bcq_sample_workspace_bytes"))
         return nullptr;
     Py_INCREF(error);
@@ -366,6 +409,7 @@ PyCFunction fast()
 PyMethodDef g_methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                            {"rotate", fast<13, rotate>(), METH_FASTCALL, nullptr},
                            {"attend", fast<13, attend>(), METH_FASTCALL, nullptr},
+                           {"attend_shared", fast<16, attend_shared>(), METH_FASTCALL, nullptr},
                            {"add", fast<10, add>(), METH_FASTCALL, nullptr},
                            {"step", fast<13, step>(), METH_FASTCALL, nullptr},
                            {"draw", fast<8, draw>(), METH_FASTCALL, nullptr},

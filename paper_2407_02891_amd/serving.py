@@ -71,6 +71,12 @@ class PagedCache:
         return self._native.attend(self._desc, self.k, self.v, q, q_start, kv_len, pages, max_new, self.head_dim ** -0.5 if scale is None else scale,
                                    causal, window, out, B.raw_stream(self._index))
 
+    def attend_shared(self, q, q_start, kv_len, pages, max_new, group_start, shared_len, max_shared, scale=None, causal=True, window=0, out=None):
+        """bcq_attend_shared: attend, for requests of which group c, group_start[c] .. group_start[c+1] - 1, share their first shared_len[c] keys (at most max_shared):
+        those are taken from the first one's pages and read once.  group_start int32 [groups + 1], shared_len int32 [groups]."""
+        return self._native.attend_shared(self._desc, self.k, self.v, q, q_start, kv_len, pages, max_new, group_start, shared_len, max_shared,
+                                          self.head_dim ** -0.5 if scale is None else scale, causal, window, out, B.raw_stream(self._index))
+
 
 class Adapters:
     """Low-rank adapters of one projection: A [count][max_rank][N], B [count][M][max_rank] contiguous, binary16 or bfloat16; scale

@@ -1,5 +1,6 @@
 """Argument checks of the table of pages and of the draw: all before any launch, so none of this needs a GPU."""
 import ctypes
+import math
 
 import pytest
 import torch
@@ -87,3 +88,33 @@ def test_objects_refuse():
     _refused(lambda: bcq.PageTable(torch.zeros((4, 2), dtype=torch.int32).t(), i, i, i[:1], 16))
     _refused(lambda: bcq.Sampler(torch.ones(2, dtype=torch.float64)))
     _refused(lambda: bcq.Sampler(torch.ones((2, 1))))
+
+
+def shared(c=(), **kw):
+    f = dict(dtype=0, kv_heads=8, head_dim=128, page_size=16, num_pages=100, page_stride=16384, head_stride=2048, slot_stride=128)
+    f.update(c)
+    a = dict(k=OK, v=OK, tokens=4, requests=2, groups=1, q_heads=64, q=OK, ld_q=8192, q_start=OK, kv_len=OK, pages=OK, max_pages=10, max_new=2, group_start=OK,
+             shared_len=OK, max_shared=100, scale=0.1, causal=1, window=0, out=OK, ld_out=8192, workspace=OK)
+    a.update(kw)
+    return bcq.lib().bcq_attend_shared(ctypes.byref(B.Cache(*f.values())), *a.values(), None)
+
+
+@pytest.mark.parametrize("kw", [dict(tokens=-1), dict(requests=-1), dict(groups=-1), dict(q_heads=0), dict(q_heads=60), dict(max_new=0), dict(max_pages=0),
+                                dict(max_shared=-1), dict(scale=0.0), dict(scale=math.nan), dict(scale=math.inf), dict(causal=2), dict(window=-1),
+                                dict(causal=0, window=5), dict(ld_q=8184), dict(ld_q=8196), dict(ld_out=8184), dict(k=None), dict(v=None), dict(q=None),
+                                dict(q_start=None), dict(kv_len=None), dict(pages=None), dict(out=None), dict(group_start=None), dict(shared_len=None),
+                                dict(k=OK + 8), dict(q=OK + 8), dict(out=OK + 2), dict(pages=OK + 2), dict(group_start=OK + 2), dict(shared_len=OK + 1)])
+def test_attend_shared_refuses(kw):
+    assert shared(**kw) == B.BCQ_ERR_INVALID_ARG
+
+
+def test_attend_shared_limits():
+    assert shared(dict(head_dim=264, slot_stride=264)) == shared(dict(page_size=24)) == B.BCQ_ERR_UNSUPPORTED
+    assert shared(dict(kv_heads=0)) == shared(dict(head_stride=4)) == B.BCQ_ERR_INVALID_ARG
+    assert shared(tokens=(1 << 20) + 1) == shared(groups=(1 << 20) + 1) == shared(max_pages=1 << 28) == B.BCQ_ERR_UNSUPPORTED
+    assert shared(tokens=1 << 20, max_pages=1 << 20) == B.BCQ_ERR_UNSUPPORTED     # blocks of all tiles
+    assert shared(workspace=None) == shared(workspace=OK + 8) == B.BCQ_ERR_WORKSPACE
+    assert shared(tokens=0, q=None) == shared(requests=0, q=None) == B.BCQ_OK     # nothing to do
+    cache = B.Cache(0, 8, 128, 16, 100, 16384, 2048, 128)
+    assert bcq.attend_shared_workspace_bytes(cache, 4, 2, 1, 64, 10) > 0
+    assert bcq.attend_shared_workspace_bytes(cache, 0, 2, 1, 64, 10) == bcq.attend_shared_workspace_bytes(cache, 4, 2, -1, 64, 10) == 0
