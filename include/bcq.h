@@ -429,13 +429,11 @@ bcq_status bcq_plan(const bcq_page_table *table, int32_t *pages, const int32_t *
  *   temperature, uniform DEVICE [rows] binary32 (uniform is bounded to 0 .. 1 - 2^-24); top_k DEVICE [rows] int32, top_p, min_p DEVICE [rows] binary32,
  *               or NULL (all)
  *   token       DEVICE [rows] int32; probability DEVICE [rows] binary32, or NULL
- *   workspace   DEVICE, bcq_sample_workspace_bytes(rows, vocab) bytes, 16-byte aligned (NULL if that is 0); scratch, no init, used by one call at a time
  * rows = 0 launches nothing.
  */
 #define BCQ_MAX_VOCAB (1 << 22)
-size_t bcq_sample_workspace_bytes(int32_t rows, int32_t vocab);
 bcq_status bcq_sample(int32_t dtype, int32_t rows, int32_t vocab, const void *logits, int64_t ld, const float *temperature, const int32_t *top_k,
-                      const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *probability, void *workspace, void *stream);
+                      const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *probability, void *stream);
 
 /*
  * Streaming-read probe: reads `bytes` (a multiple of 16) of DEVICE memory with

@@ -20,7 +20,7 @@ EXPORTS = ["bcq_packed_bytes", "bcq_workspace_bytes", "bcq_workspace_init", "bcq
            "bcq_quant_gptq", "bcq_from_linear_rows", "bcq_unpack", "bcq_gemv", "bcq_gemv_noalloc", "bcq_gemm_skinny", "bcq_read_probe_sink_bytes",
            "bcq_read_probe", "bcq_set_option", "bcq_status_string",
            "bcq_rotate", "bcq_attend_workspace_bytes", "bcq_attend", "bcq_lora_workspace_bytes", "bcq_lora",
-           "bcq_attend_shared_workspace_bytes", "bcq_attend_shared", "bcq_plan", "bcq_sample_workspace_bytes", "bcq_sample"]
+           "bcq_attend_shared_workspace_bytes", "bcq_attend_shared", "bcq_plan", "bcq_sample"]
 
 BCQ_F16, BCQ_BF16 = range(2)
 BCQ_MAX_HEAD_DIM = 256
@@ -122,8 +122,7 @@ def lib():
         L.bcq_attend_shared.restype = i32
         L.bcq_attend_shared.argtypes = [cp, vp, vp, i32, i32, i32, i32, vp, i64, vp, vp, vp, i32, i32, vp, vp, i32, f32, i32, i32, vp, i64, vp, vp]
         L.bcq_plan.restype, L.bcq_plan.argtypes = i32, [ctypes.POINTER(PageTableDesc)] + [vp] * 7 + [i32] + [vp] * 9
-        L.bcq_sample_workspace_bytes.restype, L.bcq_sample_workspace_bytes.argtypes = sz, [i32, i32]
-        L.bcq_sample.restype, L.bcq_sample.argtypes = i32, [i32, i32, i32, vp, i64] + [vp] * 9
+        L.bcq_sample.restype, L.bcq_sample.argtypes = i32, [i32, i32, i32, vp, i64] + [vp] * 8
         L.bcq_lora.restype, L.bcq_lora.argtypes = i32, [ap, vp, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp, i64, vp, vp]
         L.bcq_status_string.restype, L.bcq_status_string.argtypes = ctypes.c_char_p, [i32]
         _lib = L
@@ -314,13 +313,9 @@ def plan(table, pages, held, fixed, free_pages, free_count, cached, fresh, token
                           _stream(stream)), "bcq_plan")
 
 
-def sample_workspace_bytes(rows, vocab):
-    return int(lib().bcq_sample_workspace_bytes(rows, vocab))
-
-
-def sample(dtype, rows, vocab, logits, ld, temperature, top_k, top_p, min_p, uniform, token, probability, workspace, stream=None):
+def sample(dtype, rows, vocab, logits, ld, temperature, top_k, top_p, min_p, uniform, token, probability, stream=None):
     _check(lib().bcq_sample(dtype, rows, vocab, _ptr(logits), ld, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(uniform), _ptr(token),
-                            _ptr(probability), _ptr(workspace), _stream(stream)), "bcq_sample")
+                            _ptr(probability), _stream(stream)), "bcq_sample")
 
 
 def set_option(name, value):

@@ -138,9 +138,7 @@ struct SampleArgs {
     float *probability;
     int rows, vocab;
     bool bf16;
-    void *workspace;
 };
-size_t sample_workspace_bytes(int rows, int vocab);
 hipError_t launch_sample(const SampleArgs &a, hipStream_t stream);
 
 constexpr int kProbeBlocks = 512;  // the GEMV's grid: two workgroups per CU

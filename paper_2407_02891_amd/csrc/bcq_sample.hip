@@ -10,6 +10,8 @@
 //  * The weight and number of each unit of 512 values, in descending order, by all waves; then, in one wave, the borders one after the other: which unit, which eight values, which value,
 //    how many of its entries.
 //  * The entry: the row is read again (from L2) and the drawn value's entries counted, in the order of the index.
+#include <utility>
+
 #include "bcq_half.h"
 #include "bcq_internal.h"
 
@@ -56,17 +58,15 @@ __device__ __forceinline__ double value_at(uint32_t place)
     return to_float<BF>(bits_at(place));
 }
 
-// 2^y, y <= 0, to a few units of the last place: 2^n times the series of e^(r ln 2), |r| <= 1/2, whose next term is below 2^-53.  2^-1020 for less, and for NaN: beside
-// the largest value's weight, 1, that is none.
+// 2^y, y <= 0: 2^n times the series of e^(r ln 2), |r| <= 1/2, whose next term is below 2^-47.  2^-1020 for less, and for NaN: beside the largest value's weight, 1, that is none.
 __device__ __forceinline__ double exp2_series(double y)
 {
     y = fmax(y, -1020.0);
     const double n = __builtin_rint(y), z = (y - n) * 0.6931471805599453094;
-    double s = 1.0 / 6227020800.0;
-    constexpr double c[] = {1.0 / 479001600.0, 1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0,
-                            1.0 / 120.0,       1.0 / 24.0,       1.0 / 6.0,       0.5,            1.0,           1.0};
+    double s = 1.0 / 39916800.0;
+    constexpr double c[] = {1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
 #pragma unroll
-    for (int i = 0; i < 13; ++i) s = __builtin_fma(s, z, c[i]);
+    for (int i = 0; i < 11; ++i) s = __builtin_fma(s, z, c[i]);
     return __builtin_ldexp(s, (int)n);
 }
 
@@ -174,6 +174,42 @@ struct Chunk {
 };
 __device__ __forceinline__ int chunks_of(const uint16_t *row, int vocab) { return (int)((vocab + (reinterpret_cast<uintptr_t>(row) >> 1 & 7) + kChunk - 1) / kChunk); }
 
+// A row's chunks, which stay in registers where they are at most KEPT (not 0).
+template <int KEPT>
+struct Row {
+    const uint16_t *row;
+    int vocab, chunks;
+    Chunk kept[KEPT ? KEPT : 1];
+    __device__ __forceinline__ Row(const uint16_t *row, int vocab) : row(row), vocab(vocab), chunks(chunks_of(row, vocab))
+    {
+        if (KEPT)
+#pragma unroll
+            for (int c = 0; c < KEPT; ++c) kept[c].load(row, c, vocab);
+    }
+    template <class F, int... C>
+    __device__ __forceinline__ void in_turn(F use, std::integer_sequence<int, C...>) const
+    {
+        (void)(... || (C >= chunks || use(kept[C], C + 1 < chunks)));
+    }
+    // use(chunk, whether there are more) for one after the other, until it returns true.
+    template <class F>
+    __device__ __forceinline__ void each(F use) const
+    {
+        if constexpr (KEPT > 0) {
+            in_turn(use, std::make_integer_sequence<int, KEPT>());
+        } else {
+            Chunk next;
+            next.load(row, 0, vocab);
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
+                const Chunk now = next;
+                if (c + 1 < chunks) next.load(row, c + 1, vocab);
+                if (use(now, c + 1 < chunks)) return;
+            }
+        }
+    }
+};
+
 // Rows whose token is the first of the largest values, whatever the random number.
 __device__ __forceinline__ bool greedy(const SampleParams &p, int row)
 {
@@ -201,6 +237,21 @@ struct Wanted {
         }
         return found;
     }
+    // Whether any lane has one.
+    __device__ __forceinline__ bool any(const u32x4 &x) const
+    {
+        u32x4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = x[i] ^ pair;
+        if (mask != 0xffffffffu) y &= mask;
+        u16x2 least = {0xffff, 0xffff};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t two = y[i];
+            least = __builtin_elementwise_min(least, __builtin_bit_cast(u16x2, two));
+        }
+        return __ballot(least.x == 0 || least.y == 0) != 0;
+    }
     __device__ __forceinline__ int count(const u32x4 &x) const
     {
         u16x2 others = {0, 0};
@@ -215,32 +266,18 @@ struct Shared {
     int entries[kUnits];
     u64 best[kWaves];
     int found[kPieces * kWaves];
-    uint32_t tops[kWaves];
     uint32_t big[kMostBig];  // places of kBig entries each that are not in the table
     int num_big;
     uint32_t place;          // of the drawn value
     int nth;                 // which of its entries
 };
 
-// The place of the largest of the entries, as compared to signed numbers: right where it is zero or more and no NaN (false otherwise).
-template <bool BF>
-__device__ __forceinline__ bool top_of(uint32_t most, uint32_t &place)
-{
-    place = kPlus0 - most;
-    return most <= kInfinity<BF>;
-}
-
 // The first entry of the largest value: place << 32 | index, all ones if there is none.  All threads get it.
-template <bool BF>
-__device__ __forceinline__ u64 first_of_largest(const uint16_t *row, int vocab, Shared &sh)
+template <bool BF, int KEPT>
+__device__ __forceinline__ u64 first_of_largest(const Row<KEPT> &row, Shared &sh)
 {
     u64 best = ~0ull;
-    Chunk next;
-    next.load(row, 0, vocab);
-    const int chunks = chunks_of(row, vocab);
-    for (int c = 0; c < chunks; ++c) {
-        const Chunk now = next;
-        if (c + 1 < chunks) next.load(row, c + 1, vocab);
+    row.each([&](const Chunk &now, bool) {
         // (places less kFirst, so that NaN of either sign and -infinity are behind all others)
         constexpr u16x2 first = {(unsigned short)kFirst<BF>, (unsigned short)kFirst<BF>};
         u16x2 least = {0xffff, 0xffff};
@@ -261,7 +298,8 @@ __device__ __forceinline__ u64 first_of_largest(const uint16_t *row, int vocab, 
                 if (found) best = (u64)place << 32 | (uint32_t)(now.index(j) + __builtin_ctz(found));
             }
         }
-    }
+        return false;
+    });
     best = least_of_all(best);
     if ((threadIdx.x & 63) == 0) sh.best[threadIdx.x >> 6] = best;
     __syncthreads();
@@ -271,53 +309,58 @@ __device__ __forceinline__ u64 first_of_largest(const uint16_t *row, int vocab, 
     return best;
 }
 
-// How often each value occurs: the counters of magnitude m are in word m.  Returns the place of the largest, kEnd or more if there is none.
-template <bool BF>
-__device__ __forceinline__ uint32_t count_values(const uint16_t *row, int vocab, uint32_t *table, Shared &sh)
+// How often each value occurs: the counters of magnitude m are in word m.
+template <bool BF, int KEPT>
+__device__ __forceinline__ void count_values(const Row<KEPT> &row, uint32_t *table, Shared &sh)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Chunk next;
-    next.load(row, 0, vocab);
+    const int lane = threadIdx.x & 63;
     const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) reinterpret_cast<u32x4 *>(table)[i * kThreads + threadIdx.x] = zero;
+    for (int i = 0; i < 32768 / 4 / kThreads; ++i) reinterpret_cast<u32x4 *>(table)[i * kThreads + threadIdx.x] = zero;
     if (threadIdx.x == 0) sh.num_big = 0;
     __syncthreads();
-    s16x2 most = {-32768, -32768};
-    const int chunks = chunks_of(row, vocab);
-    for (int c = 0; c < chunks; ++c) {
-        const Chunk now = next;
-        if (c + 1 < chunks) next.load(row, c + 1, vocab);
+    row.each([&](const Chunk &now, bool more) {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-            if (!now.any(j, vocab)) break;
+            if (!now.any(j, row.vocab)) break;
             const u32x4 x = now.x[j];
-            // entries that are all alike, a mask's: one by one they would take 64 turns each
-            const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[0]);
-            u16x2 magnitude = {0, 0};
+            u16x2 high = {0, 0};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t two = x[i];  // (of a vector's element itself __builtin_bit_cast makes element 0)
-                magnitude = __builtin_elementwise_max(magnitude, __builtin_bit_cast(u16x2, two & 0x7fff7fffu));
-                most = __builtin_elementwise_max(most, __builtin_bit_cast(s16x2, two));
+                high = __builtin_elementwise_max(high, __builtin_bit_cast(u16x2, two));
             }
-            if (__ballot(x[0] == w && x[1] == w && x[2] == w && x[3] == w) == ~0ull && w >> 16 == (w & 0xffffu)) {
-                if ((w & 0x7fffu) < kInfinity<BF> + (w >> 31 ? 0u : 1u) && lane == 0) atomicAdd(table + (w & 0x7fffu), 512u << (w >> 31 << 4));
-                continue;
-            }
-            // infinities and NaN: not counted, but for +infinity (a mask of them would all meet at one counter)
-            const bool odd = __ballot(max((uint32_t)magnitude.x, (uint32_t)magnitude.y) >= kInfinity<BF>) != 0;
+            const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[0]);
+            if (__ballot(x[0] == w) == ~0ull && w >> 16 == (w & 0xffffu) && __ballot(x[1] == w && x[2] == w && x[3] == w) == ~0ull) {
+                // entries that are all alike, a mask's: one by one they would take 64 turns each
+                if ((w & 0xffffu) < kEnd<BF> && lane == 0) atomicAdd(table + (w & 0x7fffu), 512u << (w >> 31 << 4));
+            } else if (__ballot(max((uint32_t)high.x, (uint32_t)high.y) >= kEnd<BF>)) {
+                // -infinities, another mask, would all meet at one counter
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t address = (e ? x[i] >> 14 : x[i] << 2) & 0x1fffcu, negative = x[i] >> (e ? 31 : 15) & 1u;
-                    if (odd && address >= 4 * kInfinity<BF> + (negative ? 0 : 4)) continue;
-                    atomicAdd(reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(table) + address), negative * 0xffffu + 1u);
+                    for (int e = 0; e < 2; ++e) {
+                        const uint32_t bits = e ? x[i] >> 16 : x[i] & 0xffffu;
+                        if (bits < kEnd<BF>) atomicAdd(table + (bits & 0x7fffu), bits >> 15 ? 0x10000u : 1u);
+                    }
+            } else {
+                // (three vector instructions an entry: the low and the high half's address and what is added)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t two = x[i], magnitudes = two & 0x7fff7fffu;
+                    const s16x2 sign = __builtin_bit_cast(s16x2, two) >> (s16x2){15, 15};  // 0 or 0xffff
+                    uint32_t low, high;
+                    asm("v_lshlrev_b32_sdwa %0, %2, %3 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:WORD_0\n\t"
+                        "v_lshlrev_b32_sdwa %1, %2, %3 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:WORD_1"
+                        : "=&v"(low), "=v"(high)
+                        : "v"(2), "v"(magnitudes));
+                    atomicAdd(reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(table) + low), (uint32_t)(uint16_t)sign.x + 1u);
+                    atomicAdd(reinterpret_cast<uint32_t *>(reinterpret_cast<char *>(table) + high), (uint32_t)(uint16_t)sign.y + 1u);
                 }
+            }
         }
         __syncthreads();
-        if (c + 1 < chunks) {  // what the next chunk could bring beyond 16 bits
+        if (more) {  // what the next chunk could bring beyond 16 bits
             for (int i = threadIdx.x; i < 32768 / 4; i += kThreads) {
                 u32x4 x = reinterpret_cast<u32x4 *>(table)[i];
                 if (!((x[0] | x[1] | x[2] | x[3]) & 0x80008000u)) continue;
@@ -332,43 +375,40 @@ __device__ __forceinline__ uint32_t count_values(const uint16_t *row, int vocab,
             }
             __syncthreads();
         }
-    }
-    int top_signed = max((int)most.x, (int)most.y);
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) top_signed = max(top_signed, __shfl_xor(top_signed, s));
-    if (lane == 0) sh.tops[wave] = (uint32_t)top_signed;
-    if (threadIdx.x == 0 && table[0] >> 16) {  // -0 are zeros
+        return false;
+    });
+    // NaN go, -0 are zeros
+    static_assert(0x7fff - kInfinity<BF> <= kThreads, "");
+    if (threadIdx.x < 0x7fff - kInfinity<BF>) table[kInfinity<BF> + 1 + threadIdx.x] = 0;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < sh.num_big; ++i)
+            if (sh.big[i] < kFirst<BF>) sh.big[i] = 0xffffffffu;
         const uint32_t zeros = (table[0] >> 16) + (table[0] & 0xffffu);
         table[0] = zeros & 0x7fffu;
-        for (uint32_t n = zeros / kBig; n > 0; --n) sh.big[atomicAdd(&sh.num_big, 1)] = kPlus0;
+        for (uint32_t n = zeros / kBig; n > 0; --n) sh.big[sh.num_big++] = kPlus0;
     }
     __syncthreads();
-    int largest = (int)sh.tops[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) largest = max(largest, (int)sh.tops[w]);
-    uint32_t top;
-    if (largest >= 0 && top_of<BF>((uint32_t)largest, top)) return (uint32_t)__builtin_amdgcn_readfirstlane((int)top);
-    // all of them negative, or a NaN among them: from the table
-    top = 0xffffffffu;
-    for (int m = threadIdx.x; m <= (int)kInfinity<BF>; m += kThreads) {
-        if (table[m] & 0xffffu) top = min(top, kPlus0 - m);
-        if (table[m] >> 16) top = min(top, kMinus0 + m);
-    }
-    for (int i = threadIdx.x; i < sh.num_big; i += kThreads) top = min(top, sh.big[i]);
-#pragma unroll
-    for (int s = 32; s > 0; s >>= 1) top = min(top, (uint32_t)__shfl_xor((int)top, s));
-    __syncthreads();
-    if (lane == 0) sh.tops[wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = min(top, sh.tops[w]);
-    return (uint32_t)__builtin_amdgcn_readfirstlane((int)top);
 }
 
 // What is counted.
 struct Counts {
     const uint32_t *table;
     const Shared &sh;
+    int num_big;
+    // Of a block of words (the positive unit kUnits / 2 - 1 - b and the negative one kUnits / 2 + b) what the lane has; the table alone.
+    __device__ __forceinline__ void block(int b, int lane, int &low, int &high) const
+    {
+        const u32x4 *const at = reinterpret_cast<const u32x4 *>(table + b * kUnit + 4 * lane);
+        const u32x4 c[2] = {at[0], at[64]};
+        uint32_t l = 0, h = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t two = c[e >> 2][e & 3];
+            l = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2, two), (u16x2){1, 0}, l, false);
+            h = __builtin_amdgcn_udot2(__builtin_bit_cast(u16x2, two), (u16x2){0, 1}, h, false);
+        }
+        low = (int)l, high = (int)h;
+    }
     // A unit's, eight a lane.
     __device__ __forceinline__ void unit(int u, int lane, int (&n)[8]) const
     {
@@ -378,56 +418,78 @@ struct Counts {
 #pragma unroll
         for (int e = 0; e < 8; ++e) n[e] = (int)(negative ? c[e >> 2][e & 3] >> 16 : c[(7 - e) >> 2][3 - (e & 3)] & 0xffffu);
         const uint32_t first = u * kUnit + 8 * lane;
-        for (int i = 0; i < sh.num_big; ++i)
+        for (int i = 0; i < num_big; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) n[e] += sh.big[i] == first + e ? kBig : 0;
     }
     __device__ __forceinline__ int of(uint32_t place) const
     {
         int n = (int)(place & 0x8000u ? table[place & 0x7fffu] >> 16 : table[kPlus0 - place] & 0xffffu);
-        for (int i = 0; i < sh.num_big; ++i) n += sh.big[i] == place ? kBig : 0;
+        for (int i = 0; i < num_big; ++i) n += sh.big[i] == place ? kBig : 0;
         return n;
     }
 };
 
-// The draw of a row whose largest value is at `top`: the value, and which of its entries, in sh.  False if there is nothing to draw from.
+// The draw of a row: the value, and which of its entries, in sh.  False if there is nothing to draw from.
 template <bool BF>
-__device__ __forceinline__ bool draw(const SampleParams &p, int row, uint32_t top, const Counts &c, Shared &sh)
+__device__ __forceinline__ bool draw(const SampleParams &p, int row, const Counts &c, Shared &sh)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (top >= kEnd<BF>) {
+    // ---- number of each unit's entries, then the largest value, then their weight as far as a border needs it ----
+    for (int b = wave; b < kUnits / 2; b += kWaves) {
+        int low, high;
+        c.block(b, lane, low, high);
+        low = sum_all(low), high = sum_all(high);
+        if (lane == 0) sh.entries[kUnits / 2 - 1 - b] = low, sh.entries[kUnits / 2 + b] = high;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < c.num_big && sh.big[threadIdx.x] < 0x10000u) atomicAdd(sh.entries + sh.big[threadIdx.x] / kUnit, kBig);
+    if (c.num_big) __syncthreads();
+    const int e0 = sh.entries[2 * lane], e1 = sh.entries[2 * lane + 1];
+    const int entries_upto = sum_upto(e0 + e1, lane), n0 = entries_upto - (e0 + e1);
+    const int all = from_lane(entries_upto, 63), top_k = p.top_k ? p.top_k[row] : 0;
+    const double top_p = p.top_p ? p.top_p[row] : 1.0, min_p = p.min_p ? p.min_p[row] : 0.0;
+    if (all == 0) {
         if (threadIdx.x == 0) write_token(p, row, -1, 0.0f);
         return false;
     }
+    int top_unit = 2 * __builtin_ctzll(__ballot(e0 || e1));
+    if (!from_lane(e0, top_unit / 2)) ++top_unit;
     Weigh weigh;
-    weigh.top = top;
-    weigh.most = value_at<BF>(top);
+    {
+        int n[8], e = 8;
+        c.unit(top_unit, lane, n);
+#pragma unroll
+        for (int i = 7; i >= 0; --i) e = n[i] ? i : e;
+        const int l = __builtin_ctzll(__ballot(e < 8));
+        weigh.top = top_unit * kUnit + 8 * l + from_lane(e, l);
+    }
+    weigh.most = value_at<BF>(weigh.top);
     weigh.per = 1.4426950408889634074 / (double)p.temperature[row];
-    // ---- weight and number of each unit's entries ----
+    int last_unit = kUnits - 1;  // that counts: of the first top_k entries; without top_p, of those with weights of min_p
+    if (top_k > 0 && top_k < all) {
+        const int l = __builtin_ctzll(__ballot(entries_upto >= top_k));
+        last_unit = 2 * l + (from_lane(n0 + e0, l) >= top_k ? 0 : 1);
+    }
+    if (min_p > 0.0 && !(top_p < 1.0)) {
+        const double least = fmin(min_p, 1.0);
+        const u64 behind0 = __ballot(weigh.of<BF>(2 * lane * kUnit) < least), behind1 = __ballot(weigh.of<BF>(2 * lane * kUnit + kUnit) < least);
+        last_unit = min(last_unit, max(kUnits - 1 - __popcll(behind0) - __popcll(behind1), top_unit));
+    }
     for (int u = wave; u < kUnits; u += kWaves) {
         double mass = 0.0;
-        int entries = 0;
-        if (u >= (int)(top / kUnit)) {
+        if (u <= last_unit && sh.entries[u]) {
             int n[8];
             c.unit(u, lane, n);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) entries += n[e];
-            if (__ballot(entries)) {
-                mass = sum_all(weigh.eight<BF>(u * kUnit + 8 * lane, n));
-                entries = sum_all(entries);
-            }
+            mass = sum_all(weigh.eight<BF>(u * kUnit + 8 * lane, n));
         }
-        if (lane == 0) sh.mass[u] = mass, sh.entries[u] = entries;
+        if (lane == 0) sh.mass[u] = mass;
     }
     __syncthreads();
     // ---- the borders, in one wave ----
     if (wave == 0) {
         const double m0 = sh.mass[2 * lane], m1 = sh.mass[2 * lane + 1];
-        const int e0 = sh.entries[2 * lane], e1 = sh.entries[2 * lane + 1];
         const double mass_upto = sum_upto(m0 + m1, lane), before0 = mass_upto - (m0 + m1);  // before the lane's first unit
-        const int entries_upto = sum_upto(e0 + e1, lane), n0 = entries_upto - (e0 + e1);
-        const int all = from_lane(entries_upto, 63), top_k = p.top_k ? p.top_k[row] : 0;
-        const double top_p = p.top_p ? p.top_p[row] : 1.0, min_p = p.min_p ? p.min_p[row] : 0.0;
         const float number = p.uniform[row];
         // the end of what is kept: `kept` entries of the value at `end`, all of those before it
         uint32_t end = 0xffffffffu;
@@ -509,24 +571,21 @@ __device__ __forceinline__ bool draw(const SampleParams &p, int row, uint32_t to
 }
 
 // The drawn entry: its piece, in the order of pieces, chunk after chunk.
-__device__ __forceinline__ void find_entry(const SampleParams &p, int row, const uint16_t *logits, Shared &sh)
+template <int KEPT>
+__device__ __forceinline__ void find_entry(const SampleParams &p, int row, const Row<KEPT> &logits, Shared &sh)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Wanted wanted(sh.place);
     int nth = sh.nth;
-    Chunk next;
-    next.load(logits, 0, p.vocab);
-    const int chunks = chunks_of(logits, p.vocab);
-    for (int c = 0; c < chunks; ++c) {
-        const Chunk now = next;
-        if (c + 1 < chunks) next.load(logits, c + 1, p.vocab);
+    logits.each([&](const Chunk &now, bool) {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
-            const int found = now.any(j, p.vocab) ? wanted.count(now.x[j]) : 0;
             int all = 0;
-            if (__ballot(found))
+            if (now.any(j, p.vocab) && wanted.any(now.x[j])) {
+                const int found = wanted.count(now.x[j]);
 #pragma unroll
                 for (int bit = 0; bit < 4; ++bit) all += __popcll(__ballot(found >> bit & 1)) << bit;
+            }
             if (lane == 0) sh.found[j * kWaves + wave] = all;
         }
         __syncthreads();
@@ -534,7 +593,7 @@ __device__ __forceinline__ void find_entry(const SampleParams &p, int row, const
         const u64 votes = __ballot(upto > nth);
         if (votes) {
             const int l = __builtin_ctzll(votes);
-            if (l % kWaves != wave) return;
+            if (l % kWaves != wave) return true;
             const int before = from_lane(upto - here, l);
             uint32_t bits = 0;
             int index = 0;
@@ -542,42 +601,52 @@ __device__ __forceinline__ void find_entry(const SampleParams &p, int row, const
             for (int j = 0; j < kPieces; ++j)
                 if (j == l / kWaves) bits = wanted.which(now.x[j]), index = now.index(j);
             const int own = __popc(bits), in_front = before + sum_upto(own, lane) - own;
-            if (nth < in_front || nth >= in_front + own) return;
+            if (nth < in_front || nth >= in_front + own) return true;
             for (int i = in_front; i < nth; ++i) bits &= bits - 1;
             p.token[row] = index + __builtin_ctz(bits);
-            return;
+            return true;
         }
         nth -= from_lane(upto, 63);
         __syncthreads();
-    }
+        return false;
+    });
 }
 static_assert(kPieces * kWaves == 64, "");
 
 }  // namespace
 
-template <bool BF>
+template <bool BF, int KEPT>
 __global__ __launch_bounds__(kThreads) void bcq_sample_kernel(SampleParams p)
 {
     __shared__ __attribute__((aligned(16))) uint32_t table[32768];
     __shared__ Shared sh;
     const int row = blockIdx.x;
-    const uint16_t *const logits = p.logits + row * p.ld;
+    const Row<KEPT> logits(p.logits + row * p.ld, p.vocab);
     if (greedy(p, row)) {
-        const u64 best = first_of_largest<BF>(logits, p.vocab, sh);
+        const u64 best = first_of_largest<BF>(logits, sh);
         if (threadIdx.x == 0) write_token(p, row, best == ~0ull ? -1 : (int)(uint32_t)best, best == ~0ull ? 0.0f : 1.0f);
         return;
     }
-    const uint32_t top = count_values<BF>(logits, p.vocab, table, sh);
-    if (draw<BF>(p, row, top, Counts{table, sh}, sh)) find_entry(p, row, logits, sh);
+    count_values<BF>(logits, table, sh);
+    if (draw<BF>(p, row, Counts{table, sh, __builtin_amdgcn_readfirstlane(sh.num_big)}, sh)) find_entry(p, row, logits, sh);
 }
 
-size_t sample_workspace_bytes(int, int) { return 0; }
+namespace {
+
+template <bool BF>
+void sample(const SampleParams &p, int rows, hipStream_t s)
+{
+    if (p.vocab + 7 <= kChunk) bcq_sample_kernel<BF, 1><<<rows, kThreads, 0, s>>>(p);
+    else bcq_sample_kernel<BF, 0><<<rows, kThreads, 0, s>>>(p);
+}
+
+}  // namespace
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t stream)
 {
     const SampleParams p = {a.logits, a.temperature, a.top_p, a.min_p, a.uniform, a.top_k, a.token, a.probability, a.ld, a.vocab};
-    if (a.bf16) bcq_sample_kernel<true><<<a.rows, kThreads, 0, stream>>>(p);
-    else bcq_sample_kernel<false><<<a.rows, kThreads, 0, stream>>>(p);
+    if (a.bf16) sample<true>(p, a.rows, stream);
+    else sample<false>(p, a.rows, stream);
     return hipGetLastError();
 }
 

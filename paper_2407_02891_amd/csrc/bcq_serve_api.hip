@@ -206,31 +206,18 @@ bcq_status bcq_plan(const bcq_page_table *table, int32_t *pages, const int32_t *
     return launch_plan(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
 }
 
-static bcq_status sample_shape(int32_t rows, int32_t vocab)
-{
-    if (rows < 0 || vocab < 1) return BCQ_ERR_INVALID_ARG;
-    return rows > kMaxTokens || vocab > BCQ_MAX_VOCAB ? BCQ_ERR_UNSUPPORTED : BCQ_OK;
-}
-
-size_t bcq_sample_workspace_bytes(int32_t rows, int32_t vocab)
-{
-    return sample_shape(rows, vocab) != BCQ_OK || rows == 0 ? 0 : sample_workspace_bytes(rows, vocab);
-}
-
 bcq_status bcq_sample(int32_t dtype, int32_t rows, int32_t vocab, const void *logits, int64_t ld, const float *temperature, const int32_t *top_k,
-                      const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *probability, void *workspace, void *stream)
+                      const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *probability, void *stream)
 {
     if (dtype != BCQ_F16 && dtype != BCQ_BF16) return BCQ_ERR_INVALID_ARG;
-    const bcq_status why = sample_shape(rows, vocab);
-    if (why != BCQ_OK) return why;
-    if (ld < vocab) return BCQ_ERR_INVALID_ARG;
+    if (rows < 0 || vocab < 1 || ld < vocab) return BCQ_ERR_INVALID_ARG;
+    if (rows > kMaxTokens || vocab > BCQ_MAX_VOCAB) return BCQ_ERR_UNSUPPORTED;
     if (rows == 0) return BCQ_OK;
     if (!logits || !temperature || !uniform || !token) return BCQ_ERR_INVALID_ARG;
     if (!aligned(logits, 2) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) || !aligned(uniform, 4) ||
         !aligned(token, 4) || !aligned(probability, 4))
         return BCQ_ERR_INVALID_ARG;
-    if (sample_workspace_bytes(rows, vocab) > 0 && (!workspace || !aligned(workspace, 16))) return BCQ_ERR_WORKSPACE;
-    SampleArgs a{half(logits), ld, temperature, top_p, min_p, uniform, top_k, token, probability, rows, vocab, dtype == BCQ_BF16, workspace};
+    SampleArgs a{half(logits), ld, temperature, top_p, min_p, uniform, top_k, token, probability, rows, vocab, dtype == BCQ_BF16};
     return launch_sample(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;
 }
 

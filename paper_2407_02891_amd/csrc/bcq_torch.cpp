@@ -24,7 +24,6 @@ struct {
     decltype(&bcq_attend_shared_workspace_bytes) attend_shared_workspace_bytes;
     decltype(&bcq_plan) plan;
     decltype(&bcq_sample) sample;
-    decltype(&bcq_sample_workspace_bytes) sample_workspace_bytes;
 } g_bcq;
 
 // A refusal or a failed call, on its way to Python.
@@ -365,11 +364,9 @@ PyObject *draw(PyObject *const *a)
         token = tensor(PyTuple_GET_ITEM(a[6], 0), where, "out[0]"), probability = tensor(PyTuple_GET_ITEM(a[6], 1), where, "out[1]");
         place.vector<float>(PyTuple_GET_ITEM(a[6], 1), "out[1]", R, at::kFloat);
     }
-    const size_t bytes = g_bcq.sample_workspace_bytes((int32_t)R, (int32_t)V);
-    const at::Tensor workspace = bytes ? place.scratch(bytes) : at::Tensor();
     succeeded(g_bcq.sample(place.type == at::kBFloat16 ? BCQ_BF16 : BCQ_F16, (int32_t)R, (int32_t)V, logits.data_ptr(), ld,
                            place.vector<float>(a[0], "temperature", R, at::kFloat), top_k, top_p, min_p, uniform, static_cast<int32_t *>(token.data_ptr()),
-                           static_cast<float *>(probability.data_ptr()), bytes ? workspace.data_ptr() : nullptr, address<void>(a[7])),
+                           static_cast<float *>(probability.data_ptr()), address<void>(a[7])),
               where);
     PyObject *const t = THPVariable_Wrap(token), *const p = THPVariable_Wrap(probability);
     PyObject *const both = t && p ? PyTuple_Pack(2, t, p) : nullptr;
@@ -393,7 +390,7 @@ PyObject *bind(PyObject *, PyObject *args)
     if (!find(g_bcq.rotate, "bcq_rotate") || !find(g_bcq.attend, "bcq_attend") || !find(g_bcq.attend_workspace_bytes, "bcq_attend_workspace_bytes") ||
         !find(g_bcq.lora, "bcq_lora") || !find(g_bcq.lora_workspace_bytes, "bcq_lora_workspace_bytes") ||
         !find(g_bcq.attend_shared, "bcq_attend_shared") || !find(g_bcq.attend_shared_workspace_bytes, "bcq_attend_shared_workspace_bytes") ||
-        !find(g_bcq.plan, "bcq_plan") || !find(g_bcq.sample, "bcq_sample") || !find(g_bcq.sample_workspace_bytes, "bcq_sample_workspace_bytes"))
+        !find(g_bcq.plan, "bcq_plan") || !find(g_bcq.sample, "bcq_sample"))
         return nullptr;
     Py_INCREF(error);
     Py_XSETREF(g_error, error);

@@ -160,8 +160,8 @@ def test_rows_that_begin_anywhere(vocab, offset, more, dtype):
 
 
 @pytest.mark.parametrize("rows,vocab", [(700, 66000), (1500, 40)])
-def test_more_rows_than_a_launch(rows, vocab):
-    """More slices than the workspace is for at a time; each row is as it is alone."""
+def test_many_rows(rows, vocab):
+    """More than the chip has compute units; each row is as it is alone."""
     g = torch.Generator(device="cuda").manual_seed(3)
     x = (torch.randn((rows, vocab), generator=g, device="cuda") * 2).bfloat16()
     s = _settings(rows, 4)

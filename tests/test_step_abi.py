@@ -21,7 +21,7 @@ def plan(t=(), **kw):
 
 
 def sample(**kw):
-    a = dict(dtype=0, rows=4, vocab=100, logits=OK, ld=100, temperature=OK, top_k=OK, top_p=OK, min_p=OK, uniform=OK, token=OK, probability=OK, workspace=OK)
+    a = dict(dtype=0, rows=4, vocab=100, logits=OK, ld=100, temperature=OK, top_k=OK, top_p=OK, min_p=OK, uniform=OK, token=OK, probability=OK)
     a.update(kw)
     return bcq.lib().bcq_sample(*a.values(), None)
 
@@ -55,17 +55,6 @@ def test_sample_limits():
     assert sample(rows=(1 << 20) + 1) == B.BCQ_ERR_UNSUPPORTED
     assert sample(vocab=B.BCQ_MAX_VOCAB + 1, ld=1 << 40) == B.BCQ_ERR_UNSUPPORTED
     assert sample(rows=0, logits=None, token=None) == B.BCQ_OK   # nothing to do
-    assert sample(vocab=200000, ld=200000, workspace=None) == B.BCQ_ERR_WORKSPACE
-    assert sample(vocab=200000, ld=200000, workspace=OK + 8) == B.BCQ_ERR_WORKSPACE
-
-
-def test_sample_workspace():
-    assert bcq.sample_workspace_bytes(-1, 100) == bcq.sample_workspace_bytes(4, 0) == bcq.sample_workspace_bytes(0, 100) == 0
-    assert bcq.sample_workspace_bytes(4, B.BCQ_MAX_VOCAB + 1) == 0
-    for rows in (1, 2, 100, 1000, 1 << 20):  # bounded, however many rows there are
-        for vocab in (1, 50, 4097, 32000, 65528, 65529, 262144, B.BCQ_MAX_VOCAB):
-            assert 0 <= bcq.sample_workspace_bytes(rows, vocab) < 200 << 20
-    assert bcq.sample_workspace_bytes(1, 262144) > 0
 
 
 def _refused(call):
