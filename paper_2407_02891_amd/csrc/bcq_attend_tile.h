@@ -49,9 +49,10 @@ struct Tile {
 };
 
 // Sums over the keys of the tile's blocks, relative to `most` (times log2 e), and their weight, this lane's half of it.  Number 4 u + i of o[d] is element 32 d + 8 u + 4 (lane / 32) + i
-// of the lane's row.  All waves of the workgroup together; afterwards they may still be reading LDS.
+// of the lane's row.  All waves of the workgroup together.
+// Returns (all waves the same) whether some may still be reading LDS.
 template <int DT, bool BF, bool ANY, bool PASSING>
-__device__ __forceinline__ void attend_tile(const AttendParams &p, const Tile &t, f32x16 (&o)[DT / 32], float &most, float &sum)
+__device__ __forceinline__ bool attend_tile(const AttendParams &p, const Tile &t, f32x16 (&o)[DT / 32], float &most, float &sum)
 {
     constexpr int KB = tile_keys(DT), KT = KB / 32, C = DT / 16, DV = DT / 32;
     constexpr int kPieces = DT / 8, kRows = 64 / kPieces;       // 16-byte pieces of a key; keys of one transfer of a wave
@@ -303,6 +304,7 @@ __device__ __forceinline__ void attend_tile(const AttendParams &p, const Tile &t
         careful = __builtin_amdgcn_readfirstlane(any) != 0;
         if (!careful) break;
     }
+    return careful;
 }
 
 }  // namespace
