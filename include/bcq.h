@@ -355,7 +355,8 @@ bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v
  *   workspace   DEVICE, bcq_attend_shared_workspace_bytes(...) bytes, 16-byte aligned; scratch, no init, used by one call at a time
  * The other arguments as for bcq_attend.  tokens = 0 or requests = 0 launches nothing.
  */
-size_t bcq_attend_shared_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t groups, int32_t q_heads, int32_t max_pages);
+size_t bcq_attend_shared_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t groups, int32_t q_heads, int32_t max_pages,
+                                         int32_t max_new);
 bcq_status bcq_attend_shared(const bcq_cache *cache, const void *k_cache, const void *v_cache, int32_t tokens, int32_t requests, int32_t groups,
                              int32_t q_heads, const void *q, int64_t ld_q, const int32_t *q_start, const int32_t *kv_len, const int32_t *pages,
                              int32_t max_pages, int32_t max_new, const int32_t *group_start, const int32_t *shared_len, int32_t max_shared, float scale,

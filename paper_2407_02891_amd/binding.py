@@ -118,7 +118,7 @@ def lib():
         L.bcq_attend.restype = i32
         L.bcq_attend.argtypes = [cp, vp, vp, i32, i32, i32, vp, i64, vp, vp, vp, i32, i32, f32, i32, i32, vp, i64, vp, vp]
         L.bcq_lora_workspace_bytes.restype, L.bcq_lora_workspace_bytes.argtypes = sz, [ap, i32]
-        L.bcq_attend_shared_workspace_bytes.restype, L.bcq_attend_shared_workspace_bytes.argtypes = sz, [cp] + [i32] * 5
+        L.bcq_attend_shared_workspace_bytes.restype, L.bcq_attend_shared_workspace_bytes.argtypes = sz, [cp] + [i32] * 6
         L.bcq_attend_shared.restype = i32
         L.bcq_attend_shared.argtypes = [cp, vp, vp, i32, i32, i32, i32, vp, i64, vp, vp, vp, i32, i32, vp, vp, i32, f32, i32, i32, vp, i64, vp, vp]
         L.bcq_plan.restype, L.bcq_plan.argtypes = i32, [ctypes.POINTER(PageTableDesc)] + [vp] * 7 + [i32] + [vp] * 9
@@ -286,8 +286,8 @@ def attend(cache, k_cache, v_cache, tokens, requests, q_heads, q, ld_q, q_start,
                             _ptr(out), ld_out, _ptr(workspace), _stream(stream)), "bcq_attend")
 
 
-def attend_shared_workspace_bytes(cache, tokens, requests, groups, q_heads, max_pages):
-    return int(lib().bcq_attend_shared_workspace_bytes(ctypes.byref(cache), tokens, requests, groups, q_heads, max_pages))
+def attend_shared_workspace_bytes(cache, tokens, requests, groups, q_heads, max_pages, max_new):
+    return int(lib().bcq_attend_shared_workspace_bytes(ctypes.byref(cache), tokens, requests, groups, q_heads, max_pages, max_new))
 
 
 def attend_shared(cache, k_cache, v_cache, tokens, requests, groups, q_heads, q, ld_q, q_start, kv_len, pages, max_pages, max_new, group_start, shared_len,

@@ -94,6 +94,8 @@ __device__ __forceinline__ int prefix_sum(int v, int lane)
 __device__ __forceinline__ int first_block(int worker, int workers, int total) { return (int)((long long)worker * total / workers); }
 __device__ __forceinline__ int worker_of(int block, int workers, int total) { return (int)((((long long)block + 1) * workers - 1) / total); }
 
+constexpr long long kPassingBytes = 128ll << 20;  // a cache of so many bytes: half of what the last level holds
+
 // What elements behind head_dim are loaded from.
 static __device__ __attribute__((aligned(16))) const uint16_t g_zeros[8] = {};
 

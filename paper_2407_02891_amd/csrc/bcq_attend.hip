@@ -32,7 +32,6 @@ constexpr int kStreamRows = 16;
 template <bool BF>
 using StreamWeights = Weights<BF, 1>;  // (renewing costs nothing where memory is waited for)
 constexpr int kMostRows = 128;  // of a tile of either kernel
-constexpr long long kPassingBytes = 128ll << 20;  // half of what the last level holds
 
 // Waves per SIMD: what the registers allow.
 constexpr int stream_occupancy(int dim, bool any) { return dim == 64 ? 3 : dim == 128 ? 2 : 1; }

@@ -32,6 +32,7 @@ template <int DT, bool BF, bool ANY, bool PASSING>
 __global__ __launch_bounds__(64 * kWaves, tile_occupancy(DT)) void bcq_attend_chunk_kernel(AttendParams p)
 {
     constexpr int KB = tile_keys(DT), DV = DT / 32;
+    __shared__ __attribute__((aligned(1024))) uint16_t k0[KB * DT], k1[KB * DT], v0[KB * DT], v1[KB * DT];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r32 = lane & 31, h = lane >> 5;
 
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(64 * kWaves, tile_occupancy(DT)) void bcq_attend_ch
     t.q = p.q + (long long)(q.start + (real ? token : 0)) * p.ld_q + (head * p.group + (real ? member : 0)) * p.head_dim;
     f32x16 o[DV];
     float most, sum;
-    attend_tile<DT, BF, ANY, PASSING>(p, t, o, most, sum);
+    attend_tile<DT, BF, ANY, PASSING>(p, t, k0, k1, v0, v1, o, most, sum);
 
     // ---- results: lane (h, r32) has of row r32 the elements 32 d + 8 u + 4 h + i in number 4 u + i of o[d] ----
     const auto twin = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, sum), __builtin_bit_cast(unsigned, sum), false, false);

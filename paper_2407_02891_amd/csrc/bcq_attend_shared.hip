@@ -2,13 +2,14 @@
 //
 //   out = sum_j softmax_j(scale q . k_j) v_j = join of (sums over the shared keys) and (sums over the request's own)
 //
-// A row is a (new token, query head) pair.  The rows of all requests of a group are the tiles of the shared keys (bcq_attend_tile.h), the rows of a request
-// those of its own keys.  Bound by the matrix instructions where many rows share much, by the bytes of K and V where few do, or own much.
-//  * The blocks of keys of the shared tiles form one line, those of the others a second.  Each is cut into as many equal pieces as there are workgroups for a kv head, and a
-//    workgroup has one of each: half of them begin with the first, half with the second, so that what is bound by the matrix instructions runs beside what is bound by memory.  A
-//    workgroup walks its pieces, over the ends of tiles, and leaves sums, maximum and weight of each row of a tile (place: the row, and 128 further for each worker, which no
-//    two share).  The lengths are on the device, so a first launch lays out the lines.
-//  * A last launch joins what was left of a row: of its shared keys and of its own.
+// A row is a (new token, query head) pair.  The rows of all requests of a group are the tiles of the shared keys: bound by the matrix instructions where there are many.  The
+// rows of a request are a tile of its own keys: bound by the bytes of K and V where they are few.  One launch does both, so that each runs beside the other.
+//  * Tiles of up to 128 rows (bcq_attend_tile.h): their blocks of keys form a line, shared keys first.  The own keys of requests with up to 16 rows form a second line,
+//    of blocks of 32, which single waves stream as the kernel for few rows (bcq_attend.hip) does, four of them independent of each other in a workgroup.
+//  * A compute unit has two workgroups of a kv head.  The first has a piece of the line of tiles, the second a piece of the other; who would be through first has a piece of
+//    the other's line too (cuts below).  They walk their pieces over the ends of tiles and requests and leave sums, maximum and weight of each row (place: the row, and 128 or 16
+//    further for each piece, which no two share).
+//  * The lengths are on the device, so a first launch lays out the lines.  A last one joins what was left of a row: of its shared keys and of its own.
 #include "bcq_attend_tile.h"
 
 namespace bcq {
@@ -17,11 +18,13 @@ namespace {
 
 constexpr int kLineThreads = 1024;
 constexpr int kJoinThreads = 256;
+constexpr int kFewRows = 16, kFewKeys = 32;  // of a request whose own keys are streamed; of a block of them
+constexpr bool streams(int dim) { return dim <= 128; }  // (heads of 256: the waves' blocks would be more LDS than two tiles')
 
-// A tile and its place in its line (64 bytes, one scalar load).
+// A tile and its place in its line.
 struct Slot {
-    int upto;         // blocks of the line up to and with it
-    int part;         // whose tile: of a group's shared keys (below `groups`), of a request's own; -1: nobody's
+    int upto;         // blocks of the line of tiles up to and with it
+    int few_upto;     // the same of the other line
     int row0;         // its first row in the part
     int block;        // its first block of keys
     int start, rows;  // of the part: first token; rows
@@ -29,19 +32,22 @@ struct Slot {
     int requests;     // of a group; a request's group, or -1
     int from, to;     // keys of the part
     int n, len;       // of a request: new tokens, keys; of a group: whether each row sees all of the keys
-    int worker;       // the first that has a block of it
+    int piece;        // the first that has a block of it
     int pieces;       // how many have
-    int unused[2];
+    int part;         // whose tile: of a group's shared keys (below `groups`), of a request's own; -1: nobody's
+    int few;          // whether it is of the other line
+    int group_start, group_slot;  // of a request: first token and slot of its group
 };
-static_assert(sizeof(Slot) == 64, "");
 
 struct SharedParams {
     AttendParams a;  // (workers, part, stat too)
     const int *group_start, *shared_len;
     int groups, max_shared;
     Slot *slots;
+    int *sums;                 // three numbers for each slot
     int num_slots, own_slots;  // the slots of requests' own keys begin at own_slots
-    long long space;           // rows that a kv head's sums have room for, of each line
+    int few;                   // whether there may be requests of few rows, whose own keys are streamed
+    long long space, own_place, few_place;  // rows that a kv head's sums have room for; where those of own keys' tiles begin, and of the other line
 };
 
 __device__ __forceinline__ int start_of(const SharedParams &p, int r) { return min(max(p.a.q_start[r], 0), p.a.tokens); }
@@ -64,6 +70,26 @@ __device__ __forceinline__ int group_of(const SharedParams &p, int r)
     return p.groups > 0 && first_of_group(p, low) <= r && r < first_of_group(p, low + 1) ? low : -1;
 }
 
+// A line's blocks [0, middle) are cut into w0 pieces, the others into w1 more.
+struct Cut {
+    int total, middle, w0, w1;
+    __device__ __forceinline__ Cut(int total, int others, int most0, int most1) : total(total), middle(total - others), w0(min(most0, max(middle, 1))), w1(min(most1, max(others, 1))) {}
+    __device__ __forceinline__ int begin(int piece) const { return piece < w0 ? first_block(piece, w0, middle) : middle + first_block(piece - w0, w1, total - middle); }
+    __device__ __forceinline__ int end(int piece) const { return piece < w0 ? first_block(piece + 1, w0, middle) : middle + first_block(piece - w0 + 1, w1, total - middle); }
+    __device__ __forceinline__ int piece_of(int block) const { return block < middle ? worker_of(block, w0, middle) : w0 + worker_of(block - middle, w1, total - middle); }
+};
+
+// The first half of the workgroups has the line of tiles, the second the other; what of a line the other half helps with.  A workgroup takes 2.2 us for a tile's block, beside one that
+// streams or another of its kind (1.5 alone), and 0.9 for four waves' blocks of the other line; to begin with tiles costs as much as two of their blocks.
+struct Cuts {
+    Cut tiles, few;
+    __device__ __forceinline__ Cuts(int half, int rest, int tiles, int few)
+        : tiles(tiles, half == 0 ? tiles : tiles <= half ? 0 : max(0, (tiles - (int)(0.4f * few)) / 2 - 2 * rest), half, rest),
+          few(few, few <= kTileWaves * rest ? 0 : min(max(0, (few - (int)(1.85f * tiles)) / 2), half ? few : 0), kTileWaves * rest, kTileWaves * half)
+    {
+    }
+};
+
 // The tiles of a part begin at this slot.
 __device__ __forceinline__ int slots_before(const SharedParams &p, int v, int start)
 {
@@ -75,130 +101,432 @@ __device__ __forceinline__ int slots_before(const SharedParams &p, int v, int st
 __device__ __forceinline__ Slot load_slot(const SharedParams &p, int slot)
 {
     typedef const __attribute__((address_space(4))) int *scalar_int;
-    const scalar_int from = (scalar_int) reinterpret_cast<const int *>(p.slots + __builtin_amdgcn_readfirstlane(slot));
+    slot = __builtin_amdgcn_readfirstlane(slot);
+    asm volatile("" : "+s"(slot));
+    const scalar_int from = (scalar_int) reinterpret_cast<const int *>(p.slots + slot);
     Slot s;
-    s.upto = from[0], s.part = from[1], s.row0 = from[2], s.block = from[3], s.start = from[4], s.rows = from[5], s.request = from[6];
-    s.requests = from[7], s.from = from[8], s.to = from[9], s.n = from[10], s.len = from[11], s.worker = from[12], s.pieces = from[13];
+    s.upto = from[0], s.few_upto = from[1], s.row0 = from[2], s.block = from[3], s.start = from[4], s.rows = from[5], s.request = from[6];
+    s.requests = from[7], s.from = from[8], s.to = from[9], s.n = from[10], s.len = from[11], s.piece = from[12], s.pieces = from[13];
+    s.part = from[14], s.few = from[15];
     return s;
 }
 
 }  // namespace
 
-// Lays out the lines: the tiles of each part, then the sums of their blocks, then who has them.
+// What a slot of a part holds, but for what follows from the sums.
 template <int DT>
-__global__ __launch_bounds__(kLineThreads) void bcq_attend_shared_line_kernel(SharedParams p)
+__device__ __forceinline__ Slot make_slot(const SharedParams &p, int v, int slot, int &first_slot)
 {
     constexpr int KB = tile_keys(DT);
-    __shared__ int sums[kLineThreads / 64];
     const AttendParams &a = p.a;
-    const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
-    for (int s = thread; s < p.num_slots; s += kLineThreads) p.slots[s].upto = 0, p.slots[s].part = -1;
-    __syncthreads();
-    for (int v = thread; v < p.groups; v += kLineThreads) {
+    Slot q = {};
+    q.part = v;
+    if (v < p.groups) {
         const int first = first_of_group(p, v), end = max(first_of_group(p, v + 1), first);
-        Slot q = {};
-        q.part = v;
         q.start = start_of(p, first);
         q.rows = max(start_of(p, end) - q.start, 0) * a.group;
         q.request = min(first, a.requests - 1);
         q.requests = end - first;
         q.to = shared_keys(p, v);
+        first_slot = slots_before(p, v, q.start);
+        q.row0 = (slot - first_slot) * kChunkRows;
         q.n = a.window == 0;
         q.upto = (q.to + KB - 1) / KB;
-        for (int s = slots_before(p, v, q.start); q.row0 < q.rows && s < p.own_slots; q.row0 += kChunkRows, ++s) p.slots[s] = q;
+        return q;
     }
-    __syncthreads();
-    for (int r = thread; r < a.requests; r += kLineThreads) {
-        const Request own = load_request(a, r);
-        const int c = group_of(p, r);
-        Slot q = {};
-        q.part = p.groups + r;
-        q.start = own.start;
-        q.rows = own.todo * a.group;
-        q.request = r;
-        q.requests = c;
-        q.from = c < 0 ? 0 : shared_keys(p, c);
-        q.to = own.len;
-        q.n = own.n, q.len = own.len;
-        for (int s = slots_before(p, q.part, q.start); q.row0 < q.rows && s < p.num_slots; q.row0 += kChunkRows, ++s) {
-            // the keys that a row of the tile sees
-            int low, high, unused;
-            visible_keys(a, own.n, own.len, q.row0 / a.group, low, unused);
-            visible_keys(a, own.n, own.len, (min(q.row0 + kChunkRows, q.rows) - 1) / a.group, unused, high);
-            low = max(low, q.from);
-            q.block = low / KB;
-            q.upto = low < high ? (high + KB - 1) / KB - q.block : 0;
-            p.slots[s] = q;
-        }
-        // does each of its rows see all that is shared?
-        int unused, high;
-        visible_keys(a, own.n, own.len, 0, unused, high);
-        if (c >= 0 && own.n > 0 && (high < q.from || own.todo < own.n)) {
-            const int first = start_of(p, first_of_group(p, c)), rows = max(start_of(p, first_of_group(p, c + 1)) - first, 0) * a.group;
-            const int s = slots_before(p, c, first);
-            for (int i = 0; i * kChunkRows < rows && s + i < p.own_slots; ++i) p.slots[s + i].n = 0;
-        }
+    const int r = v - p.groups, c = group_of(p, r);
+    const Request own = load_request(a, r);
+    q.start = own.start;
+    q.rows = own.todo * a.group;
+    q.request = r;
+    q.requests = c;
+    q.to = own.len;
+    q.n = own.n, q.len = own.len;
+    q.few = p.few && q.rows <= kFewRows;
+    if (c >= 0) {
+        q.from = shared_keys(p, c);
+        q.group_start = start_of(p, first_of_group(p, c));
+        q.group_slot = slots_before(p, c, q.group_start);
     }
-    __syncthreads();
-    const auto lay = [&](int first, int end) {
-        int before = 0;
-        for (int c = first; c < end; c += kLineThreads) {
-            const int s = c + thread;
-            const int upto = prefix_sum(s < end ? p.slots[s].upto : 0, lane);
-            if (lane == 63) sums[wave] = upto;
-            __syncthreads();
-            int mine = before + upto;
-            for (int w = 0; w < kLineThreads / 64; ++w) {
-                if (w < wave) mine += sums[w];
-                before += sums[w];
-            }
-            if (s < end) p.slots[s].upto = mine;
-            __syncthreads();
-        }
-        const int workers = min(a.workers, max(before, 1));
-        for (int s = first + thread; s < end; s += kLineThreads) {
-            const int from = s > first ? p.slots[s - 1].upto : 0, upto = p.slots[s].upto;
-            const int w0 = upto > from ? worker_of(from, workers, before) : 0;
-            p.slots[s].worker = w0;
-            p.slots[s].pieces = upto > from ? worker_of(upto - 1, workers, before) - w0 + 1 : 0;
-        }
-    };
-    lay(0, p.own_slots);
-    lay(p.own_slots, p.num_slots);
+    first_slot = slots_before(p, v, q.start);
+    q.row0 = (slot - first_slot) * kChunkRows;
+    return q;
 }
 
-// The pieces of both lines.
-template <int DT, bool BF, bool ANY>
+// Blocks of keys that a row of a request's tile sees.
+template <int DT>
+__device__ __forceinline__ void own_blocks(const SharedParams &p, Slot &q)
+{
+    const AttendParams &a = p.a;
+    int low, high, unused;
+    visible_keys(a, q.n, q.len, q.row0 / a.group, low, unused);
+    visible_keys(a, q.n, q.len, (min(q.row0 + kChunkRows, q.rows) - 1) / a.group, unused, high);
+    low = max(low, q.from);
+    const int keys = q.few ? kFewKeys : tile_keys(DT);
+    q.block = low / keys;
+    (q.few ? q.few_upto : q.upto) = low < high ? (high + keys - 1) / keys - q.block : 0;
+}
+
+// Lays out the lines: the blocks of each part's tiles, their sums, then what the slots hold.  sums: of each slot the two sums and whose it is (bit 31 of a group's: a row of it does
+// not see all keys), in LDS where they are few.
+template <int DT>
+__global__ __launch_bounds__(kLineThreads) void bcq_attend_shared_line_kernel(SharedParams p)
+{
+    constexpr int kLocal = 3072 / 3;
+    __shared__ int local[3 * kLocal], sums[kLineThreads / 64][2];
+    const AttendParams &a = p.a;
+    const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, n = p.num_slots;
+    int *const upto = n <= kLocal ? local : p.sums, *const few_upto = upto + n, *const owner = few_upto + n;
+    for (int s = thread; s < 3 * n; s += kLineThreads) upto[s] = s < 2 * n ? 0 : -1;
+    __syncthreads();
+    const auto parts = p.groups + a.requests;
+    for (int v = thread; v < parts; v += kLineThreads) {
+        int slot;
+        Slot q = make_slot<DT>(p, v, 0, slot);
+        const int end_slot = v < p.groups ? p.own_slots : n;
+        q.row0 = 0;
+        for (int s = slot; q.row0 < q.rows && s < end_slot; q.row0 += kChunkRows, ++s) {
+            if (v >= p.groups) own_blocks<DT>(p, q);
+            upto[s] = q.upto, few_upto[s] = q.few_upto, owner[s] = v;
+        }
+    }
+    __syncthreads();
+    for (int r = thread; r < a.requests; r += kLineThreads) {  // does each of its rows see all that is shared?
+        const Request own = load_request(a, r);
+        const int c = group_of(p, r);
+        int unused, high;
+        visible_keys(a, own.n, own.len, 0, unused, high);
+        if (c < 0 || own.n == 0 || (high >= shared_keys(p, c) && own.todo == own.n)) continue;
+        const int first = start_of(p, first_of_group(p, c)), rows = max(start_of(p, first_of_group(p, c + 1)) - first, 0) * a.group;
+        const int s = slots_before(p, c, first);
+        for (int i = 0; i * kChunkRows < rows && s + i < p.own_slots; ++i) atomicOr(owner + s + i, 1 << 30);
+    }
+    __syncthreads();
+    int before = 0, few_before = 0;
+    for (int c = 0; c < n; c += kLineThreads) {
+        const int s = c + thread;
+        const int tiles = prefix_sum(s < n ? upto[s] : 0, lane), few = prefix_sum(s < n ? few_upto[s] : 0, lane);
+        if (lane == 63) sums[wave][0] = tiles, sums[wave][1] = few;
+        __syncthreads();
+        int mine = before + tiles, few_mine = few_before + few;
+        for (int w = 0; w < kLineThreads / 64; ++w) {
+            if (w < wave) mine += sums[w][0], few_mine += sums[w][1];
+            before += sums[w][0], few_before += sums[w][1];
+        }
+        if (s < n) upto[s] = mine, few_upto[s] = few_mine;
+        __syncthreads();
+    }
+    const Cuts cuts(a.workers / 2, a.workers - a.workers / 2, before, few_before);
+    for (int s = thread; s < n; s += kLineThreads) {
+        Slot q = {};
+        q.part = -1;
+        if (owner[s] >= 0) {
+            int unused;
+            q = make_slot<DT>(p, owner[s] & ~(1 << 30), s, unused);
+            if (q.part >= p.groups) own_blocks<DT>(p, q);
+            if (owner[s] >> 30) q.n = 0;
+        }
+        q.upto = upto[s], q.few_upto = few_upto[s];
+        const int to = q.few ? q.few_upto : q.upto, from = s == 0 ? 0 : q.few ? few_upto[s - 1] : upto[s - 1];
+        if (to > from) {
+            const Cut cut = q.few ? cuts.few : cuts.tiles;
+            q.piece = cut.piece_of(from);
+            q.pieces = cut.piece_of(to - 1) - q.piece + 1;
+        }
+        p.slots[s] = q;
+    }
+}
+
+namespace {
+
+// The slot that holds block `at` of a line: the first with upto(slot) > at (all lanes).
+template <class F>
+__device__ __forceinline__ int slot_of(const SharedParams &p, int lane, int at, F upto)
+{
+    int slot = 0;
+    for (int high = p.num_slots - 1; slot < high;) {
+        const int stride = (high - slot + 63) / 64, probe = slot + lane * stride;
+        const int beyond = __popcll(__ballot(probe < high && upto(probe) <= at));  // (rises, so these are the first lanes)
+        if (!beyond) break;
+        const int last = slot + (beyond - 1) * stride;  // not yet
+        high = min(high, last + stride);
+        slot = last + 1;
+    }
+    return __builtin_amdgcn_readfirstlane(slot);
+}
+
+template <bool BF>
+using FewWeights = Weights<BF, 1>;
+
+// One wave: blocks [at, stop) of the line of requests with few rows, a piece of it; ks: LDS, 2 * kFewKeys * DT elements of the wave's own.  Column r16 of the products is token r16 / group, query
+// head r16 mod group.  K and V come in whole rows and pass through LDS, the next block's are on their way; weights meet the values as the sum of two 16-bit numbers.
+template <int DT, bool BF, bool ANY, bool PASSING>
+__device__ __forceinline__ void stream_piece(const SharedParams &p, int head, int piece, int at, int stop, uint16_t *const ks)
+{
+    constexpr int C = DT / 32, DV = DT / 16;                    // matrix steps over head_dim; tiles of O
+    constexpr int kRowLanes = DT / 8, kRows = 64 / kRowLanes;   // a load covers kRows keys
+    const AttendParams &a = p.a;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));  // (what follows from it is not worth registers beside the tiles)
+    const int r16 = lane & 15, g = lane >> 4;
+    uint16_t *const vs = ks + kFewKeys * DT;
+    // element d of key j in LDS: units of a row (8 elements of K, 16 of V) exchanged by the key, so that the units of one number fill all banks
+    const auto k_at = [&](int key, int d) { return ks + key * DT + ((d >> 3 ^ (DT == 64 ? key >> 1 & 7 : key & 15)) << 3); };
+    const auto v_at = [&](int key, int d) {
+        const int turn = DT == 64 ? key >> 1 & 3 : key & 7;
+        return vs + key * DT + ((d >> 4 ^ turn) << 4) + (d & 15);
+    };
+    const int token = r16 / a.group, member = r16 - token * a.group;
+    // where the block is that is computed, the one that is on its way, the one whose pages are looked up
+    struct Place {
+        Slot s;
+        int key;
+    };
+    int slot = slot_of(p, lane, at, [&](int s) { return p.slots[s].few_upto; });
+    int before = slot ? load_slot(p, slot - 1).few_upto : 0;
+    Place now, next, ahead;
+    ahead.s = load_slot(p, slot);
+    const auto look_at = [&](int block) {
+        while (block >= ahead.s.few_upto) before = ahead.s.few_upto, ahead.s = load_slot(p, ++slot);
+        ahead.key = (ahead.s.block + block - before) * kFewKeys;
+    };
+    look_at(at);
+    const int in_rows = lane / kRowLanes, d_own = 8 * (lane % kRowLanes);
+    const long long head_offset = head * a.head_stride;
+    int dim = a.head_dim;
+    u32x4 kr[2][C], vr[2][C];
+    int id[2];  // page numbers of the block that is requested next
+    const auto find_pages = [&](const Place &b) {
+        if (ANY) return;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) id[t] = page_of_all(a, b.s.request, min(b.key + 16 * t, max(b.s.len - 1, 0) & ~15));
+    };
+    const auto request = [&](const Place &b) {
+        const Slot &s = b.s;
+        const int last = max(s.len - 1, 0);
+        if (ANY) asm volatile("" : "+v"(dim));  // (compared here, not held as masks through the loop)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int key = min(b.key + 16 * t, last & ~15);  // keys behind the last are the last's copies, and masked
+            if (!ANY) {
+                const long long base = __builtin_amdgcn_readfirstlane(id[t]) * a.page_stride + head_offset + (long long)((key & ((1 << a.page_shift) - 1)) * a.slot_stride);
+                const char *const kp = reinterpret_cast<const char *>(a.k + base), *const vp = reinterpret_cast<const char *>(a.v + base);
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const unsigned off = 2 * (unsigned)(min(c * kRows + in_rows, last - key) * a.slot_stride + d_own);
+                    const u32x4 *const ka = reinterpret_cast<const u32x4 *>(kp + off), *const va = reinterpret_cast<const u32x4 *>(vp + off);
+                    if (PASSING) kr[t][c] = __builtin_nontemporal_load(ka), vr[t][c] = __builtin_nontemporal_load(va);
+                    else kr[t][c] = *ka, vr[t][c] = *va;
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const int j = min(key + c * kRows + in_rows, last);
+                    const long long place = page_of(a, s.request, j) * a.page_stride + head_offset + (long long)((j & ((1 << a.page_shift) - 1)) * a.slot_stride);
+                    kr[t][c] = *reinterpret_cast<const u32x4 *>(d_own < dim ? a.k + place + d_own : g_zeros);
+                    vr[t][c] = *reinterpret_cast<const u32x4 *>(d_own < dim ? a.v + place + d_own : g_zeros);
+                }
+            }
+        }
+    };
+    find_pages(ahead);
+    request(ahead);
+    now = next = ahead;
+    if (at + 1 < stop) {
+        look_at(at + 1);
+        find_pages(ahead);
+    }
+    u32x4 q[C];
+    f32x4 o[DV];
+    float most, base, sum;
+    int from, to;          // keys that the row sees
+    int all_from, all_to;  // keys that every row sees
+    const auto begin_request = [&](const Slot &s) {
+        int unused;
+        visible_keys(a, s.n, s.len, 0, unused, all_to);
+        visible_keys(a, s.n, s.len, s.rows / a.group - 1, all_from, unused);
+        visible_keys(a, s.n, s.len, token, from, to);
+        all_from = max(all_from, s.from), from = max(from, s.from);
+        most = -INFINITY;
+        base = sum = 0.0f;
+#pragma unroll
+        for (int d = 0; d < DV; ++d) o[d] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        const bool real = r16 < s.rows;
+        const uint16_t *const src = a.q + (long long)(s.start + (real ? token : 0)) * a.ld_q + (head * a.group + member) * a.head_dim;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            q[c] = u32x4{0, 0, 0, 0};
+            if (real && (!ANY || 32 * c + 8 * g < dim)) q[c] = *reinterpret_cast<const u32x4 *>(src + 32 * c + 8 * g);
+        }
+    };
+    begin_request(now.s);
+#pragma unroll 1
+    for (;;) {
+        const int key0 = now.key;
+        const bool masked = key0 + kFewKeys > all_to || key0 < all_from;
+        // Infinities or NaN among the values: zero times them must not reach the rows that do not see them, nor must the second number of a weight, which may be zero or
+        // negative, or a weight too small for its type, make a NaN of an infinity.  They are replaced by zeros, and what they make of the rows that do see them is found by products of ones.
+        float zero = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) zero = times_zero<BF>(vr[t][c][i], zero);
+        const bool odd = __ballot(zero != 0.0f) != 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                *reinterpret_cast<u32x4 *>(k_at(16 * t + c * kRows + in_rows, d_own)) = kr[t][c];
+                *reinterpret_cast<u32x4 *>(v_at(16 * t + c * kRows + in_rows, d_own)) = vr[t][c];
+            }
+        ++at;
+        const bool through = at == now.s.few_upto || at == stop;  // with this request, or this piece of it
+        if (at < stop) {
+            request(ahead);
+            next = ahead;
+            if (at + 1 < stop) {
+                look_at(at + 1);
+                find_pages(ahead);
+            }
+        }
+        f32x4 s[2];
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int c = 0; c < C; ++c) s[t] = mfma16<BF>(*reinterpret_cast<const u32x4 *>(k_at(16 * t + r16, 32 * c + 8 * g)), q[c], s[t]);
+        }
+        // weights: number 4 t + i of a lane is key 16 t + 4 g + i
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = s[e >> 2][e & 3] * a.scale;
+        if (masked) {
+            const unsigned span = max(to - from, 0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = (unsigned)(key0 + 16 * (e >> 2) + 4 * g + (e & 3) - from) < span ? x[e] : -INFINITY;
+        }
+        float high = x[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) high = fmaxf(high, x[e]);
+        if (__ballot(high > most + FewWeights<BF>::grow)) {
+            const float m = fmaxf(most, max_over_groups(high));
+            const float shrink = most == -INFINITY ? 1.0f : shrink_by(most - m);
+            most = m;
+            base = m == -INFINITY ? 0.0f : m - FewWeights<BF>::lift;
+            sum *= shrink;
+#pragma unroll
+            for (int d = 0; d < DV; ++d) o[d] *= shrink;
+        }
+        u32x4 high_part, low_part;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float w0 = exp2_fast(x[e] - base), w1 = exp2_fast(x[e + 1] - base);
+            sum += w0 + w1;
+            const uint32_t pair = from_float2<BF>(w0, w1);
+            const f32x2 kept = to_float2<BF>(pair);
+            high_part[e / 2] = pair;
+            low_part[e / 2] = from_float2<BF>(w0 - kept.x, w1 - kept.y);
+        }
+        asm volatile("" ::: "memory");
+        const auto column = [&](int d) {  // the operand V^T: elements 16 d + r16 of keys 4 g .. and 16 + 4 g ..
+            const u32x2 v0 = lds_column(v_at(lane >> 2, 16 * d + 4 * (lane & 3))), v1 = lds_column(v_at(16 + (lane >> 2), 16 * d + 4 * (lane & 3)));
+            return u32x4{v0.x, v0.y, v1.x, v1.y};
+        };
+        if (odd) {
+            u32x4 sees;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int key = key0 + 16 * (e >> 1) + 4 * g + 2 * (e & 1);
+                sees[e] = (key >= from && key < to ? kOne<BF> : 0u) | (key + 1 >= from && key + 1 < to ? kOne<BF> << 16 : 0u);
+            }
+#pragma unroll
+            for (int d = 0; d < DV; ++d) {
+                const u32x4 v = column(d);
+                u32x4 up, down;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) up[e] = ones_where_infinite<BF>(v[e], 0), down[e] = ones_where_infinite<BF>(v[e], 0x8000u);
+                const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+                const f32x4 ups = mfma16<BF>(up, sees, none), downs = mfma16<BF>(down, sees, none);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[d][i] += (ups[i] > 0.0f ? INFINITY : 0.0f) - (downs[i] > 0.0f ? INFINITY : 0.0f);
+                __builtin_amdgcn_sched_barrier(0);  // (rare: registers count, not time)
+            }
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    u32x4 *const mine = reinterpret_cast<u32x4 *>(v_at(16 * t + c * kRows + in_rows, d_own));
+                    u32x4 v = *mine;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = finite_only<BF>(v[i]);
+                    *mine = v;
+                }
+            asm volatile("" ::: "memory");
+        }
+#pragma unroll
+        for (int d = 0; d < DV; ++d) {
+            const u32x4 v = column(d);
+            o[d] = mfma16<BF>(v, low_part, mfma16<BF>(v, high_part, o[d]));
+        }
+        asm volatile("" ::: "memory");
+        if (!through) {
+            now.key = next.key;
+            continue;
+        }
+        const float weight = sum_over_groups(sum);
+        if (r16 < now.s.rows) {
+            const long long place = head * p.space + p.few_place + (long long)now.s.start * a.group + r16 + (long long)kFewRows * piece;
+#pragma unroll
+            for (int d = 0; d < DV; ++d) *reinterpret_cast<f32x4 *>(a.part + place * DT + 16 * d + 4 * g) = o[d];
+            // (the tiles' weights are less: what both leave is relative to the maximum less the tiles' lift)
+            if (g == 0) a.stat[place] = f32x2{most - (FewWeights<BF>::lift - TileWeights<BF>::lift), weight};
+        }
+        if (at == stop) return;
+        now = next;
+        begin_request(now.s);
+    }
+}
+
+}  // namespace
+
+// The pieces of both lines.  PASSING: what is streamed leaves nothing in the caches.
+template <int DT, bool BF, bool ANY, bool PASSING>
 __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_attend_shared_kernel(SharedParams p)
 {
-    constexpr int DV = DT / 32;
+    constexpr int KB = tile_keys(DT), DV = DT / 32;
+    __shared__ __attribute__((aligned(1024))) uint16_t k0[KB * DT], k1[KB * DT], v0[KB * DT], v1[KB * DT];
+    static_assert(!streams(DT) || KB * DT >= 2 * kFewKeys * DT, "");
     __shared__ int bounds[kTileWaves][2];
     const AttendParams &a = p.a;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r32 = lane & 31, h = lane >> 5;
-    const int head = blockIdx.x % a.kv_heads, me = blockIdx.x / a.kv_heads;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = blockIdx.x % a.kv_heads, me = blockIdx.x / a.kv_heads, half = a.workers / 2;
+    const bool first_half = me < half;
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
-        // the second line is shared out from the last worker on: few blocks of each are then not one worker's
-        const bool of_group = (turn == 0) == (2 * me < a.workers);
-        const int first_slot = of_group ? 0 : p.own_slots, end_slot = of_group ? p.own_slots : p.num_slots;
-        const int total = load_slot(p, end_slot - 1).upto, workers = min(a.workers, max(total, 1)), worker = of_group ? me : a.workers - 1 - me;
-        if (worker >= workers) continue;
-        int at = first_block(worker, workers, total);
-        const int stop = first_block(worker + 1, workers, total);
-        if (at >= stop) continue;
-        // the slot that holds block `at`: the first with upto > at
-        int slot = first_slot;
-        for (int high = end_slot - 1; slot < high;) {
-            const int stride = (high - slot + 63) / 64, probe = slot + lane * stride;
-            const int beyond = __popcll(__ballot(probe < high && p.slots[probe].upto <= at));  // (rises, so these are the first lanes)
-            if (!beyond) break;
-            const int last = slot + (beyond - 1) * stride;  // not yet
-            high = min(high, last + stride);
-            slot = last + 1;
+        const Slot end_slot = load_slot(p, p.num_slots - 1);  // (again in each turn: not worth registers)
+        const Cuts cuts(half, a.workers - half, end_slot.upto, end_slot.few_upto);
+        if ((turn == 0) != first_half) {
+            if constexpr (streams(DT)) {
+                const int mine = kTileWaves * (first_half ? me : me - half) + wave;
+                if (mine < (first_half ? cuts.few.w1 : cuts.few.w0)) {
+                    const int piece = first_half ? cuts.few.w0 + mine : mine, at = cuts.few.begin(piece), stop = cuts.few.end(piece);
+                    if (at < stop) stream_piece<DT, BF, ANY, PASSING>(p, head, piece, at, stop, wave == 0 ? k0 : wave == 1 ? k1 : wave == 2 ? v0 : v1);
+                }
+                __syncthreads();  // (the tiles' buffers)
+            }
+            continue;
         }
-        slot = __builtin_amdgcn_readfirstlane(slot);
-        int before = slot > first_slot ? load_slot(p, slot - 1).upto : 0;
+        const int mine = first_half ? me : me - half, piece = first_half ? mine : cuts.tiles.w0 + mine;
+        if (mine >= (first_half ? cuts.tiles.w0 : cuts.tiles.w1)) continue;
+        int at = __builtin_amdgcn_readfirstlane(cuts.tiles.begin(piece));
+        const int stop = __builtin_amdgcn_readfirstlane(cuts.tiles.end(piece));
+        if (at >= stop) continue;
+        int slot = slot_of(p, threadIdx.x & 63, at, [&](int s) { return p.slots[s].upto; });
+        int before = slot ? load_slot(p, slot - 1).upto : 0;
 #pragma unroll 1
         for (; at < stop; ++slot) {
             const Slot s = load_slot(p, slot);
@@ -207,7 +535,11 @@ __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_atten
                 before = s.upto;
                 continue;
             }
+            const bool of_group = s.part < p.groups;
             // ---- the lane's row, and what it sees ----
+            int lane = threadIdx.x & 63;
+            asm volatile("" : "+v"(lane));  // (the same beside what is streamed)
+            const int r32 = lane & 31, h = lane >> 5;
             const int row = s.row0 + 32 * wave + r32;
             const int token = row / a.group, member = row - token * a.group;
             bool real = row < s.rows;
@@ -270,12 +602,13 @@ __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_atten
             t.q = a.q + (long long)(real ? s.start + token : min(s.start, a.tokens - 1)) * a.ld_q + (head * a.group + (real ? member : 0)) * a.head_dim;
             f32x16 o[DV];
             float most, sum;
-            const bool reading = attend_tile<DT, BF, ANY, false>(a, t, o, most, sum);
+            __builtin_amdgcn_s_setprio(2);  // (beside a workgroup that streams: 256 requests behind 32768 keys 380 us, 404 without)
+            const bool reading = attend_tile<DT, BF, ANY, false>(a, t, k0, k1, v0, v1, o, most, sum);
 
             const auto twin = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, sum), __builtin_bit_cast(unsigned, sum), false, false);
             sum = __builtin_bit_cast(float, (unsigned)twin[0]) + __builtin_bit_cast(float, (unsigned)twin[1]);
             if (real) {
-                const long long place = (2ll * head + (of_group ? 0 : 1)) * p.space + (long long)s.start * a.group + row + (long long)kChunkRows * worker;
+                const long long place = head * p.space + (of_group ? 0 : p.own_place) + (long long)s.start * a.group + row + (long long)kChunkRows * piece;
 #pragma unroll
                 for (int d = 0; d < DV; ++d)
 #pragma unroll
@@ -288,6 +621,8 @@ __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_atten
             before = s.upto;
             if (reading) __syncthreads();
         }
+        __builtin_amdgcn_s_setprio(0);
+        __syncthreads();  // (before the waves' own blocks take the tiles' buffers)
     }
 }
 
@@ -295,7 +630,7 @@ __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_atten
 template <int DT, bool BF>
 __global__ __launch_bounds__(kJoinThreads) void bcq_attend_shared_join_kernel(SharedParams p)
 {
-    constexpr int kLanes = DT / 4, kAhead = 4;
+    constexpr int kLanes = DT / 4, kAhead = 8;
     const AttendParams &a = p.a;
     const int head = blockIdx.x % a.kv_heads, row = blockIdx.x / a.kv_heads * (kJoinThreads / kLanes) + (int)threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
     const int token = row / a.group, member = row - token * a.group;
@@ -317,16 +652,16 @@ __global__ __launch_bounds__(kJoinThreads) void bcq_attend_shared_join_kernel(Sh
     const Slot &mine = p.slots[min(s1, p.num_slots - 1)];
     const int c = mine.requests;
     int pieces0 = 0, pieces = mine.pieces;
-    const long long place1 = (2ll * head + 1) * p.space + (long long)token * a.group + member + (long long)kChunkRows * mine.worker;
+    const int step1 = mine.few ? kFewRows : kChunkRows;
+    const long long place1 = head * p.space + (mine.few ? p.few_place : p.own_place) + (long long)token * a.group + member + (long long)step1 * mine.piece;
     long long place0 = 0;
     if (c >= 0) {
-        const int start = start_of(p, first_of_group(p, c));
-        const Slot &shared = p.slots[min(slots_before(p, c, start) + max((token - start) * a.group + member, 0) / kChunkRows, p.own_slots - 1)];
+        const Slot &shared = p.slots[min(mine.group_slot + max((token - mine.group_start) * a.group + member, 0) / kChunkRows, p.own_slots - 1)];
         pieces0 = shared.pieces;
-        place0 = 2ll * head * p.space + (long long)token * a.group + member + (long long)kChunkRows * shared.worker;
+        place0 = head * p.space + (long long)token * a.group + member + (long long)kChunkRows * shared.piece;
     }
     pieces += pieces0;
-    const auto at = [&](int n) { return n < pieces0 ? place0 + (long long)n * kChunkRows : place1 + (long long)(n - pieces0) * kChunkRows; };
+    const auto at = [&](int n) { return n < pieces0 ? place0 + (long long)n * kChunkRows : place1 + (long long)(n - pieces0) * step1; };
     f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
     float most = -INFINITY, weight = 0.0f;
     for (int n = 0; n < pieces; n += kAhead) {
@@ -366,11 +701,11 @@ __global__ __launch_bounds__(kJoinThreads) void bcq_attend_shared_join_kernel(Sh
 namespace {
 
 struct SharedPlan {
-    int dim, workers, num_slots, own_slots;
-    long long space;
+    int dim, workers, num_slots, own_slots, few;
+    long long space, own_place, few_place;
     size_t slot_bytes, part_bytes, stat_bytes;
 };
-SharedPlan shared_plan(const bcq_cache &c, int tokens, int requests, int groups, int q_heads)
+SharedPlan shared_plan(const bcq_cache &c, int tokens, int requests, int groups, int q_heads, int max_new)
 {
     SharedPlan s;
     s.dim = c.head_dim <= 64 ? 64 : c.head_dim <= 128 ? 128 : 256;
@@ -379,39 +714,46 @@ SharedPlan shared_plan(const bcq_cache &c, int tokens, int requests, int groups,
     s.workers = per_head > 1 ? per_head : 1;
     s.own_slots = (int)((long long)tokens * group / kChunkRows) + groups + 1;
     s.num_slots = s.own_slots + (int)((long long)tokens * group / kChunkRows) + requests + 1;
-    s.space = (long long)tokens * group + (long long)kChunkRows * s.workers;
-    s.slot_bytes = (size_t)s.num_slots * sizeof(Slot);
-    s.part_bytes = (size_t)s.space * 2 * c.kv_heads * s.dim * sizeof(float);
-    s.stat_bytes = (size_t)s.space * 2 * c.kv_heads * sizeof(f32x2);
+    // rows of the shared tiles, of own keys' tiles where a request may have them, of the other line where it may
+    const long long rows = (long long)tokens * group, tiles = rows + (long long)kChunkRows * s.workers;
+    s.few = streams(s.dim) && group <= kFewRows;
+    s.own_place = tiles;
+    s.few_place = s.own_place + (s.few && (long long)max_new * group <= kFewRows ? 0 : tiles);
+    s.space = s.few_place + (s.few ? rows + (long long)kFewRows * kTileWaves * s.workers : 0);
+    s.slot_bytes = (size_t)s.num_slots * (sizeof(Slot) + 3 * sizeof(int));
+    s.slot_bytes = (s.slot_bytes + 15) / 16 * 16;
+    s.part_bytes = (size_t)s.space * c.kv_heads * s.dim * sizeof(float);
+    s.stat_bytes = (size_t)s.space * c.kv_heads * sizeof(f32x2);
     return s;
 }
 
 template <int DT, bool BF>
-void shared_launches(const SharedParams &p, bool any, hipStream_t s)
+void shared_launches(const SharedParams &p, bool any, bool passing, hipStream_t s)
 {
     const AttendParams &a = p.a;
     bcq_attend_shared_line_kernel<DT><<<1, kLineThreads, 0, s>>>(p);
     const unsigned groups = (unsigned)a.workers * a.kv_heads;
-    if (any) bcq_attend_shared_kernel<DT, BF, true><<<groups, 64 * kTileWaves, 0, s>>>(p);
-    else bcq_attend_shared_kernel<DT, BF, false><<<groups, 64 * kTileWaves, 0, s>>>(p);
+    if (any) bcq_attend_shared_kernel<DT, BF, true, false><<<groups, 64 * kTileWaves, 0, s>>>(p);
+    else if (passing && streams(DT)) bcq_attend_shared_kernel<DT, BF, false, streams(DT)><<<groups, 64 * kTileWaves, 0, s>>>(p);
+    else bcq_attend_shared_kernel<DT, BF, false, false><<<groups, 64 * kTileWaves, 0, s>>>(p);
     const long long rows = (long long)a.tokens * a.group;
     constexpr int kRows = kJoinThreads / (DT / 4);
     bcq_attend_shared_join_kernel<DT, BF><<<(unsigned)((rows + kRows - 1) / kRows * a.kv_heads), kJoinThreads, 0, s>>>(p);
 }
 
 template <bool BF>
-void shared_by_dim(const SharedParams &p, int dim, bool any, hipStream_t s)
+void shared_by_dim(const SharedParams &p, int dim, bool any, bool passing, hipStream_t s)
 {
-    if (dim == 64) shared_launches<64, BF>(p, any, s);
-    else if (dim == 128) shared_launches<128, BF>(p, any, s);
-    else shared_launches<256, BF>(p, any, s);
+    if (dim == 64) shared_launches<64, BF>(p, any, passing, s);
+    else if (dim == 128) shared_launches<128, BF>(p, any, passing, s);
+    else shared_launches<256, BF>(p, any, passing, s);
 }
 
 }  // namespace
 
-size_t attend_shared_workspace_bytes(const bcq_cache &c, int tokens, int requests, int groups, int q_heads)
+size_t attend_shared_workspace_bytes(const bcq_cache &c, int tokens, int requests, int groups, int q_heads, int max_new)
 {
-    const SharedPlan s = shared_plan(c, tokens, requests, groups, q_heads);
+    const SharedPlan s = shared_plan(c, tokens, requests, groups, q_heads, max_new);
     return s.part_bytes + s.stat_bytes + s.slot_bytes;
 }
 
@@ -419,13 +761,14 @@ hipError_t launch_attend_shared(const AttendSharedArgs &args, hipStream_t stream
 {
     const AttendArgs &a = args.of;
     const bcq_cache &c = a.cache;
-    const SharedPlan plan = shared_plan(c, a.tokens, a.requests, args.groups, a.q_heads);
+    const SharedPlan plan = shared_plan(c, a.tokens, a.requests, args.groups, a.q_heads, a.max_new);
     char *const ws = static_cast<char *>(a.workspace);
     SharedParams s = {};
     AttendParams &p = s.a;
     p.k = a.k, p.v = a.v, p.q = a.q, p.q_start = a.q_start, p.kv_len = a.kv_len, p.pages = a.pages, p.out = a.out;
     p.part = reinterpret_cast<float *>(ws);
     s.slots = reinterpret_cast<Slot *>(ws + plan.part_bytes);
+    s.sums = reinterpret_cast<int *>(s.slots + plan.num_slots);
     p.stat = reinterpret_cast<f32x2 *>(ws + plan.part_bytes + plan.slot_bytes);
     p.ld_q = a.ld_q, p.ld_out = a.ld_out, p.page_stride = c.page_stride, p.head_stride = c.head_stride, p.slot_stride = (int)c.slot_stride;
     p.tokens = a.tokens, p.requests = a.requests, p.kv_heads = c.kv_heads, p.group = a.q_heads / c.kv_heads;
@@ -435,10 +778,12 @@ hipError_t launch_attend_shared(const AttendSharedArgs &args, hipStream_t stream
     p.scale = (float)(a.scale * 1.4426950408889634);
     p.workers = plan.workers;
     s.group_start = args.group_start, s.shared_len = args.shared_len, s.groups = args.groups, s.max_shared = args.max_shared;
-    s.num_slots = plan.num_slots, s.own_slots = plan.own_slots, s.space = plan.space;
+    s.num_slots = plan.num_slots, s.own_slots = plan.own_slots, s.few = plan.few;
+    s.space = plan.space, s.own_place = plan.own_place, s.few_place = plan.few_place;
     const bool any = c.head_dim != plan.dim || c.page_size < 16;
-    if (c.dtype == BCQ_BF16) shared_by_dim<true>(s, plan.dim, any, stream);
-    else shared_by_dim<false>(s, plan.dim, any, stream);
+    const bool passing = 4 * (long long)c.num_pages * c.page_stride >= kPassingBytes;
+    if (c.dtype == BCQ_BF16) shared_by_dim<true>(s, plan.dim, any, passing, stream);
+    else shared_by_dim<false>(s, plan.dim, any, passing, stream);
     return hipGetLastError();
 }
 

@@ -51,14 +51,14 @@ struct Tile {
 // Sums over the keys of the tile's blocks, relative to `most` (times log2 e), and their weight, this lane's half of it.  Number 4 u + i of o[d] is element 32 d + 8 u + 4 (lane / 32) + i
 // of the lane's row.  All waves of the workgroup together.
 // Returns (all waves the same) whether some may still be reading LDS.
+// k0, k1, v0, v1: LDS, tile_keys(DT) * DT elements each, as objects of their own: the compiler holds reads of one back for the transfers to it alone.
 template <int DT, bool BF, bool ANY, bool PASSING>
-__device__ __forceinline__ bool attend_tile(const AttendParams &p, const Tile &t, f32x16 (&o)[DT / 32], float &most, float &sum)
+__device__ __forceinline__ bool attend_tile(const AttendParams &p, const Tile &t, uint16_t *k0, uint16_t *k1, uint16_t *v0, uint16_t *v1, f32x16 (&o)[DT / 32], float &most,
+                                            float &sum)
 {
     constexpr int KB = tile_keys(DT), KT = KB / 32, C = DT / 16, DV = DT / 32;
     constexpr int kPieces = DT / 8, kRows = 64 / kPieces;       // 16-byte pieces of a key; keys of one transfer of a wave
     constexpr int kTransfers = KB / (kRows * kTileWaves);       // of a wave for a block of K, and for one of V
-    // Two buffers each, as objects of their own: the compiler holds reads of one back for the transfers to it alone.
-    __shared__ __attribute__((aligned(1024))) uint16_t k0[KB * DT], k1[KB * DT], v0[KB * DT], v1[KB * DT];
     __shared__ int votes[kTileWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r32 = lane & 31, h = lane >> 5, from = t.from, to = t.to, b0 = t.b0, b1 = t.b1;

@@ -103,7 +103,7 @@ struct AttendSharedArgs {
     const int *group_start, *shared_len;
     int groups, max_shared;
 };
-size_t attend_shared_workspace_bytes(const bcq_cache &c, int tokens, int requests, int groups, int q_heads);
+size_t attend_shared_workspace_bytes(const bcq_cache &c, int tokens, int requests, int groups, int q_heads, int max_new);
 hipError_t launch_attend_shared(const AttendSharedArgs &a, hipStream_t stream);
 
 struct LoraArgs {

@@ -134,10 +134,11 @@ static bcq_status attend_shared_shape(const bcq_cache *cache, int32_t tokens, in
     return tiles * (max_pages * (int64_t)cache->page_size / 32 + 1) > 0x7fffffffLL ? BCQ_ERR_UNSUPPORTED : BCQ_OK;  // blocks of keys of all tiles are int
 }
 
-size_t bcq_attend_shared_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t groups, int32_t q_heads, int32_t max_pages)
+size_t bcq_attend_shared_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t groups, int32_t q_heads, int32_t max_pages,
+                                         int32_t max_new)
 {
-    if (attend_shared_shape(cache, tokens, requests, groups, q_heads, max_pages) != BCQ_OK || tokens == 0 || requests == 0) return 0;
-    return attend_shared_workspace_bytes(*cache, tokens, requests, groups, q_heads);
+    if (attend_shared_shape(cache, tokens, requests, groups, q_heads, max_pages) != BCQ_OK || max_new < 1 || tokens == 0 || requests == 0) return 0;
+    return attend_shared_workspace_bytes(*cache, tokens, requests, groups, q_heads, max_new);
 }
 
 bcq_status bcq_attend_shared(const bcq_cache *cache, const void *k_cache, const void *v_cache, int32_t tokens, int32_t requests, int32_t groups,

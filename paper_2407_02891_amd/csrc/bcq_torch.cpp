@@ -242,7 +242,7 @@ at::Tensor attend_shared(PyObject *const *a)
     const at::Tensor out = x.result(a[14]);
     const int64_t ld_out = x.place.rows(out, "out", x.T, x.q.size(1));
     const size_t bytes =
-        g_bcq.attend_shared_workspace_bytes(x.cache, (int32_t)x.T, (int32_t)x.R, (int32_t)groups, (int32_t)x.q_heads, (int32_t)x.max_pages);
+        g_bcq.attend_shared_workspace_bytes(x.cache, (int32_t)x.T, (int32_t)x.R, (int32_t)groups, (int32_t)x.q_heads, (int32_t)x.max_pages, x.max_new);
     const at::Tensor workspace = bytes ? x.place.scratch(bytes) : at::Tensor();
     succeeded(g_bcq.attend_shared(x.cache, x.k.data_ptr(), x.v.data_ptr(), (int32_t)x.T, (int32_t)x.R, (int32_t)groups, (int32_t)x.q_heads, x.q.data_ptr(), x.ld,
                                   x.q_start, x.kv_len, static_cast<const int32_t *>(x.pages.data_ptr()), (int32_t)x.max_pages, x.max_new, group_start, shared_len,

@@ -105,5 +105,5 @@ def test_attend_shared_limits():
     assert shared(workspace=None) == shared(workspace=OK + 8) == B.BCQ_ERR_WORKSPACE
     assert shared(tokens=0, q=None) == shared(requests=0, q=None) == B.BCQ_OK     # nothing to do
     cache = B.Cache(0, 8, 128, 16, 100, 16384, 2048, 128)
-    assert bcq.attend_shared_workspace_bytes(cache, 4, 2, 1, 64, 10) > 0
-    assert bcq.attend_shared_workspace_bytes(cache, 0, 2, 1, 64, 10) == bcq.attend_shared_workspace_bytes(cache, 4, 2, -1, 64, 10) == 0
+    assert bcq.attend_shared_workspace_bytes(cache, 4, 2, 1, 64, 10, 2) > 0
+    assert bcq.attend_shared_workspace_bytes(cache, 0, 2, 1, 64, 10, 2) == bcq.attend_shared_workspace_bytes(cache, 4, 2, -1, 64, 10, 2) == 0
