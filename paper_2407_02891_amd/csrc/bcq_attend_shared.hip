@@ -18,6 +18,8 @@ namespace {
 
 constexpr int kLineThreads = 1024;
 constexpr int kJoinThreads = 256;
+constexpr int kLocalSlots = 1024;  // whose sums the first launch has in LDS
+constexpr int kFusedSlots = 128;   // that each workgroup lays out for itself, without a launch before it
 constexpr int kFewRows = 16, kFewKeys = 32;  // of a request whose own keys are streamed; of a block of them
 constexpr bool streams(int dim) { return dim <= 128; }  // (heads of 256: the waves' blocks would be more LDS than two tiles')
 
@@ -97,21 +99,47 @@ __device__ __forceinline__ int slots_before(const SharedParams &p, int v, int st
     return v < p.groups ? at + v : p.own_slots + at + v - p.groups;
 }
 
-// A slot by scalar loads (all lanes the same one, laid out by an earlier launch).
-__device__ __forceinline__ Slot load_slot(const SharedParams &p, int slot)
-{
-    typedef const __attribute__((address_space(4))) int *scalar_int;
-    slot = __builtin_amdgcn_readfirstlane(slot);
-    asm volatile("" : "+s"(slot));
-    const scalar_int from = (scalar_int) reinterpret_cast<const int *>(p.slots + slot);
-    Slot s;
-    s.upto = from[0], s.few_upto = from[1], s.row0 = from[2], s.block = from[3], s.start = from[4], s.rows = from[5], s.request = from[6];
-    s.requests = from[7], s.from = from[8], s.to = from[9], s.n = from[10], s.len = from[11], s.piece = from[12], s.pieces = from[13];
-    s.part = from[14], s.few = from[15];
-    return s;
-}
-
-}  // namespace
+// The slots as a workgroup has them: its own in LDS (FUSED), or those that an earlier launch laid out.
+template <bool FUSED>
+struct SlotList {
+    const Slot *at;
+    int n;
+    // One slot, the same for all lanes.
+    __device__ __forceinline__ Slot load(int slot) const
+    {
+        slot = __builtin_amdgcn_readfirstlane(slot);
+        Slot s;
+        if constexpr (FUSED) {
+            s = at[slot];
+            int *const x = reinterpret_cast<int *>(&s);
+#pragma unroll
+            for (int i = 0; i < (int)(sizeof(Slot) / sizeof(int)); ++i) x[i] = __builtin_amdgcn_readfirstlane(x[i]);
+        } else {  // by scalar loads
+            typedef const __attribute__((address_space(4))) int *scalar_int;
+            asm volatile("" : "+s"(slot));
+            const scalar_int from = (scalar_int) reinterpret_cast<const int *>(at + slot);
+            s.upto = from[0], s.few_upto = from[1], s.row0 = from[2], s.block = from[3], s.start = from[4], s.rows = from[5], s.request = from[6];
+            s.requests = from[7], s.from = from[8], s.to = from[9], s.n = from[10], s.len = from[11], s.piece = from[12], s.pieces = from[13];
+            s.part = from[14], s.few = from[15];
+        }
+        return s;
+    }
+    // That holds block `block` of a line: the first with upto(slot) > block (all lanes).
+    template <class F>
+    __device__ __forceinline__ int that_holds(int block, int lane, F upto) const
+    {
+        int slot = 0;
+        for (int high = n - 1; slot < high;) {
+            const int stride = (high - slot + 63) / 64, probe = slot + lane * stride;
+            const int beyond = __popcll(__ballot(probe < high && upto(at[probe]) <= block));  // (rises, so these are the first lanes)
+            if (!beyond) break;
+            const int last = slot + (beyond - 1) * stride;  // not yet
+            high = min(high, last + stride);
+            slot = last + 1;
+        }
+        return __builtin_amdgcn_readfirstlane(slot);
+    }
+};
 
 // What a slot of a part holds, but for what follows from the sums.
 template <int DT>
@@ -167,49 +195,55 @@ __device__ __forceinline__ void own_blocks(const SharedParams &p, Slot &q)
     (q.few ? q.few_upto : q.upto) = low < high ? (high + keys - 1) / keys - q.block : 0;
 }
 
-// Lays out the lines: the blocks of each part's tiles, their sums, then what the slots hold.  sums: of each slot the two sums and whose it is (bit 31 of a group's: a row of it does
-// not see all keys), in LDS where they are few.
-template <int DT>
-__global__ __launch_bounds__(kLineThreads) void bcq_attend_shared_line_kernel(SharedParams p)
+// Lays out the lines, all of THREADS threads: the blocks of each part's tiles, their sums, then what the slots hold.  upto, few_upto, owner: of each slot the two sums and whose it
+// is (bit 30 of a group's: a row of it does not see all keys).
+template <int DT, int THREADS>
+__device__ __forceinline__ void lay_out(const SharedParams &p, int *upto, int *few_upto, int *owner, Slot *slots)
 {
-    constexpr int kLocal = 3072 / 3;
-    __shared__ int local[3 * kLocal], sums[kLineThreads / 64][2];
+    __shared__ int sums[THREADS / 64][2];
     const AttendParams &a = p.a;
     const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, n = p.num_slots;
-    int *const upto = n <= kLocal ? local : p.sums, *const few_upto = upto + n, *const owner = few_upto + n;
-    for (int s = thread; s < 3 * n; s += kLineThreads) upto[s] = s < 2 * n ? 0 : -1;
+    for (int s = thread; s < n; s += THREADS) upto[s] = few_upto[s] = 0, owner[s] = -1;
     __syncthreads();
-    const auto parts = p.groups + a.requests;
-    for (int v = thread; v < parts; v += kLineThreads) {
-        int slot;
-        Slot q = make_slot<DT>(p, v, 0, slot);
-        const int end_slot = v < p.groups ? p.own_slots : n;
-        q.row0 = 0;
-        for (int s = slot; q.row0 < q.rows && s < end_slot; q.row0 += kChunkRows, ++s) {
-            if (v >= p.groups) own_blocks<DT>(p, q);
-            upto[s] = q.upto, few_upto[s] = q.few_upto, owner[s] = v;
+    // The parts, a thread each; what a thread has looked up of its first one it keeps.
+    const int parts = p.groups + a.requests;
+    int kept_slot = 0;
+    Slot kept = {};
+    if (thread < parts) kept = make_slot<DT>(p, thread, 0, kept_slot);
+    const auto each_part = [&](auto use) {  // use(part's slot as it would be at its first tile, that slot, where the slots of its kind end)
+        for (int v = thread; v < parts; v += THREADS) {
+            int slot = kept_slot;
+            Slot q = kept;
+            if (v != thread) q = make_slot<DT>(p, v, 0, slot);
+            q.row0 = 0;
+            use(q, slot, v < p.groups ? p.own_slots : n);
         }
-    }
+    };
+    each_part([&](Slot q, int s, int end) {
+        for (; q.row0 < q.rows && s < end; q.row0 += kChunkRows, ++s) {
+            if (q.part >= p.groups) own_blocks<DT>(p, q);
+            upto[s] = q.upto, few_upto[s] = q.few_upto, owner[s] = q.part;
+        }
+    });
     __syncthreads();
-    for (int r = thread; r < a.requests; r += kLineThreads) {  // does each of its rows see all that is shared?
-        const Request own = load_request(a, r);
-        const int c = group_of(p, r);
+    each_part([&](const Slot &q, int, int) {  // does each row of a request see all that is shared?
+        if (q.part < p.groups || q.requests < 0 || q.n == 0) return;
         int unused, high;
-        visible_keys(a, own.n, own.len, 0, unused, high);
-        if (c < 0 || own.n == 0 || (high >= shared_keys(p, c) && own.todo == own.n)) continue;
-        const int first = start_of(p, first_of_group(p, c)), rows = max(start_of(p, first_of_group(p, c + 1)) - first, 0) * a.group;
-        const int s = slots_before(p, c, first);
+        visible_keys(a, q.n, q.len, 0, unused, high);
+        if (high >= q.from && q.rows == q.n * a.group) return;
+        const int first = start_of(p, first_of_group(p, q.requests)), rows = max(start_of(p, first_of_group(p, q.requests + 1)) - first, 0) * a.group;
+        const int s = slots_before(p, q.requests, first);
         for (int i = 0; i * kChunkRows < rows && s + i < p.own_slots; ++i) atomicOr(owner + s + i, 1 << 30);
-    }
+    });
     __syncthreads();
     int before = 0, few_before = 0;
-    for (int c = 0; c < n; c += kLineThreads) {
+    for (int c = 0; c < n; c += THREADS) {
         const int s = c + thread;
         const int tiles = prefix_sum(s < n ? upto[s] : 0, lane), few = prefix_sum(s < n ? few_upto[s] : 0, lane);
         if (lane == 63) sums[wave][0] = tiles, sums[wave][1] = few;
         __syncthreads();
         int mine = before + tiles, few_mine = few_before + few;
-        for (int w = 0; w < kLineThreads / 64; ++w) {
+        for (int w = 0; w < THREADS / 64; ++w) {
             if (w < wave) mine += sums[w][0], few_mine += sums[w][1];
             before += sums[w][0], few_before += sums[w][1];
         }
@@ -217,7 +251,7 @@ __global__ __launch_bounds__(kLineThreads) void bcq_attend_shared_line_kernel(Sh
         __syncthreads();
     }
     const Cuts cuts(a.workers / 2, a.workers - a.workers / 2, before, few_before);
-    for (int s = thread; s < n; s += kLineThreads) {
+    for (int s = thread; s < n; s += THREADS) {
         Slot q = {};
         q.part = -1;
         if (owner[s] >= 0) {
@@ -233,35 +267,30 @@ __global__ __launch_bounds__(kLineThreads) void bcq_attend_shared_line_kernel(Sh
             q.piece = cut.piece_of(from);
             q.pieces = cut.piece_of(to - 1) - q.piece + 1;
         }
-        p.slots[s] = q;
+        slots[s] = q;
     }
+    __syncthreads();
+}
+
+}  // namespace
+
+template <int DT>
+__global__ __launch_bounds__(kLineThreads) void bcq_attend_shared_line_kernel(SharedParams p)
+{
+    __shared__ int local[3 * kLocalSlots];
+    int *const sums = p.num_slots <= kLocalSlots ? local : p.sums;
+    lay_out<DT, kLineThreads>(p, sums, sums + p.num_slots, sums + 2 * p.num_slots, p.slots);
 }
 
 namespace {
-
-// The slot that holds block `at` of a line: the first with upto(slot) > at (all lanes).
-template <class F>
-__device__ __forceinline__ int slot_of(const SharedParams &p, int lane, int at, F upto)
-{
-    int slot = 0;
-    for (int high = p.num_slots - 1; slot < high;) {
-        const int stride = (high - slot + 63) / 64, probe = slot + lane * stride;
-        const int beyond = __popcll(__ballot(probe < high && upto(probe) <= at));  // (rises, so these are the first lanes)
-        if (!beyond) break;
-        const int last = slot + (beyond - 1) * stride;  // not yet
-        high = min(high, last + stride);
-        slot = last + 1;
-    }
-    return __builtin_amdgcn_readfirstlane(slot);
-}
 
 template <bool BF>
 using FewWeights = Weights<BF, 1>;
 
 // One wave: blocks [at, stop) of the line of requests with few rows, a piece of it; ks: LDS, 2 * kFewKeys * DT elements of the wave's own.  Column r16 of the products is token r16 / group, query
 // head r16 mod group.  K and V come in whole rows and pass through LDS, the next block's are on their way; weights meet the values as the sum of two 16-bit numbers.
-template <int DT, bool BF, bool ANY, bool PASSING>
-__device__ __forceinline__ void stream_piece(const SharedParams &p, int head, int piece, int at, int stop, uint16_t *const ks)
+template <int DT, bool BF, bool ANY, bool PASSING, bool FUSED>
+__device__ __forceinline__ void stream_piece(const SharedParams &p, const SlotList<FUSED> &slots, int head, int piece, int at, int stop, uint16_t *const ks)
 {
     constexpr int C = DT / 32, DV = DT / 16;                    // matrix steps over head_dim; tiles of O
     constexpr int kRowLanes = DT / 8, kRows = 64 / kRowLanes;   // a load covers kRows keys
@@ -282,12 +311,12 @@ __device__ __forceinline__ void stream_piece(const SharedParams &p, int head, in
         Slot s;
         int key;
     };
-    int slot = slot_of(p, lane, at, [&](int s) { return p.slots[s].few_upto; });
-    int before = slot ? load_slot(p, slot - 1).few_upto : 0;
+    int slot = slots.that_holds(at, lane, [](const Slot &s) { return s.few_upto; });
+    int before = slot ? slots.load(slot - 1).few_upto : 0;
     Place now, next, ahead;
-    ahead.s = load_slot(p, slot);
+    ahead.s = slots.load(slot);
     const auto look_at = [&](int block) {
-        while (block >= ahead.s.few_upto) before = ahead.s.few_upto, ahead.s = load_slot(p, ++slot);
+        while (block >= ahead.s.few_upto) before = ahead.s.few_upto, ahead.s = slots.load(++slot);
         ahead.key = (ahead.s.block + block - before) * kFewKeys;
     };
     look_at(at);
@@ -493,8 +522,8 @@ __device__ __forceinline__ void stream_piece(const SharedParams &p, int head, in
 
 }  // namespace
 
-// The pieces of both lines.  PASSING: what is streamed leaves nothing in the caches.
-template <int DT, bool BF, bool ANY, bool PASSING>
+// The pieces of both lines.  PASSING: what is streamed leaves nothing in the caches.  FUSED: there was no launch before this one.
+template <int DT, bool BF, bool ANY, bool PASSING, bool FUSED>
 __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_attend_shared_kernel(SharedParams p)
 {
     constexpr int KB = tile_keys(DT), DV = DT / 32;
@@ -505,16 +534,25 @@ __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_atten
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int head = blockIdx.x % a.kv_heads, me = blockIdx.x / a.kv_heads, half = a.workers / 2;
     const bool first_half = me < half;
+    SlotList<FUSED> slots{p.slots, p.num_slots};
+    if constexpr (FUSED) {
+        __shared__ Slot own[kFusedSlots];
+        int *const sums = reinterpret_cast<int *>(k0);  // (not in use yet)
+        lay_out<DT, 64 * kTileWaves>(p, sums, sums + p.num_slots, sums + 2 * p.num_slots, own);
+        slots.at = own;
+        if (blockIdx.x == 0)  // for the join
+            for (int i = threadIdx.x; i < p.num_slots; i += 64 * kTileWaves) p.slots[i] = own[i];
+    }
 #pragma unroll 1
     for (int turn = 0; turn < 2; ++turn) {
-        const Slot end_slot = load_slot(p, p.num_slots - 1);  // (again in each turn: not worth registers)
+        const Slot end_slot = slots.load(p.num_slots - 1);  // (again in each turn: not worth registers)
         const Cuts cuts(half, a.workers - half, end_slot.upto, end_slot.few_upto);
         if ((turn == 0) != first_half) {
             if constexpr (streams(DT)) {
                 const int mine = kTileWaves * (first_half ? me : me - half) + wave;
                 if (mine < (first_half ? cuts.few.w1 : cuts.few.w0)) {
                     const int piece = first_half ? cuts.few.w0 + mine : mine, at = cuts.few.begin(piece), stop = cuts.few.end(piece);
-                    if (at < stop) stream_piece<DT, BF, ANY, PASSING>(p, head, piece, at, stop, wave == 0 ? k0 : wave == 1 ? k1 : wave == 2 ? v0 : v1);
+                    if (at < stop) stream_piece<DT, BF, ANY, PASSING, FUSED>(p, slots, head, piece, at, stop, wave == 0 ? k0 : wave == 1 ? k1 : wave == 2 ? v0 : v1);
                 }
                 __syncthreads();  // (the tiles' buffers)
             }
@@ -525,11 +563,11 @@ __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_atten
         int at = __builtin_amdgcn_readfirstlane(cuts.tiles.begin(piece));
         const int stop = __builtin_amdgcn_readfirstlane(cuts.tiles.end(piece));
         if (at >= stop) continue;
-        int slot = slot_of(p, threadIdx.x & 63, at, [&](int s) { return p.slots[s].upto; });
-        int before = slot ? load_slot(p, slot - 1).upto : 0;
+        int slot = slots.that_holds(at, threadIdx.x & 63, [](const Slot &s) { return s.upto; });
+        int before = slot ? slots.load(slot - 1).upto : 0;
 #pragma unroll 1
         for (; at < stop; ++slot) {
-            const Slot s = load_slot(p, slot);
+            const Slot s = slots.load(slot);
             const int end = min(s.upto, stop);
             if (end <= at) {  // (a slot without blocks)
                 before = s.upto;
@@ -727,15 +765,25 @@ SharedPlan shared_plan(const bcq_cache &c, int tokens, int requests, int groups,
     return s;
 }
 
+template <int DT, bool BF, bool FUSED>
+void shared_main(const SharedParams &p, bool any, bool passing, hipStream_t s)
+{
+    const unsigned groups = (unsigned)p.a.workers * p.a.kv_heads;
+    if (any) bcq_attend_shared_kernel<DT, BF, true, false, FUSED><<<groups, 64 * kTileWaves, 0, s>>>(p);
+    else if (passing && streams(DT)) bcq_attend_shared_kernel<DT, BF, false, streams(DT), FUSED><<<groups, 64 * kTileWaves, 0, s>>>(p);
+    else bcq_attend_shared_kernel<DT, BF, false, false, FUSED><<<groups, 64 * kTileWaves, 0, s>>>(p);
+}
+
 template <int DT, bool BF>
 void shared_launches(const SharedParams &p, bool any, bool passing, hipStream_t s)
 {
     const AttendParams &a = p.a;
-    bcq_attend_shared_line_kernel<DT><<<1, kLineThreads, 0, s>>>(p);
-    const unsigned groups = (unsigned)a.workers * a.kv_heads;
-    if (any) bcq_attend_shared_kernel<DT, BF, true, false><<<groups, 64 * kTileWaves, 0, s>>>(p);
-    else if (passing && streams(DT)) bcq_attend_shared_kernel<DT, BF, false, streams(DT)><<<groups, 64 * kTileWaves, 0, s>>>(p);
-    else bcq_attend_shared_kernel<DT, BF, false, false><<<groups, 64 * kTileWaves, 0, s>>>(p);
+    if (p.num_slots <= kFusedSlots) {
+        shared_main<DT, BF, true>(p, any, passing, s);
+    } else {
+        bcq_attend_shared_line_kernel<DT><<<1, kLineThreads, 0, s>>>(p);
+        shared_main<DT, BF, false>(p, any, passing, s);
+    }
     const long long rows = (long long)a.tokens * a.group;
     constexpr int kRows = kJoinThreads / (DT / 4);
     bcq_attend_shared_join_kernel<DT, BF><<<(unsigned)((rows + kRows - 1) / kRows * a.kv_heads), kJoinThreads, 0, s>>>(p);
