@@ -664,15 +664,18 @@ __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_atten
     }
 }
 
-// Joins what was left of a row, its shared keys' pieces and its own: four elements to a thread.
-template <int DT, bool BF>
+// Joins what was left of a row, its shared keys' pieces and its own: four elements to a thread, SHARE threads to share the pieces of them.
+template <int DT, bool BF, int SHARE>
 __global__ __launch_bounds__(kJoinThreads) void bcq_attend_shared_join_kernel(SharedParams p)
 {
-    constexpr int kLanes = DT / 4, kAhead = 8;
+    constexpr int kLanes = DT / 4, kAhead = SHARE > 1 ? 4 : 8, kOwn = kJoinThreads / SHARE;
+    __shared__ f32x4 shared_y[SHARE > 1 ? kJoinThreads : 1];
+    __shared__ f32x2 shared_stat[SHARE > 1 ? kJoinThreads : 1];
     const AttendParams &a = p.a;
-    const int head = blockIdx.x % a.kv_heads, row = blockIdx.x / a.kv_heads * (kJoinThreads / kLanes) + (int)threadIdx.x / kLanes, d = 4 * (threadIdx.x % kLanes);
+    const int share = threadIdx.x / kOwn, thread = threadIdx.x % kOwn;
+    const int head = blockIdx.x % a.kv_heads, row = min(blockIdx.x / a.kv_heads * (kOwn / kLanes) + thread / kLanes, a.tokens * a.group - 1), d = 4 * (thread % kLanes);
+    const bool twice = blockIdx.x / a.kv_heads * (kOwn / kLanes) + thread / kLanes >= a.tokens * a.group;  // (the last row again)
     const int token = row / a.group, member = row - token * a.group;
-    if (token >= a.tokens || d >= a.head_dim) return;
     // the request of the token: where each has one, as many behind the first
     int r = min(token, a.requests - 1);
     if (a.q_start[r] > token || a.q_start[r + 1] <= token) {
@@ -685,8 +688,8 @@ __global__ __launch_bounds__(kJoinThreads) void bcq_attend_shared_join_kernel(Sh
     }
     const Request own = load_request(a, r);
     const int i = token - own.start;
-    if (i < 0 || i >= own.todo) return;
-    const int s1 = slots_before(p, p.groups + r, own.start) + (i * a.group + member) / kChunkRows;
+    const bool real = !twice && i >= 0 && i < own.todo && d < a.head_dim;
+    const int s1 = slots_before(p, p.groups + r, own.start) + max(i * a.group + member, 0) / kChunkRows;
     const Slot &mine = p.slots[min(s1, p.num_slots - 1)];
     const int c = mine.requests;
     int pieces0 = 0, pieces = mine.pieces;
@@ -698,16 +701,16 @@ __global__ __launch_bounds__(kJoinThreads) void bcq_attend_shared_join_kernel(Sh
         pieces0 = shared.pieces;
         place0 = head * p.space + (long long)token * a.group + member + (long long)kChunkRows * shared.piece;
     }
-    pieces += pieces0;
+    pieces = real ? pieces + pieces0 : 0;
     const auto at = [&](int n) { return n < pieces0 ? place0 + (long long)n * kChunkRows : place1 + (long long)(n - pieces0) * step1; };
     f32x4 y = {0.0f, 0.0f, 0.0f, 0.0f};
     float most = -INFINITY, weight = 0.0f;
-    for (int n = 0; n < pieces; n += kAhead) {
+    for (int n = share; n < pieces; n += kAhead * SHARE) {
         f32x4 part[kAhead];
         f32x2 stat[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const long long place = at(min(n + k, pieces - 1));
+            const long long place = at(min(n + k * SHARE, pieces - 1));
             stat[k] = a.stat[place];
             part[k] = *reinterpret_cast<const f32x4 *>(a.part + place * DT + d);
         }
@@ -720,13 +723,32 @@ __global__ __launch_bounds__(kJoinThreads) void bcq_attend_shared_join_kernel(Sh
         most = high;
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (n + k < pieces) {
+            if (n + k * SHARE < pieces) {
                 const float scale = shrink_by(stat[k].x - base);
                 weight = fmaf(stat[k].y, scale, weight);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y[e] = fmaf(part[k][e], scale, y[e]);
             }
     }
+    if constexpr (SHARE > 1) {
+        shared_y[threadIdx.x] = y;
+        shared_stat[threadIdx.x] = f32x2{most, weight};
+        __syncthreads();
+        if (share) return;
+#pragma unroll
+        for (int k = 1; k < SHARE; ++k) most = fmaxf(most, shared_stat[k * kOwn + thread].x);
+        const float base = most == -INFINITY ? 0.0f : most;
+        y = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        weight = 0.0f;
+#pragma unroll
+        for (int k = 0; k < SHARE; ++k) {
+            const f32x2 stat = shared_stat[k * kOwn + thread];
+            const float scale = shrink_by(stat.x - base);
+            weight = fmaf(stat.y, scale, weight);
+            y += shared_y[k * kOwn + thread] * scale;
+        }
+    }
+    if (!real) return;
     int from, to;
     visible_keys(a, own.n, own.len, i, from, to);
     const float unit = 1.0f / weight;
@@ -786,7 +808,12 @@ void shared_launches(const SharedParams &p, bool any, bool passing, hipStream_t 
     }
     const long long rows = (long long)a.tokens * a.group;
     constexpr int kRows = kJoinThreads / (DT / 4);
-    bcq_attend_shared_join_kernel<DT, BF><<<(unsigned)((rows + kRows - 1) / kRows * a.kv_heads), kJoinThreads, 0, s>>>(p);
+    // (with fewer rows than the chip has room for threads, latency counts: calls of 4 requests 17.0 us with one
+    // thread to a row's four elements, 15.0 with four; of 5 with drafts 41.8 and 38.1)
+    if (rows * a.kv_heads < (long long)kRows * 8 * compute_units())
+        bcq_attend_shared_join_kernel<DT, BF, 4><<<(unsigned)((4 * rows + kRows - 1) / kRows * a.kv_heads), kJoinThreads, 0, s>>>(p);
+    else
+        bcq_attend_shared_join_kernel<DT, BF, 1><<<(unsigned)((rows + kRows - 1) / kRows * a.kv_heads), kJoinThreads, 0, s>>>(p);
 }
 
 template <bool BF>
