@@ -96,7 +96,7 @@ __device__ __forceinline__ void fill_row(const PlanArgs &p, int t, int r, int st
 
 }  // namespace
 
-// FEW: at most 1024 requests, and so few rows of the batch that they are filled here too.
+// FEW: at most 1024 requests, a thread keeps its own; then so few rows of the batch as kOneLaunch are filled here too.
 template <bool FEW>
 __global__ __launch_bounds__(kThreads) void bcq_plan_kernel(PlanArgs p)
 {
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void bcq_plan_kernel(PlanArgs p)
     if (thread == 0) *p.free_count_out = there - taken;
 
     // ---- rows of the batch ----
-    if (FEW) {
+    if (FEW && p.tokens <= kOneLaunch) {
         const int all = requests ? starts[requests - 1] : 0;
         for (int t = thread; t < p.tokens; t += kThreads) {
             const int r = t < all ? first_beyond(starts, requests, t) : 0;
@@ -197,10 +197,10 @@ __global__ __launch_bounds__(kFillThreads) void bcq_plan_fill_kernel(PlanArgs p)
 
 hipError_t launch_plan(const PlanArgs &p, hipStream_t stream)
 {
-    if (p.tokens <= kOneLaunch && p.requests <= kThreads) {
-        bcq_plan_kernel<true><<<1, kThreads, 0, stream>>>(p);
-    } else {
-        bcq_plan_kernel<false><<<1, kThreads, 0, stream>>>(p);
+    const bool few = p.requests <= kThreads;
+    if (few) bcq_plan_kernel<true><<<1, kThreads, 0, stream>>>(p);
+    else bcq_plan_kernel<false><<<1, kThreads, 0, stream>>>(p);
+    if (!few || p.tokens > kOneLaunch) {
         bcq_plan_fill_kernel<<<(p.tokens + kFillThreads - 1) / kFillThreads, kFillThreads, 0, stream>>>(p);
     }
     return hipGetLastError();
