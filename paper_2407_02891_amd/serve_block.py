@@ -2,10 +2,12 @@
 coding, each request's low-rank adapter beside it, norm and rotation of q and k with the append to a paged cache, attention over the
 pages, and the output projection with its adapter.  Everything runs in the library's kernels on torch's current stream; `step` allocates
 from torch alone, so a step of single tokens can be captured in a graph and replayed while `positions`, `slots` and `kv_len` are advanced
-in place.
+in place.  `Decoder` puts it between an embedding and a head, hands pages out as requests grow, reads a prompt that they share once and draws
+their tokens, all on the device.
 
-Run as a module for timings with random weights (prompts as one chunk, then single tokens, eagerly and as a replayed graph):
-    python -m paper_2407_02891_amd.serve_block --requests 16 --prompt 100 --tokens 16
+Run as a module for timings with random weights (prompts as one chunk, then single tokens, eagerly and as a replayed graph; with --shared, then
+drawn tokens of requests that begin with a prompt of so many):
+    python -m paper_2407_02891_amd.serve_block --requests 16 --prompt 100 --tokens 16 --shared 1000
 """
 import argparse
 import json
@@ -14,7 +16,7 @@ import time
 import torch
 
 from . import binding as B
-from .serving import Adapters, PagedCache
+from .serving import Adapters, PagedCache, PageTable, Sampler
 
 
 def product(layer, X):
@@ -76,18 +78,93 @@ class AttentionBlock:
         self.qkv, self.o, self.q_heads, self.cache, self.cos_sin, self.eps = qkv, o, q_heads, cache, cos_sin, eps
         self.q_weight, self.k_weight, self.qkv_adapters, self.o_adapters = q_weight, k_weight, qkv_adapters, o_adapters
 
-    def step(self, X, positions, slots, adapter, kv_len, q_start, pages, max_new):
-        """X [tokens][hidden] binary16 -> [tokens][hidden]; the tokens' keys and values are in the cache afterwards."""
+    def step(self, X, positions, slots, adapter, kv_len, q_start, pages, max_new, shared=None):
+        """X [tokens][hidden] binary16 -> [tokens][hidden]; the tokens' keys and values are in the cache afterwards.  shared: (group_start, shared_len,
+        max_shared) of PagedCache.attend_shared, or None."""
         y = product(self.qkv, X)
         if self.qkv_adapters is not None:
             self.qkv_adapters.add(X, adapter, y, out=y)
         q = self.cache.rotate(y, positions, self.cos_sin, slots, self.q_weight, self.k_weight, eps=self.eps,
                               out=y[:, : self.q_heads * self.cache.head_dim])
-        a = self.cache.attend(q, q_start, kv_len, pages, max_new)
+        if shared is None:
+            a = self.cache.attend(q, q_start, kv_len, pages, max_new)
+        else:
+            a = self.cache.attend_shared(q, q_start, kv_len, pages, max_new, *shared)
         z = product(self.o, a)
         if self.o_adapters is not None:
             self.o_adapters.add(a, adapter, z, out=z)
         return z
+
+
+class Decoder:
+    """Requests that begin with one prompt and go on by themselves, a drawn token at a time.  The prompt's whole pages stand in every request's row of
+    the table and are attended to as shared keys; the pages behind them are taken as the requests grow and given back by those that `leave`."""
+
+    def __init__(self, block, embedding, head, table, sampler, adapter):
+        """block: AttentionBlock; embedding [vocabulary][hidden] binary16; head: PackedLayer of vocabulary by hidden; table: PageTable with nothing held,
+        over the block's cache; sampler: Sampler, a row per request; adapter: of all requests (keys
+        that are shared depend on it), any number outside the adapters': none."""
+        self.block, self.embedding, self.head, self.table, self.sampler, self.adapter = block, embedding, head, table, sampler, adapter
+        self.count = table.pages.shape[0]
+        self.cached, self.fresh, self.fixed, self.token = (torch.zeros(self.count, dtype=torch.int32, device=table.device) for _ in range(4))
+        self.probability = torch.zeros(self.count, device=table.device)
+        self.shared, self.plan = None, None
+
+    def _pass(self, ids, plan, max_new):
+        """ids of the batch's rows -> the rows that come out of the block."""
+        adapter = torch.full_like(plan["owner"], self.adapter)
+        return self.block.step(self.embedding[ids], plan["positions"], plan["slots"], adapter, plan["kv_len"], plan["q_start"], self.table.pages, max_new,
+                               self.shared)
+
+    def _next(self, z, plan, uniform):
+        """Each request's next token from its last row, where it had one and the pages for it; else its token stays, and the step can be made again."""
+        last = (plan["q_start"][1:] - 1).clamp(min=0).long()
+        token, probability = self.sampler.draw(product(self.head, z[last]), uniform)
+        ready = (plan["lack"] == 0) & (self.fresh > 0) & (token >= 0)
+        self.token.copy_(torch.where(ready, token, self.token))
+        self.probability.copy_(torch.where(ready, probability, self.probability))
+        self.cached.add_(torch.where(plan["lack"] == 0, self.fresh, 0))
+
+    def _take(self, counts):
+        """The plan of a batch of so many tokens of each request."""
+        self.fresh.copy_(torch.tensor(counts, dtype=torch.int32))
+        return self.table.step(self.cached, self.fresh, sum(counts), self.fixed)
+
+    def prompt(self, shared, own, uniform):
+        """The ids that all requests begin with, the ids (at least one) that follow in each, and the numbers that their first tokens are drawn with."""
+        page, device, where = self.table.page_size, self.table.device, "Decoder.prompt"
+        whole = len(shared) // page * page
+        rest = [shared[whole:] + ids for ids in own]
+        pages = [-(-len(ids) // page) for ids in rest]
+        if len(own) != self.count or not all(own):
+            raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"{where} (one id or more of each of the {self.count} requests)")
+        if bool((self.cached + self.table.held).any()):
+            raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"{where} (requests that have begun)")
+        if whole // page + max(pages) > self.table.pages.shape[1] or whole // page + sum(pages) > int(self.table.free_count):
+            raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"{where} ({whole // page} pages of the shared ids and {pages} of the requests' own do not fit)")
+        if whole:
+            plan = self._take([whole] + [0] * (self.count - 1))
+            self._pass(torch.tensor(shared[:whole], device=device), plan, whole)
+            n = whole // page
+            self.table.pages[1:, :n] = self.table.pages[0, :n]
+            self.table.held.fill_(n)
+            self.fixed.fill_(n)
+            self.cached.fill_(whole)
+            self.shared = (torch.tensor([0, self.count], dtype=torch.int32, device=device), torch.full((1,), whole, dtype=torch.int32, device=device), whole)
+        plan = self._take([len(ids) for ids in rest])
+        self._next(self._pass(torch.tensor(sum(rest, []), device=device), plan, max(map(len, rest))), plan, uniform)
+        self.fresh.fill_(1)
+
+    def step(self, uniform):
+        """The keys of each request's token into the cache, and the token after it into `token`: nothing waits for the device, and a captured step can be
+        replayed (with other numbers in `uniform`)."""
+        plan = self.plan = self.table.step(self.cached, self.fresh, self.count, self.fixed, out=self.plan)
+        self._next(self._pass(self.token[plan["owner"].clamp(min=0).long()].long(), plan, 1), plan, uniform)
+
+    def leave(self, request):
+        """The request is over: its own pages go back with the next step."""
+        self.cached[request] = 0
+        self.fresh[request] = 0
 
 
 def random_block(hidden, q_heads, kv_heads, head_dim, planes, pages, page_size, longest, adapters, rank, seed=0):
@@ -117,7 +194,7 @@ def random_block(hidden, q_heads, kv_heads, head_dim, planes, pages, page_size, 
 def main():
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, value in (("hidden", 8192), ("q-heads", 64), ("kv-heads", 8), ("head-dim", 128), ("planes", 3), ("requests", 16), ("prompt", 100),
-                        ("tokens", 16), ("page", 16), ("adapters", 4), ("rank", 16)):
+                        ("tokens", 16), ("page", 16), ("adapters", 4), ("rank", 16), ("shared", 0), ("vocabulary", 32000)):
         ap.add_argument("--" + name, type=int, default=value)
     a = ap.parse_args()
     longest = a.prompt + a.requests + 2 * a.tokens + 2
@@ -159,6 +236,51 @@ def main():
     print(json.dumps({"what": "attention half of a block", "hidden": a.hidden, "requests": a.requests, "prompt_tokens": X.shape[0],
                       "prompt_ms": round(prompt_ms, 3), "token_eager_ms": round(eager_ms / a.tokens, 4), "token_graph_ms": round(graph_ms / a.tokens, 4),
                       "keys_at_end": max(requests.length)}))
+    if a.shared:
+        answers(a)
+
+
+def random_head(hidden, vocabulary, planes, seed=0):
+    """An embedding and a head of that size with random weights: (embedding, PackedLayer, (codes, alpha)); logits of rows of size one have size four."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(0, 1 << planes, (vocabulary, hidden), device="cuda", generator=g, dtype=torch.uint8)
+    step = 2.0 ** -torch.arange(planes, device="cuda")
+    alpha = (4 * (0.5 + torch.rand((vocabulary, hidden // 128, planes), device="cuda", generator=g)) * step * hidden ** -0.5).half()
+    head = B.PackedLayer(vocabulary, hidden, planes, 128, False, max_batch=B.BCQ_MAX_BATCH).pack_from(codes, alpha, None)
+    return torch.randn((vocabulary, hidden), device="cuda", generator=g).half(), head, (codes, alpha)
+
+
+def answers(a):
+    longest = a.shared + a.prompt + a.requests + 2 * a.tokens + a.page
+    width = -(-longest // a.page)
+    own = a.requests * (-(-(longest - a.shared) // a.page) + 1)
+    block, _ = random_block(a.hidden, a.q_heads, a.kv_heads, a.head_dim, a.planes, width + own, a.page, longest, a.adapters, a.rank)
+    embedding, head, _ = random_head(a.hidden, a.vocabulary, a.planes)
+    table = PageTable.empty(a.requests, width, width + own, a.page)
+    sampler = Sampler(torch.full((a.requests,), 0.8, device="cuda"), torch.full((a.requests,), 50, dtype=torch.int32, device="cuda"),
+                      torch.full((a.requests,), 0.95, device="cuda"))
+    decoder = Decoder(block, embedding, head, table, sampler, adapter=0)
+    ids = torch.randint(0, a.vocabulary, (longest,)).tolist()
+    uniform = torch.rand(a.requests, device="cuda")
+    decoder.prompt(ids[:a.shared], [ids[: a.prompt + r] for r in range(a.requests)], uniform)
+
+    def timed(f):
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(a.tokens):
+            uniform.uniform_()
+            f()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) * 1e3 / a.tokens
+
+    decoder.step(uniform)
+    eager_ms = timed(lambda: decoder.step(uniform))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        decoder.step(uniform)
+    graph_ms = timed(graph.replay)
+    print(json.dumps({"what": "answers that begin alike, block and head", "hidden": a.hidden, "vocabulary": a.vocabulary, "requests": a.requests, "shared": a.shared,
+                      "token_eager_ms": round(eager_ms, 4), "token_graph_ms": round(graph_ms, 4), "keys_at_end": int(decoder.cached.max())}))
 
 
 if __name__ == "__main__":
