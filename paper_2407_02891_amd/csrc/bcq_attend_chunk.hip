@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * kWaves, tile_occupancy(DT)) void bcq_attend_ch
     const auto twin = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, sum), __builtin_bit_cast(unsigned, sum), false, false);
     sum = __builtin_bit_cast(float, (unsigned)twin[0]) + __builtin_bit_cast(float, (unsigned)twin[1]);
     if (!real) return;
-    if (p.parts == 1) {
+    if (gridDim.y == 1) {  // (p.parts, which would have to be kept in a lane for this)
         const float unit = 1.0f / sum;
         const bool empty = to <= from;
         uint16_t *const dst = p.out + (long long)(q.start + token) * p.ld_out + (head * p.group + member) * p.head_dim;

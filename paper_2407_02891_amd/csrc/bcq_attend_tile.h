@@ -61,7 +61,7 @@ __device__ __forceinline__ bool attend_tile(const AttendParams &p, const Tile &t
     constexpr int kTransfers = KB / (kRows * kTileWaves);       // of a wave for a block of K, and for one of V
     __shared__ int votes[kTileWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r32 = lane & 31, h = lane >> 5, from = t.from, to = t.to, b0 = t.b0, b1 = t.b1;
+    const int r32 = lane & 31, h = lane >> 5, from = t.from, to = t.to, b0 = t.b0, b1 = t.b1, any_to = t.has_rows ? t.any_to : 0;
 
     // ---- K and V of a block to LDS ----
     // A wave brings KB / 4 neighbouring keys, which lie in one page of 16 slots or more.
@@ -131,7 +131,7 @@ __device__ __forceinline__ bool attend_tile(const AttendParams &p, const Tile &t
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (more) request(key0 + KB, next_k, next_v);  // (every wave is through with the other buffers)
-        const bool work = t.has_rows && key0 < t.any_to && key0 + KB > t.any_from;
+        const bool work = key0 < any_to && key0 + KB > t.any_from;
         if (DT == 256) {  // Q stays where the matrix instructions can read it and nothing else needs the place
 #pragma unroll
             for (int c = 0; c < C; ++c) asm volatile("" : "+a"(qr[c]));
