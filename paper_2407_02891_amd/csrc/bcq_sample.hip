@@ -5,8 +5,8 @@
 //
 // Logits of 16 bits have 65536 values, so a row is what its values' counts are: no token is sorted, and a weight is computed once for a value, in binary64,
 // as the borders (u M in a sum of 131072 weights) ask for.  Counts are exact in any order.
-//  * A workgroup has a row.  It counts the row's values in LDS: a word for each magnitude, the positive value's entries in its low half, the negative one's in its high half.  Counts that
-//    could pass 16 bits are moved to a list between chunks of 32768 entries.
+//  * A workgroup has a row.  It counts the row's values in LDS: a word for each magnitude, the positive value's entries in its low half, the negative one's in its high half.  Where
+//    counters pass 16 bits, they are moved to a list between chunks of 32768 entries.
 //  * The weight and number of each unit of 512 values, in descending order, by all waves; then, in one wave, the borders one after the other: which unit, which eight values, which value,
 //    how many of its entries.
 //  * The entry: the row is read again (from L2) and the drawn value's entries counted, in the order of the index.
@@ -147,6 +147,9 @@ __device__ __forceinline__ u64 least_of_all(u64 v)
     return v;
 }
 
+// Entries from the 16 bytes that a row's first one lies in to that.
+__device__ __forceinline__ int in_front(const uint16_t *row) { return (int)(reinterpret_cast<uintptr_t>(row) >> 1 & 7); }
+
 // The entries of a chunk of a row in pieces of eight that begin at 16 bytes, thread t's the pieces t, t + kThreads, ..; what is outside of the row is a
 // negative NaN.
 struct Chunk {
@@ -157,7 +160,7 @@ struct Chunk {
     // Chunk c of the row; its first one begins in front of the row if that does not begin at 16 bytes.
     __device__ __forceinline__ void load(const uint16_t *row, int c, int vocab)
     {
-        first = c * kChunk - (int)(reinterpret_cast<uintptr_t>(row) >> 1 & 7);
+        first = c * kChunk - in_front(row);
 #pragma unroll
         for (int j = 0; j < kPieces; ++j) {
             x[j] = u32x4{0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
@@ -172,7 +175,7 @@ struct Chunk {
         }
     }
 };
-__device__ __forceinline__ int chunks_of(const uint16_t *row, int vocab) { return (int)((vocab + (reinterpret_cast<uintptr_t>(row) >> 1 & 7) + kChunk - 1) / kChunk); }
+__device__ __forceinline__ int chunks_of(const uint16_t *row, int vocab) { return (vocab + in_front(row) + kChunk - 1) / kChunk; }
 
 // A row's chunks, which stay in registers where they are at most KEPT (not 0).
 template <int KEPT>
@@ -199,9 +202,11 @@ struct Row {
             in_turn(use, std::make_integer_sequence<int, KEPT>());
         } else {
             Chunk next;
-            next.load(row, 0, vocab);
+            int c = 0;
+            asm volatile("" : "+s"(c));  // (the masks of its edges are not held where a row is counted again)
+            next.load(row, c, vocab);
 #pragma unroll 1
-            for (int c = 0; c < chunks; ++c) {
+            for (; c < chunks; ++c) {
                 const Chunk now = next;
                 if (c + 1 < chunks) next.load(row, c + 1, vocab);
                 if (use(now, c + 1 < chunks)) return;
@@ -268,6 +273,7 @@ struct Shared {
     int found[kPieces * kWaves];
     uint32_t big[kMostBig];  // places of kBig entries each that are not in the table
     int num_big;
+    int passed;              // entries that were met and are not in the table
     uint32_t place;          // of the drawn value
     int nth;                 // which of its entries
 };
@@ -309,15 +315,16 @@ __device__ __forceinline__ u64 first_of_largest(const Row<KEPT> &row, Shared &sh
     return best;
 }
 
-// How often each value occurs: the counters of magnitude m are in word m.
+// How often each value occurs: the counters of magnitude m are in word m.  careful (of rows of more than a chunk): none passes 16 bits.
 template <bool BF, int KEPT>
-__device__ __forceinline__ void count_values(const Row<KEPT> &row, uint32_t *table, Shared &sh)
+__device__ __forceinline__ void count_values(const Row<KEPT> &row, uint32_t *table, Shared &sh, bool careful)
 {
     const int lane = threadIdx.x & 63;
+    int passed = 0;
     const u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 32768 / 4 / kThreads; ++i) reinterpret_cast<u32x4 *>(table)[i * kThreads + threadIdx.x] = zero;
-    if (threadIdx.x == 0) sh.num_big = 0;
+    if (threadIdx.x == 0) sh.num_big = sh.passed = 0;
     __syncthreads();
     row.each([&](const Chunk &now, bool more) {
 #pragma unroll
@@ -333,7 +340,10 @@ __device__ __forceinline__ void count_values(const Row<KEPT> &row, uint32_t *tab
             const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)x[0]);
             if (__ballot(x[0] == w) == ~0ull && w >> 16 == (w & 0xffffu) && __ballot(x[1] == w && x[2] == w && x[3] == w) == ~0ull) {
                 // entries that are all alike, a mask's: one by one they would take 64 turns each
-                if ((w & 0xffffu) < kEnd<BF> && lane == 0) atomicAdd(table + (w & 0x7fffu), 512u << (w >> 31 << 4));
+                if (lane == 0) {
+                    if ((w & 0xffffu) < kEnd<BF>) atomicAdd(table + (w & 0x7fffu), 512u << (w >> 31 << 4));
+                    else passed += 512;
+                }
             } else if (__ballot(max((uint32_t)high.x, (uint32_t)high.y) >= kEnd<BF>)) {
                 // -infinities, another mask, would all meet at one counter
 #pragma unroll
@@ -342,6 +352,7 @@ __device__ __forceinline__ void count_values(const Row<KEPT> &row, uint32_t *tab
                     for (int e = 0; e < 2; ++e) {
                         const uint32_t bits = e ? x[i] >> 16 : x[i] & 0xffffu;
                         if (bits < kEnd<BF>) atomicAdd(table + (bits & 0x7fffu), bits >> 15 ? 0x10000u : 1u);
+                        else ++passed;
                     }
             } else {
                 // (three vector instructions an entry: the low and the high half's address and what is added)
@@ -359,8 +370,8 @@ __device__ __forceinline__ void count_values(const Row<KEPT> &row, uint32_t *tab
                 }
             }
         }
-        __syncthreads();
-        if (more) {  // what the next chunk could bring beyond 16 bits
+        if (!KEPT && careful && more) {  // what the next chunk could bring beyond 16 bits
+            __syncthreads();
             for (int i = threadIdx.x; i < 32768 / 4; i += kThreads) {
                 u32x4 x = reinterpret_cast<u32x4 *>(table)[i];
                 if (!((x[0] | x[1] | x[2] | x[3]) & 0x80008000u)) continue;
@@ -377,9 +388,18 @@ __device__ __forceinline__ void count_values(const Row<KEPT> &row, uint32_t *tab
         }
         return false;
     });
+    __syncthreads();
     // NaN go, -0 are zeros
     static_assert(0x7fff - kInfinity<BF> <= kThreads, "");
-    if (threadIdx.x < 0x7fff - kInfinity<BF>) table[kInfinity<BF> + 1 + threadIdx.x] = 0;
+    if (threadIdx.x < 0x7fff - kInfinity<BF>) {
+        const uint32_t nan = table[kInfinity<BF> + 1 + threadIdx.x];
+        table[kInfinity<BF> + 1 + threadIdx.x] = 0;
+        passed += (nan & 0xffffu) + (nan >> 16);
+    }
+    if (!KEPT) {
+        passed = sum_all(passed);
+        if (lane == 0) atomicAdd(&sh.passed, passed);
+    }
     if (threadIdx.x == 0) {
         for (int i = 0; i < sh.num_big; ++i)
             if (sh.big[i] < kFirst<BF>) sh.big[i] = 0xffffffffu;
@@ -430,12 +450,10 @@ struct Counts {
     }
 };
 
-// The draw of a row: the value, and which of its entries, in sh.  False if there is nothing to draw from.
-template <bool BF>
-__device__ __forceinline__ bool draw(const SampleParams &p, int row, const Counts &c, Shared &sh)
+// The number of each unit's entries.
+__device__ __forceinline__ void count_units(const Counts &c, Shared &sh)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // ---- number of each unit's entries, then the largest value, then their weight as far as a border needs it ----
     for (int b = wave; b < kUnits / 2; b += kWaves) {
         int low, high;
         c.block(b, lane, low, high);
@@ -445,6 +463,14 @@ __device__ __forceinline__ bool draw(const SampleParams &p, int row, const Count
     __syncthreads();
     if ((int)threadIdx.x < c.num_big && sh.big[threadIdx.x] < 0x10000u) atomicAdd(sh.entries + sh.big[threadIdx.x] / kUnit, kBig);
     if (c.num_big) __syncthreads();
+}
+
+// The draw of a row: the value, and which of its entries, in sh.  False if there is nothing to draw from.
+template <bool BF>
+__device__ __forceinline__ bool draw(const SampleParams &p, int row, const Counts &c, Shared &sh)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // ---- the largest value, then the units' weight as far as a border needs it ----
     const int e0 = sh.entries[2 * lane], e1 = sh.entries[2 * lane + 1];
     const int entries_upto = sum_upto(e0 + e1, lane), n0 = entries_upto - (e0 + e1);
     const int all = from_lane(entries_upto, 63), top_k = p.top_k ? p.top_k[row] : 0;
@@ -627,7 +653,17 @@ __global__ __launch_bounds__(kThreads) void bcq_sample_kernel(SampleParams p)
         if (threadIdx.x == 0) write_token(p, row, best == ~0ull ? -1 : (int)(uint32_t)best, best == ~0ull ? 0.0f : 1.0f);
         return;
     }
-    count_values<BF>(logits, table, sh);
+    // A counter that passes 16 bits loses 65535 or 65536 entries each time, so the sum of all tells whether any did.  Then (half of the first 131072 entries alike, say) they are counted again,
+    // with a look at every counter between chunks.  (64 rows of 131072: 26.9 us, with that look in the first place 29.6.)
+    const int lane = threadIdx.x & 63, met = (p.vocab + in_front(logits.row) + 8 * kThreads - 1) / (8 * kThreads) * (8 * kThreads);
+    bool careful = KEPT > 0;
+#pragma unroll 1
+    for (;; careful = true) {
+        count_values<BF>(logits, table, sh, careful);
+        count_units(Counts{table, sh, __builtin_amdgcn_readfirstlane(sh.num_big)}, sh);
+        if (careful || sum_all(sh.entries[2 * lane] + sh.entries[2 * lane + 1]) + sh.passed == met) break;
+        __syncthreads();
+    }
     if (draw<BF>(p, row, Counts{table, sh, __builtin_amdgcn_readfirstlane(sh.num_big)}, sh)) find_entry(p, row, logits, sh);
 }
 

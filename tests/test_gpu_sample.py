@@ -122,6 +122,21 @@ def test_masked_logits(vocab, dtype):
     assert token[[6, 7, 12]].tolist() == [-1] * 3 and token[10] == 3
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("counts", [{1.5: 65535}, {1.5: 65536}, {1.5: 65537}, {-1.5: 65536}, {1.5: 65536, -1.5: 65536}, {1.5: 131072, -1.5: 70000}, {0.0: 65536, -0.0: 65536},
+                                    {float("nan"): 65536, 2.0: 10}, {-float("inf"): 140000, 0.5: 66000}, {-3.0: 196608}], ids=str)
+def test_values_that_fill_a_long_row(counts, dtype):
+    # not side by side: in front, behind and shuffled with others, what a counter of 16 bits holds and more
+    g = torch.Generator().manual_seed(11)
+    filling = torch.cat([torch.full((n,), v) for v, n in counts.items()])
+    others = torch.randn(20000, generator=g)
+    every = torch.cat([filling, others])
+    x = torch.stack([every, every.flip(0), every[torch.randperm(every.shape[0], generator=g)], every[torch.randperm(every.shape[0], generator=g)]]).to(dtype)
+    u = torch.rand(4, generator=g)
+    _check(x, torch.tensor([1.0, 0.7, 2.0, 1.0]), None, None, None, u, what=counts)
+    _check(x, torch.tensor([1.0, 0.7, 2.0, 50.0]), torch.tensor([1000, 65536, 70000, 65540], dtype=torch.int32), torch.tensor([1.0, 0.9, 0.5, 0.99]), None, u, what=counts)
+
+
 @pytest.mark.parametrize("vocab", [100, 70000])
 def test_odd_settings(vocab):
     """Numbers outside their ranges mean what the header says."""
