@@ -406,7 +406,8 @@ bcq_status bcq_lora(const bcq_adapters *desc, const void *A, const void *B, cons
  *   pages     DEVICE [requests] rows of max_pages, in place (entries behind held_out are left as they are); free_pages DEVICE [num_pages], in place
  *   cached, fresh, held, fixed (or NULL: 0), kv_len, lack, held_out DEVICE [requests]; q_start DEVICE [requests + 1]
  *   positions, slots, owner DEVICE [tokens]: the rows of the batch, which may be more than there are
- * Negative numbers count as 0, held as no more than max_pages, fixed as no more than held.  page_size a power of two, at most 65536.
+ * Negative numbers count as 0, held as no more than max_pages, fixed as no more than held.  page_size a power of two, at most 65536.  What is written overlaps
+ * nothing else, but for held_out and free_count_out as said (lengths that an earlier step wrote go to `cached` as a copy if the same kv_len is written again).
  */
 typedef struct bcq_page_table {
     int32_t page_size, num_pages;

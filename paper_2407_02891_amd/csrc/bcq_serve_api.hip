@@ -198,10 +198,20 @@ bcq_status bcq_plan(const bcq_page_table *table, int32_t *pages, const int32_t *
     if (!free_pages || !free_count || !q_start || !free_count_out) return BCQ_ERR_INVALID_ARG;
     if (table->requests > 0 && (!pages || !held || !cached || !fresh || !kv_len || !lack || !held_out)) return BCQ_ERR_INVALID_ARG;
     if (tokens > 0 && (!positions || !slots || !owner)) return BCQ_ERR_INVALID_ARG;
-    for (const int32_t *p : {(const int32_t *)pages, held, fixed, (const int32_t *)free_pages, free_count, cached, fresh, (const int32_t *)q_start,
-                             (const int32_t *)kv_len, (const int32_t *)lack, (const int32_t *)held_out, (const int32_t *)free_count_out,
-                             (const int32_t *)positions, (const int32_t *)slots, (const int32_t *)owner})
-        if (!aligned(p, 4)) return BCQ_ERR_INVALID_ARG;
+    const struct { const int32_t *at; int64_t n; } read[] = {{fixed, table->requests}, {cached, table->requests}, {fresh, table->requests}, {held, table->requests}, {free_count, 1}},
+        written[] = {{pages, (int64_t)table->requests * table->max_pages}, {free_pages, table->num_pages}, {q_start, (int64_t)table->requests + 1}, {kv_len, table->requests},
+                     {lack, table->requests}, {positions, tokens}, {slots, tokens}, {owner, tokens}, {held_out, table->requests}, {free_count_out, 1}};
+    constexpr int kRead = sizeof(read) / sizeof(*read), kWritten = sizeof(written) / sizeof(*written);
+    const auto meet = [](auto &a, auto &b) { return a.at && b.at && a.n > 0 && b.n > 0 && (uintptr_t)a.at < (uintptr_t)(b.at + b.n) && (uintptr_t)b.at < (uintptr_t)(a.at + a.n); };
+    for (int i = 0; i < kRead; ++i)
+        if (!aligned(read[i].at, 4)) return BCQ_ERR_INVALID_ARG;
+    for (int i = 0; i < kWritten; ++i) {
+        if (!aligned(written[i].at, 4)) return BCQ_ERR_INVALID_ARG;
+        for (int j = 0; j < i; ++j)
+            if (meet(written[i], written[j])) return BCQ_ERR_INVALID_ARG;
+        for (int j = 0; j < kRead; ++j)  // (held and free_count may be the counts after the step)
+            if (meet(written[i], read[j]) && !(j >= kRead - 2 && i - j == kWritten - kRead && written[i].at == read[j].at)) return BCQ_ERR_INVALID_ARG;
+    }
     PlanArgs a{pages, held, fixed, free_pages, free_count, cached, fresh, q_start, kv_len, lack, held_out, free_count_out, positions, slots, owner,
                table->page_size, __builtin_ctz(table->page_size), table->num_pages, table->max_pages, table->requests, tokens};
     return launch_plan(a, static_cast<hipStream_t>(stream)) == hipSuccess ? BCQ_OK : BCQ_ERR_HIP;

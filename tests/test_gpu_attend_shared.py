@@ -95,6 +95,12 @@ def test_many_query_heads_share_one(q_heads, kv_heads, new):
     Shared([new] * 4, [100 + new, 177, 500, 101 + new], [(4, 100)], q_heads, kv_heads, 64, 16, "f16").check()
 
 
+@pytest.mark.parametrize("q_heads,kv_heads,D", [(300, 300, 64), (514, 257, 32), (300, 300, 256), (130, 130, 128), (1000, 500, 64)])
+def test_heads_that_fill_the_chip(q_heads, kv_heads, D):
+    Shared([1, 1, 1], [150, 90, 60], [(2, 80)], q_heads, kv_heads, D, 16, "bf16").check()
+    Shared([1, 20, 2], [150, 100, 60], [(3, 50)], q_heads, kv_heads, D, 16, "f16").check()
+
+
 @pytest.mark.parametrize("new", [1, 6])
 def test_long_prefix_is_split(new):
     Shared([new] * 5, [20011 + n for n in (7, 300, 64, 2000, 6)], [(5, 20011)], 4, 1, 128, 32, "f16").check()

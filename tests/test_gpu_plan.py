@@ -163,6 +163,26 @@ def test_a_graph_of_steps():
         length = [n + 1 for n in length]
 
 
+def test_the_lengths_of_an_earlier_step():
+    """kv_len of one step as `cached` of the next: with other tensors for what that writes; the same ones are refused, for they would be read after they are written."""
+    pool = Pool(5, 8, 30, 16, 3)
+    new = [5, 40, 0, 17, 30]
+    _, first = pool.step([0] * 5, new, 100)
+    with pytest.raises(bcq.BcqError):
+        pool.table.step(first["kv_len"], _ints([1] * 5), 100, out=first)
+    with pytest.raises(bcq.BcqError):
+        pool.table.step(_ints(new), first["lack"], 100, out=first)
+    with pytest.raises(bcq.BcqError):
+        pool.table.step(_ints(new), pool.table.held, 100)
+    with pytest.raises(bcq.BcqError):
+        pool.table.step(_ints(new), _ints(new), 100, out=dict(first, slots=first["positions"]))
+    args = (16, 30, 8, pool.pages, pool.held, pool.free, pool.count, new, [1] * 5, 100)
+    got = pool.table.step(first["kv_len"], _ints([1] * 5), 100)
+    ref = plan_ref(*args)
+    for n in STEP:
+        assert got[n].tolist() == ref[n], n
+
+
 def test_refusals():
     """Shapes, types and places that do not fit are refused before anything runs."""
     table = bcq.PageTable.empty(3, 4, 10, 16)

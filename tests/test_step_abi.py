@@ -14,9 +14,11 @@ OK = 0x1000
 def plan(t=(), **kw):
     d = dict(page_size=16, num_pages=1000, requests=8, max_pages=40)
     d.update(t)
-    a = dict(pages=OK, held=OK, fixed=OK, free=OK, free_count=OK, cached=OK, fresh=OK, tokens=8, q_start=OK, kv_len=OK, lack=OK, held_out=OK, count_out=OK,
-             positions=OK, slots=OK, owner=OK)
-    a.update(kw)
+    a = dict(pages=0, held=1, fixed=2, free=3, free_count=4, cached=5, fresh=6, tokens=8, q_start=7, kv_len=8, lack=9, held_out=1, count_out=4, positions=10,
+             slots=11, owner=12)
+    at = {n: OK + 0x10000 * i for n, i in a.items() if n != "tokens"}
+    a.update(at)
+    a.update({n: at[v[0]] + v[1] if isinstance(v, tuple) else v for n, v in kw.items()})
     return bcq.lib().bcq_plan(ctypes.byref(B.PageTableDesc(*d.values())), *a.values(), None)
 
 
@@ -30,6 +32,20 @@ def sample(**kw):
                                                                   "count_out", "positions", "slots", "owner") for v in (None, OK + 2)] + [dict(fixed=OK + 1)])
 def test_plan_refuses(kw):
     assert plan(**kw) == B.BCQ_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("a,b", [("kv_len", "cached"), ("kv_len", "fresh"), ("lack", "fixed"), ("pages", "held"), ("pages", "free"), ("q_start", "kv_len"), ("positions", "slots"),
+                                 ("owner", "positions"), ("free", "free_count"), ("held_out", "cached"), ("count_out", "held"), ("held_out", "count_out"),
+                                 ("owner", "fresh")])
+@pytest.mark.parametrize("by", [0, 28, -28])
+def test_plan_refuses_what_overlaps(a, b, by):
+    if by == 28 and b in ("free_count", "count_out") or by == -28 and a == "count_out":
+        by = 0                                             # (one number: its only overlap)
+    assert plan(**{a: (b, by)}) == B.BCQ_ERR_INVALID_ARG
+
+
+def test_plan_refuses_counts_that_begin_in_the_midst():
+    assert plan(held_out=("held", 4)) == plan(held_out=("held", -4)) == B.BCQ_ERR_INVALID_ARG
 
 
 @pytest.mark.parametrize("t", [dict(page_size=0), dict(page_size=-4), dict(num_pages=0), dict(requests=-1), dict(max_pages=0)])
