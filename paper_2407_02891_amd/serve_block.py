@@ -104,6 +104,13 @@ class Decoder:
         """block: AttentionBlock; embedding [vocabulary][hidden] binary16; head: PackedLayer of vocabulary by hidden; table: PageTable with nothing held,
         over the block's cache; sampler: Sampler, a row per request; adapter: of all requests (keys
         that are shared depend on it), any number outside the adapters': none."""
+        cache, longest = block.cache, table.pages.shape[1] * table.page_size
+        for holds, why in ((table.page_size == cache.desc.page_size and table.free.shape[0] <= cache.desc.num_pages, "a table of other pages than the cache's"),
+                           (block.cos_sin.shape[0] >= longest, f"a rotation table of less than {longest} positions"),
+                           (embedding.shape[0] >= head.desc.M, "an embedding of fewer tokens than the head's"),
+                           (sampler.temperature.shape[0] == table.pages.shape[0], "a sampler of another number of rows than requests")):
+            if not holds:
+                raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"Decoder ({why})")
         self.block, self.embedding, self.head, self.table, self.sampler, self.adapter = block, embedding, head, table, sampler, adapter
         self.count = table.pages.shape[0]
         self.cached, self.fresh, self.fixed, self.token = (torch.zeros(self.count, dtype=torch.int32, device=table.device) for _ in range(4))
@@ -254,7 +261,7 @@ def answers(a):
     longest = a.shared + a.prompt + a.requests + 2 * a.tokens + a.page
     width = -(-longest // a.page)
     own = a.requests * (-(-(longest - a.shared) // a.page) + 1)
-    block, _ = random_block(a.hidden, a.q_heads, a.kv_heads, a.head_dim, a.planes, width + own, a.page, longest, a.adapters, a.rank)
+    block, _ = random_block(a.hidden, a.q_heads, a.kv_heads, a.head_dim, a.planes, width + own, a.page, width * a.page, a.adapters, a.rank)
     embedding, head, _ = random_head(a.hidden, a.vocabulary, a.planes)
     table = PageTable.empty(a.requests, width, width + own, a.page)
     sampler = Sampler(torch.full((a.requests,), 0.8, device="cuda"), torch.full((a.requests,), 50, dtype=torch.int32, device="cuda"),

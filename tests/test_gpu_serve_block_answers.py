@@ -18,7 +18,7 @@ class Recorded:
     """A sampler that keeps what it was given and what it drew."""
 
     def __init__(self, sampler):
-        self.sampler, self.calls = sampler, []
+        self.sampler, self.temperature, self.calls = sampler, sampler.temperature, []
 
     def draw(self, logits, uniform):
         token, probability = self.sampler.draw(logits, uniform)
@@ -140,3 +140,15 @@ def test_prompts_that_do_not_fit(shared, own, message):
     decoder.prompt(list(range(34)), [[1], [2]], torch.full((2,), 0.5, device="cuda"))
     with pytest.raises(BcqError, match="begun"):
         decoder.prompt([], [[1], [2]], torch.full((2,), 0.5, device="cuda"))
+
+
+def test_parts_that_do_not_belong_together():
+    d, _, _, settings = _decoder(2, 4, 5)
+    table = lambda width=4, pool=5, page=PAGE, requests=2: PageTable.empty(requests, width, pool, page)  # noqa: E731
+    other = Sampler(*(t[:1].contiguous() for t in settings))
+    for parts in ((d.embedding, d.head, table(page=2 * PAGE), d.sampler.sampler), (d.embedding, d.head, table(pool=6), d.sampler.sampler),
+                  (d.embedding, d.head, table(width=5), d.sampler.sampler), (d.embedding[:-1], d.head, table(), d.sampler.sampler), (d.embedding, d.head, table(), other),
+                  (d.embedding, d.head, table(requests=3), d.sampler.sampler)):
+        with pytest.raises(BcqError, match="Decoder"):
+            Decoder(d.block, *parts, 0)
+    Decoder(d.block, d.embedding, d.head, table(width=3, pool=4), d.sampler.sampler, 0)
