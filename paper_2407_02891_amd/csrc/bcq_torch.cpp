@@ -274,6 +274,15 @@ at::Tensor add(PyObject *const *a)
     return out;
 }
 
+// Elements [from, from + n) of a contiguous tensor, as narrow gives them but without the dispatcher (six of them took 3 us of a step's 9).
+at::Tensor stretch(const at::Tensor &all, int64_t from, int64_t n)
+{
+    auto part = c10::make_intrusive<c10::TensorImpl>(c10::Storage(all.storage()), all.key_set(), all.dtype());
+    part->set_sizes_contiguous({n});
+    part->set_storage_offset(from);
+    return at::Tensor(std::move(part));
+}
+
 // step(desc, pages, held, fixed, free_pages, free_count, cached, fresh, tokens, trial, out, names, stream): a dict of the tensors that `names` names, in the order
 // of the entry point's arguments; those of `out`, or new ones.
 PyObject *step(PyObject *const *a)
@@ -322,7 +331,7 @@ PyObject *step(PyObject *const *a)
                 Py_INCREF(t);
                 to[i] = i == 3 ? held : free_count;
             } else {
-                const at::Tensor part = all.narrow(0, from, sizes[i]);
+                const at::Tensor part = stretch(all, from, sizes[i]);
                 from += (sizes[i] + 3) & ~int64_t(3);
                 to[i] = static_cast<int32_t *>(part.data_ptr());
                 t = THPVariable_Wrap(part);
