@@ -5,6 +5,7 @@
 // Bound by the matrix instructions (4 head_dim operations for a pair of row and key), and by the vector instructions of the softmax beside
 // them.  A workgroup has a tile of 128 rows ((new token, query head) pairs that share a kv head), 32 a wave, and walks the keys that any of
 // them sees.
+//  * What a tile does with its keys is in bcq_attend_tile.h.
 //  * Few tiles and many keys: the keys of a tile are cut into `parts`, whose sums a second launch joins.
 //
 // Measured: 2048 tokens over 8192 keys, 56 heads of 128, bfloat16: 434 us, 970 TFLOP/s, three quarters of what a large library product reaches; the matrix

@@ -5,7 +5,8 @@
 //
 // Everything is a sum over the requests before, so one workgroup does it, 1024 requests at a time: first the row starts and what is given back (the
 // taking may need it), then what is taken.  The pages themselves are moved by all threads, each finding the request of its page in the sums.
-// Bound by latency: a launch, and some ten reads in a row.
+// Bound by latency: a launch (3 us), and some ten steps in a row of 0.3 to 1 us each (loads, sums over the threads, lookups).  8 requests: the kernel 5 us.  1000 requests, 50 of which
+// give back 6000 pages, 7000 rows: 9.3, and 4 for a second launch that fills rows with many workgroups (up to 4096 rows the first fills them in at most as long).
 #include "bcq_internal.h"
 
 namespace bcq {
