@@ -52,7 +52,7 @@ struct SharedParams {
     const int *group_start, *shared_len;
     int groups, max_shared;
     Slot *slots;
-    int *sums;                 // three numbers for each slot
+    int *sums;                 // four numbers for each slot
     int num_slots, own_slots;  // the slots of requests' own keys begin at own_slots
     int few;                   // whether there may be requests of few rows, whose own keys are streamed
     long long space, own_place, few_place;  // rows that a kv head's sums have room for; where those of own keys' tiles begin, and of the other line
@@ -201,15 +201,17 @@ __device__ __forceinline__ void own_blocks(const SharedParams &p, Slot &q)
     (q.few ? q.few_upto : q.upto) = low < high ? (high + keys - 1) / keys - q.block : 0;
 }
 
-// Lays out the lines, all of THREADS threads: the blocks of each part's tiles, their sums, then what the slots hold.  upto, few_upto, owner: of each slot the two sums and whose it
-// is (bit 30 of a group's: a row of it does not see all keys).
+// Lays out the lines, all of THREADS threads: the blocks of each part's tiles, their sums, then what the slots hold.  numbers: four for each slot, its two sums, whose it is (bit 30 of a
+// group's: a row of it does not see all keys), and of a group's the first key that a row of it sees.
 template <int DT, int THREADS>
-__device__ __forceinline__ void lay_out(const SharedParams &p, int *upto, int *few_upto, int *owner, Slot *slots)
+__device__ __forceinline__ void lay_out(const SharedParams &p, int *numbers, Slot *slots)
 {
+    constexpr int KB = tile_keys(DT);
     __shared__ int sums[THREADS / 64][2];
     const AttendParams &a = p.a;
     const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6, n = p.num_slots;
-    for (int s = thread; s < n; s += THREADS) upto[s] = few_upto[s] = 0, owner[s] = -1;
+    int *const upto = numbers, *const few_upto = numbers + n, *const owner = numbers + 2 * n, *const first = numbers + 3 * n;
+    for (int s = thread; s < n; s += THREADS) upto[s] = few_upto[s] = 0, owner[s] = -1, first[s] = a.window == 0 ? 0 : 0x7fffffff;
     __syncthreads();
     // The parts, a thread each; what a thread has looked up of its first one it keeps.
     const int parts = p.groups + a.requests;
@@ -232,15 +234,22 @@ __device__ __forceinline__ void lay_out(const SharedParams &p, int *upto, int *f
         }
     });
     __syncthreads();
-    each_part([&](const Slot &q, int, int) {  // does each row of a request see all that is shared?
+    each_part([&](const Slot &q, int, int) {  // does each row of a request see all that is shared?  From where on, with a window?
         if (q.part < p.groups || q.requests < 0 || q.n == 0) return;
-        int unused, high;
-        visible_keys(a, q.n, q.len, 0, unused, high);
-        if (high >= q.from && q.rows == q.n * a.group) return;
-        const int first = start_of(p, first_of_group(p, q.requests)), rows = max(start_of(p, first_of_group(p, q.requests + 1)) - first, 0) * a.group;
-        const int s = slots_before(p, q.requests, first);
-        for (int i = 0; i * kChunkRows < rows && s + i < p.own_slots; ++i) atomicOr(owner + s + i, 1 << 30);
+        int low, high;
+        visible_keys(a, q.n, q.len, 0, low, high);
+        const bool all = high >= q.from && q.rows == q.n * a.group;
+        if (all && a.window == 0) return;
+        const int begin = start_of(p, first_of_group(p, q.requests)), rows = max(start_of(p, first_of_group(p, q.requests + 1)) - begin, 0) * a.group;
+        const int s = slots_before(p, q.requests, begin), row = (q.start - begin) * a.group;
+        for (int i = 0; i * kChunkRows < rows && s + i < p.own_slots; ++i) {
+            if (!all) atomicOr(owner + s + i, 1 << 30);
+            if (row < (i + 1) * kChunkRows && row + q.rows > i * kChunkRows) atomicMin(first + s + i, low);
+        }
     });
+    __syncthreads();
+    for (int s = thread; s < p.own_slots; s += THREADS)  // blocks in front of the first key that is seen
+        if (upto[s] > 0) upto[s] = first[s] < KB * upto[s] ? upto[s] - first[s] / KB : 0;
     __syncthreads();
     int before = 0, few_before = 0;
     for (int c = 0; c < n; c += THREADS) {
@@ -264,6 +273,7 @@ __device__ __forceinline__ void lay_out(const SharedParams &p, int *upto, int *f
             int unused;
             q = make_slot<DT>(p, owner[s] & ~(1 << 30), s, unused);
             if (q.part >= p.groups) own_blocks<DT>(p, q);
+            else q.block = min(first[s], q.to) / KB;
             if (owner[s] >> 30) q.n = 0;
         }
         q.upto = upto[s], q.few_upto = few_upto[s];
@@ -283,9 +293,8 @@ __device__ __forceinline__ void lay_out(const SharedParams &p, int *upto, int *f
 template <int DT>
 __global__ __launch_bounds__(kLineThreads) void bcq_attend_shared_line_kernel(SharedParams p)
 {
-    __shared__ int local[3 * kLocalSlots];
-    int *const sums = p.num_slots <= kLocalSlots ? local : p.sums;
-    lay_out<DT, kLineThreads>(p, sums, sums + p.num_slots, sums + 2 * p.num_slots, p.slots);
+    __shared__ int local[4 * kLocalSlots];
+    lay_out<DT, kLineThreads>(p, p.num_slots <= kLocalSlots ? local : p.sums, p.slots);
 }
 
 namespace {
@@ -543,8 +552,7 @@ __global__ __launch_bounds__(64 * kTileWaves, tile_occupancy(DT)) void bcq_atten
     SlotList<FUSED> slots{p.slots, p.num_slots};
     if constexpr (FUSED) {
         __shared__ Slot own[kFusedSlots];
-        int *const sums = reinterpret_cast<int *>(k0);  // (not in use yet)
-        lay_out<DT, 64 * kTileWaves>(p, sums, sums + p.num_slots, sums + 2 * p.num_slots, own);
+        lay_out<DT, 64 * kTileWaves>(p, reinterpret_cast<int *>(k0), own);  // (which is not in use yet)
         slots.at = own;
         if (blockIdx.x == 0)  // for the join
             for (int i = threadIdx.x; i < p.num_slots; i += 64 * kTileWaves) p.slots[i] = own[i];
@@ -786,7 +794,7 @@ SharedPlan shared_plan(const bcq_cache &c, int tokens, int requests, int groups,
     s.own_place = tiles;
     s.few_place = s.own_place + (s.few && (long long)max_new * group <= kFewRows ? 0 : tiles);
     s.space = s.few_place + (s.few ? rows + (long long)kFewRows * kTileWaves * s.workers : 0);
-    s.slot_bytes = (size_t)s.num_slots * (sizeof(Slot) + 3 * sizeof(int));
+    s.slot_bytes = (size_t)s.num_slots * (sizeof(Slot) + 4 * sizeof(int));
     s.slot_bytes = (s.slot_bytes + 15) / 16 * 16;
     s.part_bytes = (size_t)s.space * c.kv_heads * s.dim * sizeof(float);
     s.stat_bytes = (size_t)s.space * c.kv_heads * sizeof(f32x2);

@@ -95,6 +95,17 @@ def test_many_query_heads_share_one(q_heads, kv_heads, new):
     Shared([new] * 4, [100 + new, 177, 500, 101 + new], [(4, 100)], q_heads, kv_heads, 64, 16, "f16").check()
 
 
+@pytest.mark.parametrize("window", [1, 60, 301, 640, 1100, 5000])
+@pytest.mark.parametrize("D,dtype", [(64, "bf16"), (128, "f16"), (256, "bf16")])
+def test_windows_that_begin_behind_shared_keys(D, dtype, window):
+    # of a group's tiles each begins where the first of its rows does, some have nothing left; by lines laid out in the workgroups and, with many requests, before them
+    own = [1, 300, 640, 64, 900, 2, 30, 31]
+    Shared([1] * len(own), [1000 + n for n in own], [(len(own), 1000)], 64, 1, D, 16, dtype).check(True, window)
+    new = [3, 1, 1, 40] * 40
+    kv = [700 + n + (37 * i) % 900 for i, n in enumerate(new)]
+    Shared(new, kv, [(90, 700), (70, 513)], 8, 2, D, 16, dtype).check(True, window)
+
+
 @pytest.mark.parametrize("q_heads,kv_heads,D", [(300, 300, 64), (514, 257, 32), (300, 300, 256), (130, 130, 128), (1000, 500, 64)])
 def test_heads_that_fill_the_chip(q_heads, kv_heads, D):
     Shared([1, 1, 1], [150, 90, 60], [(2, 80)], q_heads, kv_heads, D, 16, "bf16").check()
