@@ -12,10 +12,10 @@
 //  * The lengths are on the device, so a first launch lays out the lines (up to kFusedSlots tiles each workgroup does it for itself).  A last one joins what was left of a row: of its shared
 //    keys and of its own.
 //
-// Measured, heads 64 / 8 of 128: 64 requests behind 8192 keys, 100 to 900 of their own (binary16): 50 us and 7.5 for the join; 256 behind 32768, 60 to 1500 of their own (bfloat16): 376, 10 for
+// Measured, heads 64 / 8 of 128: 64 requests behind 8192 keys, 100 to 900 of their own (binary16): 48.5 us and 7.5 for the join; 256 behind 32768, 60 to 1500 of their own (bfloat16): 376, 10 for
 // the line, 14 for the join, 680 TFLOP/s over all, the matrix pipes busy 42 % of the time.  Of that the shared keys by themselves take 300 (916 TFLOP/s), the own ones 141: beside each other
-// they wait for the same LDS and vector pipes.  All workgroups first with tiles, then with the other line: 412 for 404, and 69 for 57 of the 64.  56 heads with a kv head each, 32 requests behind
-// 4112: 78 and 5, 5.1 TB/s.
+// they wait for the same LDS and vector pipes.  All workgroups first with tiles, then with the other line: 412 for 404, and 69 for 57 of the 64 then.  56 heads with a kv head each, 32 requests behind
+// 4112: 79 and 5, 5.2 TB/s.
 #include "bcq_attend_tile.h"
 
 namespace bcq {
@@ -82,9 +82,23 @@ __device__ __forceinline__ int group_of(const SharedParams &p, int r)
 struct Cut {
     int total, middle, w0, w1;
     __device__ __forceinline__ Cut(int total, int others, int most0, int most1) : total(total), middle(total - others), w0(min(most0, max(middle, 1))), w1(min(most1, max(others, 1))) {}
-    __device__ __forceinline__ int begin(int piece) const { return piece < w0 ? first_block(piece, w0, middle) : middle + first_block(piece - w0, w1, total - middle); }
-    __device__ __forceinline__ int end(int piece) const { return piece < w0 ? first_block(piece + 1, w0, middle) : middle + first_block(piece - w0 + 1, w1, total - middle); }
-    __device__ __forceinline__ int piece_of(int block) const { return block < middle ? worker_of(block, w0, middle) : w0 + worker_of(block - middle, w1, total - middle); }
+    // (first_block and worker_of in binary64: the products are below 2^53, and quotients of integers that small do not round to the next one.  A division of 64-bit integers takes ten
+    // times as long, and a few of them one behind the other were 1 of the 5 us before a workgroup begins)
+    __device__ __forceinline__ int begin(int piece) const
+    {
+        const bool front = piece < w0;
+        return (front ? 0 : middle) + (int)((double)(front ? piece : piece - w0) * (front ? middle : total - middle) / (front ? w0 : w1));
+    }
+    __device__ __forceinline__ int end(int piece) const
+    {
+        const bool front = piece < w0;
+        return (front ? 0 : middle) + (int)((double)(front ? piece + 1 : piece - w0 + 1) * (front ? middle : total - middle) / (front ? w0 : w1));
+    }
+    __device__ __forceinline__ int piece_of(int block) const
+    {
+        const bool front = block < middle;
+        return (front ? 0 : w0) + (int)((((double)(front ? block : block - middle) + 1.0) * (front ? w0 : w1) - 1.0) / (front ? middle : total - middle));
+    }
 };
 
 // The first half of the workgroups has the line of tiles, the second the other; what of a line the other half helps with.  A workgroup takes 2.2 us for a tile's block, beside one that
