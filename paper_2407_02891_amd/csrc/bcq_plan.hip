@@ -5,9 +5,10 @@
 //
 // Everything is a sum over the requests before, so one workgroup does it, 1024 requests at a time: first the row starts and what is given back (the
 // taking may need it), then what is taken.  The pages themselves are moved by all threads, each finding the request of its page in the sums.
-// Bound by latency: a launch (3 us), and some ten steps in a row of 0.3 to 1 us each (loads, sums over the threads, lookups).  8 requests: the kernel 5 us.  1000 requests, 50 of which
-// give back 6000 pages, 7000 rows: 9.3, and 4 for a second launch that fills rows with many workgroups (up to 4096 rows the first fills them in at most as long).
+// Bound by latency: a launch (3 us), and some ten steps in a row of 0.3 to 1 us each (loads, sums over the threads, lookups).  8 requests: the kernel 4.3 us.  1000 requests, 50 of which
+// give back 6000 pages, 7000 rows: 8.5, and 4 for a second launch that fills rows with many workgroups (up to 4096 rows the first fills them in at most as long).
 #include "bcq_internal.h"
+#include "bcq_lanes.h"
 
 namespace bcq {
 
@@ -19,17 +20,6 @@ constexpr int kFillThreads = 256;
 constexpr int kAtOnce = 4;
 
 typedef long long i64;
-
-template <class T>
-__device__ __forceinline__ T sum_upto(T v, int lane)
-{
-#pragma unroll
-    for (int step = 1; step < 64; step <<= 1) {
-        const T below = __shfl_up(v, step);
-        if (lane >= step) v += below;
-    }
-    return v;
-}
 
 // Sum over the threads up to and with this one; `all`: over all of them.  `shared`: kWaves, free again after the next barrier.
 template <class T>

@@ -18,6 +18,7 @@
 
 #include "bcq_half.h"
 #include "bcq_internal.h"
+#include "bcq_lanes.h"
 
 namespace bcq {
 
@@ -105,42 +106,6 @@ struct Weigh {
     }
 };
 
-__device__ __forceinline__ double from_lane(double v, int lane)
-{
-    const u64 b = __builtin_bit_cast(u64, v);
-    return __builtin_bit_cast(double, (u64)(uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)b, lane));
-}
-__device__ __forceinline__ int from_lane(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
-
-template <int CTRL>
-__device__ __forceinline__ int in_row(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
-template <int CTRL>
-__device__ __forceinline__ double in_row(double v)
-{
-    const u64 b = __builtin_bit_cast(u64, v);
-    return __builtin_bit_cast(double, (u64)(uint32_t)in_row<CTRL>((int)(b >> 32)) << 32 | (uint32_t)in_row<CTRL>((int)b));
-}
-
-// Sum over the lanes up to and with this one: in rows of sixteen by shifts, then the rows before.
-template <class T>
-__device__ __forceinline__ T sum_upto(T v, int lane)
-{
-    v += in_row<0x111>(v);
-    v += in_row<0x112>(v);
-    v += in_row<0x114>(v);
-    v += in_row<0x118>(v);
-    const T r0 = from_lane(v, 15), r1 = r0 + from_lane(v, 31), r2 = r1 + from_lane(v, 47);
-    return v + (lane < 32 ? lane < 16 ? T(0) : r0 : lane < 48 ? r1 : r2);
-}
-template <class T>
-__device__ __forceinline__ T sum_all(T v)
-{
-    v += in_row<0x111>(v);
-    v += in_row<0x112>(v);
-    v += in_row<0x114>(v);
-    v += in_row<0x118>(v);
-    return from_lane(v, 15) + from_lane(v, 31) + (from_lane(v, 47) + from_lane(v, 63));
-}
 __device__ __forceinline__ u64 least_of_all(u64 v)
 {
 #pragma unroll
