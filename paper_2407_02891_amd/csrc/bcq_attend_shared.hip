@@ -17,6 +17,7 @@
 // they wait for the same LDS and vector pipes.  All workgroups first with tiles, then with the other line: 412 for 404, and 69 for 57 of the 64 then.  56 heads with a kv head each, 32 requests behind
 // 4112: 79 and 5, 5.2 TB/s.
 #include "bcq_attend_tile.h"
+#include "bcq_lanes.h"
 
 namespace bcq {
 
@@ -268,7 +269,7 @@ __device__ __forceinline__ void lay_out(const SharedParams &p, int *numbers, Slo
     int before = 0, few_before = 0;
     for (int c = 0; c < n; c += THREADS) {
         const int s = c + thread;
-        const int tiles = prefix_sum(s < n ? upto[s] : 0, lane), few = prefix_sum(s < n ? few_upto[s] : 0, lane);
+        const int tiles = sum_upto(s < n ? upto[s] : 0, lane), few = sum_upto(s < n ? few_upto[s] : 0, lane);
         if (lane == 63) sums[wave][0] = tiles, sums[wave][1] = few;
         __syncthreads();
         int mine = before + tiles, few_mine = few_before + few;
