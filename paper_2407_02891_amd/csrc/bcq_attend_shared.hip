@@ -12,8 +12,8 @@
 //  * The lengths are on the device, so a first launch lays out the lines (up to kFusedSlots tiles each workgroup does it for itself).  A last one joins what was left of a row: of its shared
 //    keys and of its own.
 //
-// Measured, heads 64 / 8 of 128: 64 requests behind 8192 keys, 100 to 900 of their own (binary16): 48.5 us and 7.5 for the join; 256 behind 32768, 60 to 1500 of their own (bfloat16): 376, 10 for
-// the line, 14 for the join, 680 TFLOP/s over all, the matrix pipes busy 42 % of the time.  Of that the shared keys by themselves take 300 (916 TFLOP/s), the own ones 141: beside each other
+// Measured, heads 64 / 8 of 128: 64 requests behind 8192 keys, 100 to 900 of their own (binary16): 48.5 us and 7.5 for the join; 256 behind 32768, 60 to 1500 of their own (bfloat16): 376, 7 for
+// the line, 14 for the join, 700 TFLOP/s over all, the matrix pipes busy 42 % of the time.  Of that the shared keys by themselves take 300 (916 TFLOP/s), the own ones 141: beside each other
 // they wait for the same LDS and vector pipes.  All workgroups first with tiles, then with the other line: 412 for 404, and 69 for 57 of the 64 then.  56 heads with a kv head each, 32 requests behind
 // 4112: 79 and 5, 5.2 TB/s.
 #include "bcq_attend_tile.h"
