@@ -102,8 +102,8 @@ class Decoder:
 
     def __init__(self, block, embedding, head, table, sampler, adapter):
         """block: AttentionBlock; embedding [vocabulary][hidden] binary16; head: PackedLayer of vocabulary by hidden; table: PageTable with nothing held,
-        over the block's cache; sampler: Sampler, a row per request; adapter: of all requests (keys
-        that are shared depend on it), any number outside the adapters': none."""
+        over the block's cache; sampler: Sampler, a row per request; adapter: of all requests (keys that are shared depend on it), any number outside
+        the adapters': none."""
         cache, longest = block.cache, table.pages.shape[1] * table.page_size
         for holds, why in ((table.page_size == cache.desc.page_size and table.free.shape[0] <= cache.desc.num_pages, "a table of other pages than the cache's"),
                            (block.cos_sin.shape[0] >= longest, f"a rotation table of less than {longest} positions"),
@@ -124,7 +124,8 @@ class Decoder:
                                self.shared)
 
     def _next(self, z, plan, uniform):
-        """Each request's next token from its last row, where it had one and the pages for it; else its token stays, and the step can be made again."""
+        """Each request's next token from its last row, where it had one and the pages for it; without the pages the step can be made again.  (A token also
+        stays where no logit is a number.)"""
         last = (plan["q_start"][1:] - 1).clamp(min=0).long()
         token, probability = self.sampler.draw(product(self.head, z[last]), uniform)
         ready = (plan["lack"] == 0) & (self.fresh > 0) & (token >= 0)

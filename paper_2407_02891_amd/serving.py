@@ -131,7 +131,7 @@ class PageTable:
     def step(self, cached, fresh, tokens, fixed=None, out=None, trial=False):
         """bcq_plan: cached[r] tokens of request r are in the cache, fresh[r] more come with a batch of `tokens` rows (int32 [requests]); the first fixed[r] pages of a
         row are not its own.  Returns a dict of q_start, kv_len, lack, held, free_count, positions, slots, owner (`out`: one that an earlier step returned, whose
-        tensors are written again).  held and free_count are the table's own and move with the step.  With `trial` they stay, and those that the step would leave are
+        tensors are written again: none of them may be cached, fresh or fixed).  held and free_count are the table's own and move with the step.  With `trial` they stay, and those that the step would leave are
         tensors of their own: what a step would take and who would lack pages, before it is made (entries of `pages` behind held, and of `free` behind free_count,
         are scratch)."""
         return self._native.step(self._desc, self.pages, self.held, fixed, self.free, self.free_count, cached, fresh, tokens, trial, out, self.STEP,
