@@ -85,19 +85,21 @@ __device__ __forceinline__ void first_beyond(const int *upto, const int (&k)[N],
 
 // move(k, request, which of its pages) in two halves, for k = 0 .. all - 1 pages of requests whose sums are `upto`: all threads, kAtOnce each at a time, since each waits for what it
 // finds and then for what it loads (1000 requests of which 50 give back 6000 pages: 13.9 us a call, 15.7 with one at a time; 24 that take 7000: 11.4 and 15.0).
+// (k counts in unsigned numbers: 1024 requests may have up to 2^31 - 1 pages, and a signed k would wrap to negative places before it has passed them.)
 template <class LOAD, class STORE>
 __device__ __forceinline__ void move_pages(const int *upto, int all, LOAD load, STORE store)
 {
-    for (int k0 = threadIdx.x; k0 < all; k0 += kAtOnce * kThreads) {
+    const unsigned pages = all;
+    for (unsigned k0 = threadIdx.x; k0 < pages; k0 += kAtOnce * kThreads) {
         int k[kAtOnce], i[kAtOnce], page[kAtOnce];
 #pragma unroll
-        for (int n = 0; n < kAtOnce; ++n) k[n] = min(k0 + n * kThreads, all - 1);
+        for (int n = 0; n < kAtOnce; ++n) k[n] = (int)min(k0 + n * kThreads, pages - 1);
         first_beyond(upto, k, i);
 #pragma unroll
         for (int n = 0; n < kAtOnce; ++n) page[n] = load(k[n], i[n], k[n] - (i[n] ? upto[i[n] - 1] : 0));
 #pragma unroll
         for (int n = 0; n < kAtOnce; ++n)
-            if (k0 + n * kThreads < all) store(k[n], i[n], k[n] - (i[n] ? upto[i[n] - 1] : 0), page[n]);
+            if (k0 + n * kThreads < pages) store(k[n], i[n], k[n] - (i[n] ? upto[i[n] - 1] : 0), page[n]);
     }
 }
 
