@@ -293,6 +293,8 @@ PyObject *step(PyObject *const *a)
     const Place place{at::kInt, pages.device(), where};
     const c10::DeviceGuard there(place.device);
     const int64_t R = d->requests, T = int32(a[8], where, "tokens");
+    if (pages.dim() != 2 || pages.size(0) != R || pages.size(1) != d->max_pages || pages.scalar_type() != at::kInt || !pages.is_contiguous())
+        refuse(where, "pages: contiguous int32 [" + std::to_string(R) + "][" + std::to_string(d->max_pages) + "], as the table was made with");
     if (T < 0) refuse(where, "tokens: negative");
     int32_t *const held = place.vector<int32_t>(a[2], "held", R, at::kInt), *const fixed = place.vector<int32_t>(a[3], "fixed", R, at::kInt);
     int32_t *const free_pages = place.vector<int32_t>(a[4], "free", d->num_pages, at::kInt), *const free_count = place.vector<int32_t>(a[5], "free_count", 1, at::kInt);
