@@ -152,6 +152,20 @@ int64_t head_dim(const bcq_cache &c, const char *where)
     return c.head_dim;
 }
 
+at::ScalarType of(int32_t dtype) { return dtype == BCQ_BF16 ? at::kBFloat16 : at::kHalf; }
+
+// k and v lie as the descriptor says that they do (a program may have put others in their place).
+void check_cache(const bcq_cache &c, const at::Tensor &k, const at::Tensor &v, const char *where)
+{
+    const int64_t sizes[4] = {c.num_pages, c.kv_heads, c.page_size, c.head_dim}, strides[4] = {c.page_stride, c.head_stride, c.slot_stride, 1};
+    bool same = k.device() == v.device();
+    for (const at::Tensor *t : {&k, &v}) {
+        same = same && t->dim() == 4 && t->scalar_type() == of(c.dtype);
+        for (int i = 0; same && i < 4; ++i) same = t->size(i) == sizes[i] && (t->stride(i) == strides[i] || sizes[i] <= 1);
+    }
+    if (!same) refuse(where, "k, v: shape, strides and type that the cache was made with");
+}
+
 // rotate(desc, k, v, qkv, positions, cos_sin, slots, q_weight, k_weight, eps, interleaved, out, stream)
 at::Tensor rotate(PyObject *const *a)
 {
@@ -160,6 +174,7 @@ at::Tensor rotate(PyObject *const *a)
     const at::Tensor &k = tensor(a[1], where, "k"), &v = tensor(a[2], where, "v"), &qkv = tensor(a[3], where, "qkv");
     const Place place{k.scalar_type(), k.device(), where};
     const c10::DeviceGuard there(place.device);  // (launches go to the current device)
+    check_cache(*c, k, v, where);
     const int64_t D = head_dim(*c, where);
     if (qkv.dim() != 2 || qkv.size(1) % D || qkv.size(1) / D <= 2 * (int64_t)c->kv_heads)
         refuse(where, "qkv: [tokens][heads * head_dim], at least one q head before the k and v heads");
@@ -197,6 +212,7 @@ struct Attended {
         : cache(address<const bcq_cache>(a[0])), place{tensor(a[1], where, "k").scalar_type(), tensor(a[1], where, "k").device(), where}, k(tensor(a[1], where, "k")),
           v(tensor(a[2], where, "v")), q(tensor(a[3], where, "q")), pages(tensor(a[6], where, "pages"))
     {
+        check_cache(*cache, k, v, where);
         const int64_t D = head_dim(*cache, where);
         if (q.dim() != 2 || q.size(1) % D) refuse(where, "q: [tokens][q_heads * head_dim]");
         if (pages.dim() != 2 || pages.scalar_type() != at::kInt || pages.device() != place.device || !pages.is_contiguous())
@@ -260,6 +276,10 @@ at::Tensor add(PyObject *const *a)
     const at::Tensor &A = tensor(a[1], where, "A"), &B = tensor(a[2], where, "B"), &X = tensor(a[5], where, "X"), &base = tensor(a[7], where, "base");
     const Place place{A.scalar_type(), A.device(), where};
     const c10::DeviceGuard there(place.device);
+    if (A.dim() != 3 || A.size(0) != d->count || A.size(1) != d->max_rank || A.size(2) != d->N || B.dim() != 3 || B.size(0) != d->count || B.size(1) != d->M ||
+        B.size(2) != d->max_rank || A.scalar_type() != of(d->dtype) || B.scalar_type() != A.scalar_type() || !A.is_contiguous() || !B.is_contiguous() ||
+        B.device() != A.device())
+        refuse(where, "A, B: shape and type that the adapters were made with, contiguous");
     if (X.dim() != 2 || X.size(0) > INT32_MAX) refuse(where, "X: [tokens][N]");
     const int64_t T = X.size(0), ldx = place.rows(X, "X", T, d->N), ld_base = place.rows(base, "base", T, d->M);
     const int32_t *const adapter = place.ints(a[6], "adapter", T);
