@@ -358,8 +358,12 @@ PyObject *step(PyObject *const *a)
                 to[i] = static_cast<int32_t *>(part.data_ptr());
                 t = THPVariable_Wrap(part);
             }
-            if (t) PyDict_SetItem(out, PyTuple_GET_ITEM(names, i), t);
+            const bool put = t && PyDict_SetItem(out, PyTuple_GET_ITEM(names, i), t) == 0;
             Py_XDECREF(t);
+            if (!put) {  // (Python's own error stands)
+                Py_DECREF(out);
+                throw Refused{-1, ""};
+            }
         }
     }
     const bcq_status status = g_bcq.plan(d, static_cast<int32_t *>(pages.data_ptr()), held, fixed, free_pages, free_count, cached, fresh, (int32_t)T, to[0], to[1],

@@ -1,4 +1,4 @@
-"""Tensors that an object holds and a program has put others in the place of: a call looks at them as at its arguments, for their sizes are in the descriptor that the
+"""What native calls look at beside their arguments.  Tensors that an object holds and a program has put others in the place of: a call looks at them as at its arguments, for their sizes are in the descriptor that the
 object was made with (no GPU needed: all of it is refused before anything is launched)."""
 import ctypes
 
@@ -22,6 +22,23 @@ def test_pages_of_a_table(other):
     desc = B.PageTableDesc(16, 10, 3, 4)
     free, count = torch.zeros(10, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
     _refused(lambda: serving._load().step(ctypes.addressof(desc), other(pages), i, None, free, count, i.clone(), i.clone(), 5, False, None, bcq.PageTable.STEP, 0), "pages:")
+
+
+def test_a_result_that_cannot_be_named():
+    """An error of Python's on the way to a step's dict ends the call there, before the step is made."""
+    class Name(str):
+        asked = 0
+
+        def __hash__(self):
+            Name.asked += 1
+            raise MemoryError("no dict")
+
+    pages, i = torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    desc = B.PageTableDesc(16, 10, 3, 4)
+    free, count = torch.zeros(10, dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(MemoryError, match="no dict"):
+        serving._load().step(ctypes.addressof(desc), pages, i, None, free, count, i.clone(), i.clone(), 5, False, None, tuple(Name(n) for n in bcq.PageTable.STEP), 0)
+    assert Name.asked == 1
 
 
 def _ids(*v):
