@@ -146,6 +146,8 @@ class Decoder:
         pages = [-(-len(ids) // page) for ids in rest]
         if len(own) != self.count or not all(own):
             raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"{where} (one id or more of each of the {self.count} requests)")
+        if any(ids and not 0 <= min(ids) <= max(ids) < self.embedding.shape[0] for ids in [shared] + own):
+            raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"{where} (ids of 0 to {self.embedding.shape[0] - 1}, the embedding's)")
         if bool((self.cached + self.table.held).any()):
             raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"{where} (requests that have begun)")
         if whole // page + max(pages) > self.table.pages.shape[1] or whole // page + sum(pages) > int(self.table.free_count):
