@@ -108,6 +108,8 @@ class Decoder:
         for holds, why in ((table.page_size == cache.desc.page_size and table.free.shape[0] <= cache.desc.num_pages, "a table of other pages than the cache's"),
                            (block.cos_sin.shape[0] >= longest, f"a rotation table of less than {longest} positions"),
                            (embedding.shape[0] >= head.desc.M, "an embedding of fewer tokens than the head's"),
+                           (embedding.dtype == torch.float16 and embedding.shape[1] == block.qkv.desc.N, f"an embedding that is not binary16 of {block.qkv.desc.N} a token"),
+                           (head.desc.N == block.o.desc.M, f"a head of other than {block.o.desc.M} inputs"),
                            (sampler.temperature.shape[0] == table.pages.shape[0], "a sampler of another number of rows than requests")):
             if not holds:
                 raise B.BcqError(B.BCQ_ERR_INVALID_ARG, f"Decoder ({why})")

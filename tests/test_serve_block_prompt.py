@@ -42,3 +42,16 @@ def test_ids_that_are_not_the_embeddings(shared, own):
 def test_the_first_and_the_last_id(shared, own):
     with pytest.raises(RuntimeError, match="a step is made"):
         Decoder(**_parts()).prompt(shared, own, torch.full((2,), 0.5))
+
+
+@pytest.mark.parametrize("change", [dict(embedding=torch.zeros((VOCABULARY, HIDDEN))), dict(embedding=torch.zeros((VOCABULARY, HIDDEN), dtype=torch.bfloat16)),
+                                    dict(embedding=torch.zeros((VOCABULARY, HIDDEN + 128), dtype=torch.float16)),
+                                    dict(embedding=torch.zeros((VOCABULARY, HIDDEN // 2), dtype=torch.float16)),
+                                    dict(head=SimpleNamespace(desc=SimpleNamespace(M=VOCABULARY, N=HIDDEN // 2))),
+                                    dict(head=SimpleNamespace(desc=SimpleNamespace(M=VOCABULARY, N=2 * HIDDEN)))])
+def test_an_embedding_or_a_head_of_another_type_or_width(change):
+    """The products take an address and a row stride: another type was read as binary16, and a wider row's end was left out."""
+    Decoder(**_parts())
+    with pytest.raises(bcq.BcqError, match="Decoder") as e:
+        Decoder(**dict(_parts(), **change))
+    assert e.value.status == B.BCQ_ERR_INVALID_ARG
