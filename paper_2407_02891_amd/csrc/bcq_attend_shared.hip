@@ -104,6 +104,9 @@ struct Cut {
 
 // The first half of the workgroups has the line of tiles, the second the other; what of a line the other half helps with.  A workgroup takes 2.2 us for a tile's block, beside one that
 // streams or another of its kind (1.5 alone), and 0.9 for four waves' blocks of the other line; to begin with tiles costs as much as two of their blocks.
+// Where nothing is streamed the second half has that much less all the same: the end of the line is requests' own keys, whose tiles begin anew every block or two.  Even pieces took 40.0 us
+// for 33.5 (16 requests behind 4096 keys, heads of 256), 29.4 for 25.7 (40 query heads to a kv head); 26.0 for 27.5 with fewer blocks than that (8 behind 1500, heads of 256), and for
+// chunks 402 for 408 and 785 for 780.
 struct Cuts {
     Cut tiles, few;
     __device__ __forceinline__ Cuts(int half, int rest, int tiles, int few)
