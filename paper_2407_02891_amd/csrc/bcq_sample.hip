@@ -14,8 +14,6 @@
 // Bound by one compute unit's steps in a row.  64 rows of 131072: 26.5 us, of which 10 count (64 additions to LDS take 4 clocks, at random addresses 7.5), 1.5 sum the counts, 0.8 find the
 // largest, 1.9 weigh, 4.4 search the borders, 3.8 find the entry.  One row of 32000: 12.5.  Rows of four chunks kept in registers, and 512 threads, were slower; for the entry, a stretch of the
 // row for each wave without a barrier a chunk gained 1 us with 64 rows and lost 1 with 256.
-#include <utility>
-
 #include "bcq_half.h"
 #include "bcq_internal.h"
 #include "bcq_lanes.h"
@@ -146,29 +144,22 @@ struct Chunk {
 };
 __device__ __forceinline__ int chunks_of(const uint16_t *row, int vocab) { return (vocab + in_front(row) + kChunk - 1) / kChunk; }
 
-// A row's chunks, which stay in registers where they are at most KEPT (not 0).
-template <int KEPT>
+// A row's chunks.  KEPT: there is one, which stays in registers.
+template <bool KEPT>
 struct Row {
     const uint16_t *row;
     int vocab, chunks;
-    Chunk kept[KEPT ? KEPT : 1];
+    Chunk kept;
     __device__ __forceinline__ Row(const uint16_t *row, int vocab) : row(row), vocab(vocab), chunks(chunks_of(row, vocab))
     {
-        if (KEPT)
-#pragma unroll
-            for (int c = 0; c < KEPT; ++c) kept[c].load(row, c, vocab);
-    }
-    template <class F, int... C>
-    __device__ __forceinline__ void in_turn(F use, std::integer_sequence<int, C...>) const
-    {
-        (void)(... || (C >= chunks || use(kept[C], C + 1 < chunks)));
+        if (KEPT) kept.load(row, 0, vocab);
     }
     // use(chunk, whether there are more) for one after the other, until it returns true.
     template <class F>
     __device__ __forceinline__ void each(F use) const
     {
-        if constexpr (KEPT > 0) {
-            in_turn(use, std::make_integer_sequence<int, KEPT>());
+        if constexpr (KEPT) {
+            use(kept, false);
         } else {
             Chunk next;
             int c = 0;
@@ -248,7 +239,7 @@ struct Shared {
 };
 
 // The first entry of the largest value: place << 32 | index, all ones if there is none.  All threads get it.
-template <bool BF, int KEPT>
+template <bool BF, bool KEPT>
 __device__ __forceinline__ u64 first_of_largest(const Row<KEPT> &row, Shared &sh)
 {
     u64 best = ~0ull;
@@ -285,7 +276,7 @@ __device__ __forceinline__ u64 first_of_largest(const Row<KEPT> &row, Shared &sh
 }
 
 // How often each value occurs: the counters of magnitude m are in word m.  careful (of rows of more than a chunk): none passes 16 bits.
-template <bool BF, int KEPT>
+template <bool BF, bool KEPT>
 __device__ __forceinline__ void count_values(const Row<KEPT> &row, uint32_t *table, Shared &sh, bool careful)
 {
     const int lane = threadIdx.x & 63;
@@ -566,7 +557,7 @@ __device__ __forceinline__ bool draw(const SampleParams &p, int row, const Count
 }
 
 // The drawn entry: its piece, in the order of pieces, chunk after chunk.
-template <int KEPT>
+template <bool KEPT>
 __device__ __forceinline__ void find_entry(const SampleParams &p, int row, const Row<KEPT> &logits, Shared &sh)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -610,7 +601,7 @@ static_assert(kPieces * kWaves == 64, "");
 
 }  // namespace
 
-template <bool BF, int KEPT>
+template <bool BF, bool KEPT>
 __global__ __launch_bounds__(kThreads) void bcq_sample_kernel(SampleParams p)
 {
     __shared__ __attribute__((aligned(16))) uint32_t table[32768];
@@ -625,7 +616,7 @@ __global__ __launch_bounds__(kThreads) void bcq_sample_kernel(SampleParams p)
     // A counter that passes 16 bits loses 65535 or 65536 entries each time, so the sum of all tells whether any did.  Then (half of the first 131072 entries alike, say) they are counted again,
     // with a look at every counter between chunks.  (64 rows of 131072: 26.9 us, with that look in the first place 29.6.)
     const int lane = threadIdx.x & 63, met = (p.vocab + in_front(logits.row) + 8 * kThreads - 1) / (8 * kThreads) * (8 * kThreads);
-    bool careful = KEPT > 0;
+    bool careful = KEPT;
 #pragma unroll 1
     for (;; careful = true) {
         count_values<BF>(logits, table, sh, careful);
@@ -641,8 +632,8 @@ namespace {
 template <bool BF>
 void sample(const SampleParams &p, int rows, hipStream_t s)
 {
-    if (p.vocab + 7 <= kChunk) bcq_sample_kernel<BF, 1><<<rows, kThreads, 0, s>>>(p);
-    else bcq_sample_kernel<BF, 0><<<rows, kThreads, 0, s>>>(p);
+    if (p.vocab + 7 <= kChunk) bcq_sample_kernel<BF, true><<<rows, kThreads, 0, s>>>(p);
+    else bcq_sample_kernel<BF, false><<<rows, kThreads, 0, s>>>(p);
 }
 
 }  // namespace
