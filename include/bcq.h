@@ -352,8 +352,11 @@ bcq_status bcq_attend(const bcq_cache *cache, const void *k_cache, const void *v
  * weights rounded as in its chunks.  Positions, masks, rows that see nothing and rows of nobody as for bcq_attend.
  *   group_start DEVICE [groups + 1], rising; requests outside of all groups share nothing.  shared_len DEVICE [groups], any number of keys (no whole pages
  *               needed), bounded to 0 .. max_shared: keys behind that are taken as each request's own
- *   workspace   DEVICE, bcq_attend_shared_workspace_bytes(...) bytes, 16-byte aligned; scratch, no init, used by one call at a time
- * The other arguments as for bcq_attend.  tokens = 0 or requests = 0 launches nothing.
+ *   workspace   DEVICE, bcq_attend_shared_workspace_bytes(...) bytes, 16-byte aligned; scratch, no init, used by one call at a time.  It holds the binary32 sums of
+ *               each row of q two or three times (shared keys, own keys, and those of requests of up to 16 rows where there may be some): 55 MB for 64 single tokens of 64
+ *               heads of 128, 1.7 GB for 16384 tokens in chunks.  Long prompts are cut into calls accordingly.
+ * The other arguments as for bcq_attend; tokens times q_heads times head_dim (as 64, 128 or 256) up to 2^34, BCQ_ERR_UNSUPPORTED beyond.  tokens = 0 or requests = 0
+ * launches nothing.
  */
 size_t bcq_attend_shared_workspace_bytes(const bcq_cache *cache, int32_t tokens, int32_t requests, int32_t groups, int32_t q_heads, int32_t max_pages,
                                          int32_t max_new);
