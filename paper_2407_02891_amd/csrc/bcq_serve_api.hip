@@ -131,7 +131,7 @@ static bcq_status attend_shared_shape(const bcq_cache *cache, int32_t tokens, in
     if (groups < 0) return BCQ_ERR_INVALID_ARG;
     if (groups > kMaxTokens) return BCQ_ERR_UNSUPPORTED;
     const int64_t rows = (int64_t)tokens * (q_heads / cache->kv_heads), row_lanes = cache->head_dim <= 64 ? 16 : cache->head_dim <= 128 ? 32 : 64;
-    if ((rows * row_lanes + 256) * cache->kv_heads > 0xffffffffLL) return BCQ_ERR_UNSUPPORTED;  // the threads of a launch, of the join's a row's elements by four
+    if ((rows * row_lanes + 256) * cache->kv_heads > 0xffffffffLL) return BCQ_ERR_UNSUPPORTED;  // threads of the join's launch, four elements of a row each
     const int64_t tiles = 2 * rows / 128 + groups + requests + 1;
     return tiles * (max_pages * (int64_t)cache->page_size / 32 + 1) > 0x7fffffffLL ? BCQ_ERR_UNSUPPORTED : BCQ_OK;  // blocks of keys of all tiles are int
 }

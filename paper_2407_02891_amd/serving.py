@@ -73,7 +73,7 @@ class PagedCache:
 
     def attend_shared(self, q, q_start, kv_len, pages, max_new, group_start, shared_len, max_shared, scale=None, causal=True, window=0, out=None):
         """bcq_attend_shared: attend, for requests of which group c, group_start[c] .. group_start[c+1] - 1, share their first shared_len[c] keys (at most max_shared):
-        those are taken from the first one's pages and read once.  group_start int32 [groups + 1], shared_len int32 [groups].  Single tokens and drafts gain where that saves some 16000 keys or
+        those are taken from the first one's pages and read once.  group_start int32 [groups + 1], shared_len int32 [groups].  Single tokens gain where that saves some 16000 keys or
         more ((requests - 1) * shared_len) of prefixes of 2048 and more; for chunks, and for less, attend with the pages in every row is faster."""
         return self._native.attend_shared(self._desc, self.k, self.v, q, q_start, kv_len, pages, max_new, group_start, shared_len, max_shared,
                                           self.head_dim ** -0.5 if scale is None else scale, causal, window, out, B.raw_stream(self._index))
